@@ -463,6 +463,153 @@ int qg_conv_dense_u8s8_requant(const uint8_t* in_nhwc, int Nb, int H, int W, int
                                int pad, int stride, const qg_packed_b* Wp, const qg_requant_params* p,
                                uint8_t* out_nhwc, void* stream, int kernel);
 
+/* ---- positions, the 4-bit key/value cache and the attention over it --------- */
+
+/* Element types of the floating-point tensors below.  All arithmetic is fp32
+ * (or wider) whatever the type; a result is rounded to its type once. */
+#define QG_F32 0
+#define QG_BF16 1
+#define QG_F16 2
+
+/* A tensor [tokens][heads][head_dim] with unit channel stride; strides count
+ * elements, any sign, any alignment that the element type has by itself. */
+typedef struct {
+  void* data;             /* dev                     */
+  int64_t token_stride;
+  int64_t head_stride;
+} qg_heads;
+
+/* Rotation angles.  Pair i of rot / 2 turns at f_i = base^(-2 i / rot) per
+ * position, changed for contexts longer than the model was trained for:
+ *   QG_ROPE_PLAIN     f_i
+ *   QG_ROPE_LINEAR    f_i / factor (positions interpolated)
+ *   QG_ROPE_BY_INDEX  f_i * (1 - w) + f_i / factor * w, w rising linearly with i
+ *                     from the pair that makes `high` turns in `context` positions
+ *                     to the one that makes `low`
+ *   QG_ROPE_BY_TURNS  the same with w falling linearly with the number of turns
+ *                     t_i = context * f_i / (2 pi) itself, 0 from `high` turns up
+ *                     and 1 up to `low`
+ * The cosines and sines are multiplied by `magnitude`. */
+#define QG_ROPE_PLAIN 0
+#define QG_ROPE_LINEAR 1
+#define QG_ROPE_BY_INDEX 2
+#define QG_ROPE_BY_TURNS 3
+typedef struct {
+  double base;            /* > 1                                              */
+  double factor;          /* >= 1; ignored by QG_ROPE_PLAIN                   */
+  double low, high;       /* 0 < low < high; BY_INDEX and BY_TURNS            */
+  double context;         /* > 0: positions of the training; the same two     */
+  double magnitude;       /* > 0                                              */
+  int32_t scaling;        /* QG_ROPE_*                                        */
+  int32_t rot;            /* rotated channels, even, 2..256                   */
+  int32_t max_pos;        /* rows of the table, >= 1                          */
+} qg_rope_params;
+
+/* table_dev: fp32 [max_pos][rot], row p = cos(p f_0) .. cos(p f_(rot/2-1)),
+ * then the sines; angles, cosines and sines in 64 bits, rounded once.
+ * Computed once by a program, read by the calls below.  16-byte aligned. */
+int qg_rope_table(const qg_rope_params* p, float* table_dev, void* stream);
+
+/* Rotates the first `rot` channels of every head, copies the others:
+ *   y1 = x1 cos - x2 sin,  y2 = x2 cos + x1 sin
+ * (products and sum in fp32, each rounded) for the pairs
+ *   (i, i + rot/2)  interleaved = 0       (2 i, 2 i + 1)  interleaved = 1.
+ * inverse = 1 turns back, which is the gradient of the rotation.
+ * positions: dev int32 [tokens]; one outside 0 .. max_pos-1 makes that token's
+ * rotated channels NaN.  y may be x itself (same strides); otherwise the two
+ * must not overlap.  head_dim 2..1024, rot even and <= head_dim. */
+int qg_rope(const qg_heads* x, int dtype, int tokens, int heads, int head_dim, const int32_t* positions,
+            const float* table_dev, int max_pos, int rot, int interleaved, int inverse, const qg_heads* y,
+            void* stream);
+
+/* The cache: one device buffer of pages, each of `page_tokens` tokens (16, 32, 64,
+ * 128 or 256) of `kv_heads` heads of `head_dim` (64, 128 or 256) channels.
+ * Keys and values are affinely quantized (Eq. 1) to 4 bits with one scale and zero
+ * point per token and KV head, over 0 and the head's channels x:
+ *   lo = min(0, min x), hi = max(0, max x)
+ *   alpha = (hi - lo) * (1/15) in fp32, its low four mantissa bits cleared
+ *   theta = min(15, rne(-lo * inv)), inv = 1 / alpha, correctly rounded
+ *   code  = clamp(rne(x * inv), -theta, 15 - theta) + theta
+ *   x stands for alpha * (code - theta)
+ * alpha below 2^-126: alpha, theta and codes are 0 (the token's head is 0).  An
+ * infinity or NaN among the channels, or a range beyond fp32, makes alpha NaN:
+ * what attends to that key or value gets NaN, as with an unquantized cache.
+ * Layout of a page, for each KV head in turn, page_tokens * (head_dim + 8) bytes:
+ *   key codes    [page_tokens][head_dim/2] bytes, channel c in byte c/2, even c in
+ *                the low half
+ *   value codes  [page_tokens/8][head_dim/4][8 tokens] 16-bit words of four
+ *                channels, the lowest in the low bits
+ *   words        [page_tokens/8][key, value][8 tokens] 32-bit: bits(alpha) | theta
+ * A token is named by its slot = page * page_tokens + place in the page. */
+typedef struct {
+  void* data;             /* dev, 64-byte aligned, qg_kv4_bytes() bytes       */
+  int32_t n_pages, kv_heads, head_dim, page_tokens;
+} qg_kv4_cache;
+
+/* Bytes of the buffer; 0 for extents that are not supported. */
+size_t qg_kv4_bytes(int n_pages, int kv_heads, int head_dim, int page_tokens);
+
+/* Quantizes keys and values of `tokens` tokens into their slots, the keys rotated
+ * on the way if `positions` is given, and rotates queries in the same pass if `q`
+ * is.  Tokens whose slot is outside the cache (-1, say: padding) are not stored;
+ * their queries are rotated all the same.  No two tokens may share a slot.
+ * Rotation as qg_rope, rot a multiple of 16; a position outside the table poisons
+ * the key (alpha NaN) and the query (NaN). */
+#define QG_KV4_MAX_TOKENS 1000000 /* of one call of qg_kv4_append or qg_kv4_read */
+typedef struct {
+  qg_heads k, v;          /* [tokens][kv_heads][head_dim]                     */
+  const int64_t* slots;   /* dev [tokens]                                     */
+  const int32_t* positions; /* dev [tokens], or NULL: keys and queries are taken as they are */
+  const float* table;     /* from qg_rope_table, 16-byte aligned; with positions */
+  qg_heads q, q_out;      /* [tokens][q_heads][head_dim]; q_out.data may be q.data (same strides) */
+  int32_t dtype, tokens, q_heads; /* q_heads 0: no queries                    */
+  int32_t max_pos, rot, interleaved;
+} qg_kv4_append_params;
+int qg_kv4_append(const qg_kv4_cache* c, const qg_kv4_append_params* p, void* stream);
+
+/* What the slots hold, as values of `dtype` (fp32 product, rounded once); a slot
+ * outside the cache gives zeros.  k or v may have NULL data: not wanted. */
+int qg_kv4_read(const qg_kv4_cache* c, const int64_t* slots, int tokens, int dtype, const qg_heads* k,
+                const qg_heads* v, void* stream);
+
+/* Attention of a batch of sequences over the cache:
+ *   o = sum_j softmax_j(scale * q . k_j) v_j
+ * for query i of n of a sequence with m keys over the keys j < m, and with causal
+ * = 1 over j <= m - n + i only (the queries are the last n tokens, their own keys
+ * stored).  Query head h reads KV head h / (q_heads / kv_heads).  A query with no
+ * key to see gives 0.  Sums and softmax statistics are fp32; the codes enter the
+ * matrix cores exactly, queries as fp16 numbers scaled by row (two per channel for
+ * QG_F32), probabilities as fp16 (two for QG_F32).
+ *   pages     dev int32 [batch][pages_stride]; entry i names the page of tokens
+ *             i * page_tokens on.  Only entries below ceil(m / page_tokens) are read;
+ *             one that is no page of the cache reads as page 0.
+ *   kv_lens   dev int32 [batch]: m, read as 0 below 0 and as max_kv_len above it
+ *   q_starts  dev int32 [batch + 1]: queries of sequence b are rows q_starts[b] ..
+ *             q_starts[b+1]-1 of q; a sequence may have none.  Rows beyond max_q_len of
+ *             a sequence, or that no sequence has, are not written.  NULL: batch == tokens,
+ *             one query each.
+ *   max_q_len, max_kv_len  the most that any sequence has, <= pages_stride * page_tokens
+ *             for the latter (the grid is sized by them: near bounds are faster)
+ *   workspace dev, 16-byte aligned, qg_kv4_attention_workspace_bytes() bytes for the same extents,
+ *             zeroed once by qg_gemm_workspace_init before its first use; every call leaves
+ *             it ready for the next one on the stream.  Calls that may overlap in time need one
+ *             each.  NULL is allowed: the keys of a sequence are then never split over
+ *             workgroups, which long sequences in small batches need.
+ * The result of a call is the same every time it is made. */
+typedef struct {
+  qg_heads q, out;        /* [tokens][q_heads][head_dim]                      */
+  const int32_t* pages;
+  const int32_t* kv_lens;
+  const int32_t* q_starts;
+  void* workspace;
+  size_t workspace_bytes;
+  float scale;            /* finite                                           */
+  int32_t dtype, tokens, q_heads, batch, pages_stride, max_q_len, max_kv_len, causal;
+} qg_kv4_attention_params;
+size_t qg_kv4_attention_workspace_bytes(const qg_kv4_cache* c, int q_heads, int batch, int max_q_len,
+                                        int max_kv_len);
+int qg_kv4_attention(const qg_kv4_cache* c, const qg_kv4_attention_params* p, void* stream);
+
 const char* qg_status_string(int code);
 
 #ifdef __cplusplus

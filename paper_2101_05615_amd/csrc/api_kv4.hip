@@ -1,0 +1,288 @@
+// Host side of the positions, the 4-bit cache and its attention (qgemm.h): argument checks, the rotation's frequencies, and how a
+// sequence's keys are split over workgroups.  As in the rest of the library nothing is allocated, created or waited for here.
+#include <math.h>
+
+#include "qg_kv4.h"
+
+namespace {
+
+inline bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
+
+constexpr size_t ELEM[3] = {4, 2, 2};
+
+bool known(int dtype) { return dtype == QG_F32 || dtype == QG_BF16 || dtype == QG_F16; }
+
+int check_heads(const qg_heads& h, int dtype) {
+  if (!h.data) return QG_ENULL;
+  return aligned(h.data, ELEM[dtype]) ? QG_OK : QG_EALIGN;
+}
+
+int lg_of_page(int page_tokens) {
+  for (int l = 4; l <= 8; ++l)
+    if (page_tokens == 1 << l) return l;
+  return -1;
+}
+
+int check_cache(const qg_kv4_cache* c, qg_kv4_layout* out) {
+  if (!c) return QG_ENULL;
+  if (qg_kv4_bytes(c->n_pages, c->kv_heads, c->head_dim, c->page_tokens) == 0) return QG_EINVAL;
+  if (!c->data) return QG_ENULL;
+  if (!aligned(c->data, 64)) return QG_EALIGN;
+  out->data = static_cast<uint8_t*>(c->data);
+  out->n_pages = c->n_pages;
+  out->heads = c->kv_heads;
+  out->lgp = lg_of_page(c->page_tokens);
+  return QG_OK;
+}
+
+// A table is needed wherever positions are
+int check_rotation(const float* table, int max_pos, int rot, int interleaved, int head_dim) {
+  if (!table) return QG_ENULL;
+  if (max_pos < 1 || rot < 2 || rot % 2 != 0 || rot > head_dim || (interleaved != 0 && interleaved != 1)) return QG_EINVAL;
+  return aligned(table, 16) ? QG_OK : QG_EALIGN;
+}
+
+// ---- keys of a sequence over workgroups
+// With few sequences a workgroup per (sequence, KV head) leaves most of the 256 CUs idle, and with sequences of different lengths
+// the longest one ends alone.  Keys are dealt in chunks of equal length: as few tokens as fill the CUs FILL times over, but at
+// least LEAST (a workgroup's start and end cost as much as a few hundred tokens) and at most MOST.
+constexpr int FILL = 4, LEAST = 256, MOST = 2048, CUS = 256;
+constexpr size_t COUNTERS = 16384;  // a fixed part of every workspace, so that calls of other extents find it zero
+
+struct share {
+  int split, chunk, rows_pad;
+};
+
+share share_of(int kv_heads, int q_heads, int batch, int max_q_len, int max_kv_len) {
+  share s = {1, 0, 0};
+  const long long rows = (long long)max_q_len * (q_heads / kv_heads);
+  const long long tiles = (rows + 15) / 16, blocks = (rows + 63) / 64;
+  s.rows_pad = (int)(tiles * 16);
+  const long long units = (long long)batch * kv_heads * (rows <= 16 ? 1 : blocks);
+  const int padded = (int)(((long long)max_kv_len + 31) / 32 * 32);
+  s.chunk = padded;
+  if ((size_t)((long long)batch * kv_heads * tiles) > COUNTERS) return s;
+  long long chunk = (long long)max_kv_len * units / (FILL * CUS);
+  chunk = (chunk + 31) / 32 * 32;
+  chunk = chunk < LEAST ? LEAST : chunk > MOST && rows <= 16 ? MOST : chunk;
+  if (chunk >= max_kv_len) return s;
+  s.chunk = (int)chunk;
+  s.split = (int)((max_kv_len + chunk - 1) / chunk);
+  return s;
+}
+
+size_t share_bytes(const share& s, int kv_heads, int batch, int head_dim) {
+  if (s.split == 1) return 0;
+  return COUNTERS * 4 + (size_t)batch * kv_heads * s.split * s.rows_pad * (head_dim + 1) * 4;
+}
+
+bool extents_ok(const qg_kv4_cache* c, int q_heads, int batch, int max_q_len, int max_kv_len) {
+  if (q_heads < 1 || q_heads % c->kv_heads != 0 || batch < 0 || max_q_len < 0 || max_kv_len < 0) return false;
+  if (max_kv_len > 1 << 30) return false;
+  return (long long)max_q_len * (q_heads / c->kv_heads) <= 1 << 28;
+}
+
+}  // namespace
+
+extern "C" {
+
+int qg_rope_table(const qg_rope_params* p, float* table_dev, void* stream) {
+  if (!p || !table_dev) return QG_ENULL;
+  if (p->rot < 2 || p->rot % 2 != 0 || p->rot > 256 || p->max_pos < 1) return QG_EINVAL;
+  if (!(p->base > 1.0) || !isfinite(p->base) || !(p->magnitude > 0.0) || !isfinite(p->magnitude)) return QG_EINVAL;
+  if (p->scaling < QG_ROPE_PLAIN || p->scaling > QG_ROPE_BY_TURNS) return QG_EINVAL;
+  const bool scaled = p->scaling != QG_ROPE_PLAIN, by_band = p->scaling == QG_ROPE_BY_INDEX || p->scaling == QG_ROPE_BY_TURNS;
+  if (scaled && (!(p->factor >= 1.0) || !isfinite(p->factor))) return QG_EINVAL;
+  if (by_band && (!(p->low > 0.0) || !(p->high > p->low) || !isfinite(p->high) || !(p->context > 0.0) || !isfinite(p->context)))
+    return QG_EINVAL;
+  if (!aligned(table_dev, 16)) return QG_EALIGN;
+  const double two_pi = 6.283185307179586476925286766559;
+  // the (fractional) pair that makes `turns` turns in `context` positions: context * base^(-2 i / rot) = 2 pi turns
+  auto pair_of = [&](double turns) { return p->rot * log(p->context / (two_pi * turns)) / (2.0 * log(p->base)); };
+  const int pairs = p->rot / 2;
+  double from = 0.0, to = 1.0;
+  if (p->scaling == QG_ROPE_BY_INDEX) {
+    from = floor(pair_of(p->high));
+    to = ceil(pair_of(p->low));
+    from = from < 0.0 ? 0.0 : from;
+    to = to > pairs - 1 ? pairs - 1 : to;
+    if (to <= from) to = from + 0.001;
+  }
+  double f[128];
+  for (int i = 0; i < pairs; ++i) {
+    f[i] = pow(p->base, -2.0 * i / p->rot);
+    double w = 0.0;
+    if (p->scaling == QG_ROPE_LINEAR) w = 1.0;
+    if (p->scaling == QG_ROPE_BY_INDEX) w = (i - from) / (to - from);
+    if (p->scaling == QG_ROPE_BY_TURNS) w = (p->high - p->context * f[i] / two_pi) / (p->high - p->low);
+    w = w < 0.0 ? 0.0 : w > 1.0 ? 1.0 : w;
+    f[i] = f[i] * (1.0 - w) + (scaled ? f[i] / p->factor * w : 0.0);
+  }
+  return qg_launch_rope_table(f, p->rot, p->max_pos, p->magnitude, table_dev, static_cast<hipStream_t>(stream)) == hipSuccess
+             ? QG_OK
+             : QG_ELAUNCH;
+}
+
+int qg_rope(const qg_heads* x, int dtype, int tokens, int heads, int head_dim, const int32_t* positions, const float* table_dev,
+            int max_pos, int rot, int interleaved, int inverse, const qg_heads* y, void* stream) {
+  if (!x || !y) return QG_ENULL;
+  if (!known(dtype) || tokens < 0 || heads < 1 || heads > 65535 || head_dim < 2 || head_dim > 1024) return QG_EINVAL;
+  if (inverse != 0 && inverse != 1) return QG_EINVAL;
+  int rc = check_rotation(table_dev, max_pos, rot, interleaved, head_dim);
+  if (rc != QG_OK) return rc;
+  if (tokens == 0) return QG_OK;
+  if (!positions) return QG_ENULL;
+  if ((rc = check_heads(*x, dtype)) != QG_OK || (rc = check_heads(*y, dtype)) != QG_OK) return rc;
+  if (!aligned(positions, 4)) return QG_EALIGN;
+  if (x->data == y->data && (x->token_stride != y->token_stride || x->head_stride != y->head_stride)) return QG_EINVAL;
+  qg_rope_args a = {};
+  a.x = x->data;
+  a.y = y->data;
+  a.positions = positions;
+  a.table = table_dev;
+  a.tokens = tokens;
+  a.heads = heads;
+  a.head_dim = head_dim;
+  a.rot = rot;
+  a.max_pos = max_pos;
+  a.interleaved = interleaved;
+  a.sign = inverse ? -1.0f : 1.0f;
+  a.x_token = x->token_stride;
+  a.x_head = x->head_stride;
+  a.y_token = y->token_stride;
+  a.y_head = y->head_stride;
+  return qg_launch_rope(a, dtype, static_cast<hipStream_t>(stream)) == hipSuccess ? QG_OK : QG_ELAUNCH;
+}
+
+size_t qg_kv4_bytes(int n_pages, int kv_heads, int head_dim, int page_tokens) {
+  if (n_pages < 1 || kv_heads < 1 || kv_heads > 32767 || lg_of_page(page_tokens) < 0) return 0;
+  if (head_dim != 64 && head_dim != 128 && head_dim != 256) return 0;
+  return (size_t)n_pages * kv_heads * page_tokens * (head_dim + 8);
+}
+
+int qg_kv4_append(const qg_kv4_cache* c, const qg_kv4_append_params* p, void* stream) {
+  if (!p) return QG_ENULL;
+  qg_kv4_append_args a = {};
+  int rc = check_cache(c, &a.c);
+  if (rc != QG_OK) return rc;
+  if (!known(p->dtype) || p->tokens < 0 || p->q_heads < 0 || p->q_heads + 2 * c->kv_heads > 65535) return QG_EINVAL;
+  if (p->tokens > QG_KV4_MAX_TOKENS) return QG_EINVAL;
+  if (p->positions) {
+    if ((rc = check_rotation(p->table, p->max_pos, p->rot, p->interleaved, c->head_dim)) != QG_OK) return rc;
+    if (p->rot % 16 != 0) return QG_EUNSUPPORTED;
+    if (!aligned(p->positions, 4)) return QG_EALIGN;
+  }
+  if (p->tokens == 0) return QG_OK;
+  if (!p->slots) return QG_ENULL;
+  if (!aligned(p->slots, 8)) return QG_EALIGN;
+  if ((rc = check_heads(p->k, p->dtype)) != QG_OK || (rc = check_heads(p->v, p->dtype)) != QG_OK) return rc;
+  if (p->q_heads > 0) {
+    if ((rc = check_heads(p->q, p->dtype)) != QG_OK || (rc = check_heads(p->q_out, p->dtype)) != QG_OK) return rc;
+    if (p->q.data == p->q_out.data && (p->q.token_stride != p->q_out.token_stride || p->q.head_stride != p->q_out.head_stride))
+      return QG_EINVAL;
+  }
+  a.k = p->k.data;
+  a.v = p->v.data;
+  a.q = p->q.data;
+  a.q_out = p->q_out.data;
+  a.slots = p->slots;
+  a.positions = p->positions;
+  a.table = p->table;
+  a.tokens = p->tokens;
+  a.q_heads = p->q_heads;
+  a.rot = p->rot;
+  a.max_pos = p->max_pos;
+  a.interleaved = p->interleaved;
+  a.k_token = p->k.token_stride;
+  a.k_head = p->k.head_stride;
+  a.v_token = p->v.token_stride;
+  a.v_head = p->v.head_stride;
+  a.q_token = p->q.token_stride;
+  a.q_head = p->q.head_stride;
+  a.o_token = p->q_out.token_stride;
+  a.o_head = p->q_out.head_stride;
+  return qg_launch_kv4_append(a, c->head_dim, p->dtype, static_cast<hipStream_t>(stream)) == hipSuccess ? QG_OK : QG_ELAUNCH;
+}
+
+int qg_kv4_read(const qg_kv4_cache* c, const int64_t* slots, int tokens, int dtype, const qg_heads* k, const qg_heads* v,
+                void* stream) {
+  if (!k || !v) return QG_ENULL;
+  qg_kv4_read_args a = {};
+  int rc = check_cache(c, &a.c);
+  if (rc != QG_OK) return rc;
+  if (!known(dtype) || tokens < 0 || tokens > QG_KV4_MAX_TOKENS) return QG_EINVAL;
+  if (tokens == 0) return QG_OK;
+  if (!slots) return QG_ENULL;
+  if (!aligned(slots, 8)) return QG_EALIGN;
+  if (k->data && (rc = check_heads(*k, dtype)) != QG_OK) return rc;
+  if (v->data && (rc = check_heads(*v, dtype)) != QG_OK) return rc;
+  a.k = k->data;
+  a.v = v->data;
+  a.slots = slots;
+  a.tokens = tokens;
+  a.k_token = k->token_stride;
+  a.k_head = k->head_stride;
+  a.v_token = v->token_stride;
+  a.v_head = v->head_stride;
+  return qg_launch_kv4_read(a, c->head_dim, dtype, static_cast<hipStream_t>(stream)) == hipSuccess ? QG_OK : QG_ELAUNCH;
+}
+
+size_t qg_kv4_attention_workspace_bytes(const qg_kv4_cache* c, int q_heads, int batch, int max_q_len, int max_kv_len) {
+  if (!c || qg_kv4_bytes(c->n_pages, c->kv_heads, c->head_dim, c->page_tokens) == 0) return 0;
+  if (!extents_ok(c, q_heads, batch, max_q_len, max_kv_len) || batch == 0 || max_q_len == 0 || max_kv_len == 0) return 0;
+  return share_bytes(share_of(c->kv_heads, q_heads, batch, max_q_len, max_kv_len), c->kv_heads, batch, c->head_dim);
+}
+
+int qg_kv4_attention(const qg_kv4_cache* c, const qg_kv4_attention_params* p, void* stream) {
+  if (!p) return QG_ENULL;
+  qg_kv4_attention_args a = {};
+  int rc = check_cache(c, &a.c);
+  if (rc != QG_OK) return rc;
+  if (!known(p->dtype) || p->tokens < 0 || !extents_ok(c, p->q_heads, p->batch, p->max_q_len, p->max_kv_len)) return QG_EINVAL;
+  if (!isfinite(p->scale) || (p->causal != 0 && p->causal != 1) || p->pages_stride < 0) return QG_EINVAL;
+  if (p->max_kv_len > (long long)p->pages_stride * c->page_tokens) return QG_EINVAL;
+  if (!p->q_starts && p->batch != p->tokens) return QG_EINVAL;
+  if (p->tokens == 0 || p->batch == 0 || p->max_q_len == 0) return QG_OK;
+  if (!p->kv_lens || (!p->pages && p->max_kv_len > 0)) return QG_ENULL;
+  if (!aligned(p->kv_lens, 4) || !aligned(p->pages, 4) || !aligned(p->q_starts, 4)) return QG_EALIGN;
+  if ((rc = check_heads(p->q, p->dtype)) != QG_OK || (rc = check_heads(p->out, p->dtype)) != QG_OK) return rc;
+  const int max_q = p->q_starts ? p->max_q_len : 1;
+  share s = share_of(c->kv_heads, p->q_heads, p->batch, max_q, p->max_kv_len);
+  if (!p->workspace) {
+    s.split = 1;
+    s.chunk = (p->max_kv_len + 31) / 32 * 32;
+  }
+  if (s.split > 1) {
+    if (p->workspace_bytes < share_bytes(s, c->kv_heads, p->batch, c->head_dim)) return QG_EWORKSPACE;
+    if (!aligned(p->workspace, 16)) return QG_EALIGN;
+  }
+  if (s.chunk == 0) s.chunk = 32;
+  const long long rows = (long long)max_q * (p->q_heads / c->kv_heads);
+  if (((long long)p->batch * c->kv_heads * s.split + 8) * ((rows + 15) / 16) > 0x7fffffffll / 256) return QG_EUNSUPPORTED;
+  a.q = p->q.data;
+  a.out = p->out.data;
+  a.pages = p->pages;
+  a.kv_lens = p->kv_lens;
+  a.q_starts = p->q_starts;
+  a.tokens = p->tokens;
+  a.group = p->q_heads / c->kv_heads;
+  a.batch = p->batch;
+  a.pages_stride = p->pages_stride;
+  a.max_q_len = max_q;
+  a.max_kv_len = p->max_kv_len;
+  a.causal = p->causal;
+  a.scale_log2e = (float)((double)p->scale * 1.4426950408889634074);
+  a.split = s.split;
+  a.chunk = s.chunk;
+  a.rows_pad = s.rows_pad;
+  a.counters = static_cast<int*>(p->workspace);
+  a.partial = reinterpret_cast<float*>(static_cast<char*>(p->workspace) + (p->workspace ? COUNTERS * 4 : 0));
+  a.q_token = p->q.token_stride;
+  a.q_head = p->q.head_stride;
+  a.o_token = p->out.token_stride;
+  a.o_head = p->out.head_stride;
+  return qg_launch_kv4_attention(a, c->head_dim, p->dtype, (int)rows, static_cast<hipStream_t>(stream)) == hipSuccess ? QG_OK
+                                                                                                                  : QG_ELAUNCH;
+}
+
+}  // extern "C"

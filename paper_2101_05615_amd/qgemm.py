@@ -28,6 +28,9 @@ EXPORTS = [
     "qg_conv_dense_u8s8_requant", "qg_pack_b_transposed",
     "qg_gemm_workspace_init", "qg_gemm_splitk_workspace_bytes", "qg_gemm_splitk_factor",
     "qg_gemm_u8s8_requant_splitk", "qg_gemm_u8s8_acc32_splitk", "qg_gemm_u8s8_requant_noalloc",
+    # positions and the 4-bit key/value cache: marshalled in kv4.py
+    "qg_rope_table", "qg_rope", "qg_kv4_bytes", "qg_kv4_append", "qg_kv4_read", "qg_kv4_attention_workspace_bytes",
+    "qg_kv4_attention",
 ]
 
 KERNEL_AUTO, KERNEL_LAST = 0, 10
