@@ -271,7 +271,9 @@ int qg_kv4_attention(const qg_kv4_cache* c, const qg_kv4_attention_params* p, vo
   a.max_q_len = max_q;
   a.max_kv_len = p->max_kv_len;
   a.causal = p->causal;
-  a.scale_log2e = (float)((double)p->scale * 1.4426950408889634074);
+  const double to_log2 = (double)p->scale * 1.4426950408889634074;
+  a.scale_log2e = (float)to_log2;
+  a.scale_log2e_lo = (float)(to_log2 - (double)a.scale_log2e);
   a.split = s.split;
   a.chunk = s.chunk;
   a.rows_pad = s.rows_pad;

@@ -8,10 +8,18 @@
 // register each, and what a lane gets of S^T, tokens 8g .. 8g+7 (g = l / 16; the rows of the two key tiles are dealt that way),
 // is in place as the second operand of the other product.
 //
-// The codes never become dequantized numbers.  code - theta is a whole number of at most 15 and exact in fp16: a dword of codes
-// becomes eight of them with one shift, four and-or (the exponent of 1024 put around a nibble) and four packed additions that
-// take away 1024 + theta.  The scales go to the other side: a key's onto the score, a value's onto the probability.  The 16
-// scale-and-theta words of 8 tokens lie in the 16 lanes of a DPP row, where every lane of the row reaches them as an operand.
+// The codes never become dequantized numbers: the scales go to the other side, a key's onto the score, a value's onto the
+// probability.  The 16 scale-and-theta words of 8 tokens lie in the 16 lanes of a DPP row, where every lane of the row reaches them
+// as an operand.  The zero points:
+//   values  code - theta is a whole number of at most 15 and exact in fp16.  A dword of codes becomes eight of them with one shift,
+//           four and-or (the exponent of 1024 put around a nibble) and four packed additions that take away 1024 + theta.
+//   keys    a nibble alone in bits 4 to 7 of an fp16 is the number code * 2^-20, which the matrix cores take as it is (four ANDs and
+//           three shifts), and theta comes off the sum, sum q (code - theta) = sum q code - theta sum q, with one fused multiply-add
+//           per score.  fp32 results would see the cancellation: there keys go as values do.
+// (Taking theta off the second product's sums as well is 10 % fewer instructions, but where the token that has all the weight is
+// worth 0, 2^-21 of its neighbours' size is left: measured, 6 % of a result that came from the other tokens.  Nibbles in bits 0
+// to 3 would save two shifts, but products of numbers this small are aligned by the exponent 2^-14 that their format gives them:
+// over 32 products code * 2^-24 measured 2e-6 off the sum of their sizes, code * 2^-20 5e-8.)
 //
 // Rounding.  Queries become fp16 after a power of two per row that puts the largest channel near 2^14: exact for fp16 and
 // bf16 channels down to 2^-24 of the largest; fp32 queries take two fp16 (22 bits).  Probabilities times value scale become fp16
@@ -50,14 +58,27 @@ union frag {
 
 __device__ inline h2 as_h2(unsigned x) { return __builtin_bit_cast(h2, x); }
 
-// Eight codes of a dword less theta, as four pairs (nibbles 0 4, 1 5, 2 6, 3 7).  low: -(1024 + theta) twice; high: -(64 + theta).
-__device__ inline void unpack(unsigned x, h2 low, h2 high, h2* out) {
+// Eight codes of a dword as four pairs (nibbles 0 4, 1 5, 2 6, 3 7), times 2^-20
+__device__ inline void spread(unsigned x, unsigned* out) {
+  out[0] = x << 4 & 0x00f000f0u;
+  out[1] = x & 0x00f000f0u;
+  out[2] = x >> 4 & 0x00f000f0u;
+  out[3] = x >> 8 & 0x00f000f0u;
+}
+
+// The same less theta, in units of 1: 1024 + c or 1024 + 16 c, whose bits are a nibble under the exponent of 1024, less 1024 + theta.
+// low: -(1024 + theta) twice; high: -(64 + theta).  (The masks live in registers: and-or takes no constants.)
+struct masks {
+  unsigned even, odd, magic;
+  __device__ inline masks() : even(0x000f000fu), odd(0x00f000f0u), magic(0x64006400u) { asm("" : "+s"(even), "+s"(odd), "+v"(magic)); }
+};
+__device__ inline void spread_less(unsigned x, const masks& m, h2 low, h2 high, unsigned* out) {
   const h2 sixteenth = {(_Float16)0.0625f, (_Float16)0.0625f};
   const unsigned y = x >> 8;
-  out[0] = as_h2((x & 0x000f000fu) | 0x64006400u) + low;                                        // 1024 + c
-  out[1] = __builtin_elementwise_fma(as_h2((x & 0x00f000f0u) | 0x64006400u), sixteenth, high);  // 1024 + 16 c
-  out[2] = as_h2((y & 0x000f000fu) | 0x64006400u) + low;
-  out[3] = __builtin_elementwise_fma(as_h2((y & 0x00f000f0u) | 0x64006400u), sixteenth, high);
+  out[0] = __builtin_bit_cast(unsigned, as_h2((x & m.even) | m.magic) + low);
+  out[1] = __builtin_bit_cast(unsigned, __builtin_elementwise_fma(as_h2((x & m.odd) | m.magic), sixteenth, high));
+  out[2] = __builtin_bit_cast(unsigned, as_h2((y & m.even) | m.magic) + low);
+  out[3] = __builtin_bit_cast(unsigned, __builtin_elementwise_fma(as_h2((y & m.odd) | m.magic), sixteenth, high));
 }
 
 template <int D>
@@ -67,36 +88,47 @@ struct tile_bits {
   unsigned w;             // a word of the row's 8 tokens: keys 0 .. 7, then values
 };
 
-// What a wave reads of the cache.  SMALL: pages of 16 tokens, two to a tile; otherwise a tile lies in one page.
+// What a wave reads of the cache.  SMALL: pages of 16 tokens, two to a tile; otherwise a tile lies in one page, whose address is
+// the same for all lanes.
 template <int D, bool SMALL>
 struct reader {
-  const qg_kv4_attention_args& p;
+  uint8_t* data;
   const int32_t* table;  // the sequence's pages
-  int head, last_page;   // the last page that holds a key
-  int kq, r, g;          // lane / 16 again for channels, lane % 16, lane / 16
+  int n_pages, heads, lgp, head, last_page;   // the last page that holds a key
+  unsigned key_lane, value_lane, word_lane;   // this lane's bytes past the tile's
+  bool key_half, value_half;                  // SMALL: the lane's run of 8 tokens lies in the tile's second page
 
+  __device__ inline reader(const qg_kv4_attention_args& p, int seq, int kv_head, int keys, int r, int g)
+      : data(p.c.data), table(p.pages + (int64_t)seq * p.pages_stride), n_pages(p.c.n_pages), heads(p.c.heads), lgp(SMALL ? 4 : p.c.lgp),
+        head(kv_head), last_page(max((keys - 1) >> (SMALL ? 4 : p.c.lgp), 0)) {
+    const int key_run = r >> 2, key_at = SMALL ? key_run & 1 : key_run, value_at = SMALL ? g & 1 : g;
+    key_lane = (unsigned)((8 * key_at + (r & 3)) * (D / 2) + g * (D / 8));
+    value_lane = (unsigned)(value_at * (4 * D) + r * (D / 4));
+    word_lane = (unsigned)(value_at * 64 + r * 4);
+    key_half = key_run >= 2;
+    value_half = g >= 2;
+  }
   __device__ inline const uint8_t* block(int index) const {
     unsigned page = (unsigned)table[min(index, last_page)];
-    page = page < (unsigned)p.c.n_pages ? page : 0u;
-    return p.c.data + qg_kv4_block<D>(p.c, (int)page, head);
+    page = page < (unsigned)n_pages ? page : 0u;
+    return data + ((size_t)page * heads + head) * ((size_t)(D + 8) << lgp);
   }
   __device__ inline void load(int t0, tile_bits<D>& b) const {
-    const int P = 1 << p.c.lgp;
-    const uint8_t *kb, *vb;
-    int kat, vat;  // first token of the lane's run of 8 in its page
+    const int P = 1 << lgp;
+    const uint8_t *kb, *vb, *wb;
     if (SMALL) {
-      const int kt = t0 + 8 * (r >> 2), vt = t0 + 8 * g;
-      kb = block(kt >> 4);
-      vb = block(vt >> 4);
-      kat = kt & 15;
-      vat = vt & 15;
+      const uint8_t *first = block(t0 >> 4), *second = block((t0 >> 4) + 1);
+      kb = key_half ? second : first;
+      vb = (value_half ? second : first) + 16 * (D / 2);
+      wb = vb + 16 * (D / 2);
     } else {
+      const uint8_t* page = block(t0 >> lgp);
       const int at = t0 & (P - 1);
-      kb = vb = block(t0 >> p.c.lgp);
-      kat = at + 8 * (r >> 2);
-      vat = at + 8 * g;
+      kb = page + at * (D / 2);
+      vb = page + (P + at) * (D / 2);
+      wb = page + P * D + at * 8;
     }
-    const uint8_t* k = kb + (kat + (r & 3)) * (D / 2) + kq * (D / 8);
+    const uint8_t* k = kb + key_lane;
 #pragma unroll
     for (int a = 0; a < 2; ++a) {
       if (D == 64) {
@@ -112,10 +144,10 @@ struct reader {
         }
       }
     }
-    const uint8_t* v = vb + P * (D / 2) + (vat >> 3) * (4 * D) + r * (D / 4);
+    const uint8_t* v = vb + value_lane;
 #pragma unroll
     for (int i = 0; i < D / 64; ++i) b.v[i] = reinterpret_cast<const u4*>(v)[i];
-    b.w = *reinterpret_cast<const unsigned*>(vb + P * D + (vat >> 3) * 64 + r * 4);
+    b.w = *reinterpret_cast<const unsigned*>(wb + word_lane);
   }
 };
 
@@ -124,7 +156,9 @@ template <int D, int DIG, int NR>
 struct state {
   frag q[NR][DIG][D / 32];
   f4 o[NR][D / 16];
-  float m[NR], l[NR], factor[NR];  // reference of the exponents (log2), sum (this lane's tokens), log2 score of a scaled product
+  float m[NR], l[NR];              // reference of the exponents (log2), sum (this lane's tokens)
+  float factor[NR], factor_lo[NR]; // log2 score of a product and a key's scale, in two parts (the second: DIG 2)
+  float q_sum[NR];                 // DIG 1: less the sum of the queries, times 2^-20
   int limit[NR];                   // last token that the row sees
   int vref;                        // biased exponent of the value scales' reference, 1 .. 253
 };
@@ -138,26 +172,41 @@ __device__ inline float across_sum(float x) {
   return x + __shfl_xor(x, 32);
 }
 
+template <int DIG>
+__device__ inline float exponent(float z, float factor, float factor_lo, float base) {
+  // DIG 2: the factor's own rounding (2^-24 of every score) is more than the rest of an fp32 result's error
+  return DIG == 2 ? __builtin_fmaf(z, factor, __builtin_fmaf(z, factor_lo, base)) : __builtin_fmaf(z, factor, base);
+}
+
 // One tile.  MASKED: tokens from `end` on are not there, and a row may end inside.
 template <int D, int DIG, int NR, bool MASKED>
-__device__ inline void step(state<D, DIG, NR>& s, tile_bits<D> b, int t0, int end, int r, int g) {
-  if (MASKED && t0 + 8 * g + (r & 7) >= end) b.w = 0u;
-  const unsigned theta = b.w & 15u;
-  const float scale = __builtin_bit_cast(float, b.w & ~15u);
+__device__ inline void step(state<D, DIG, NR>& s, const tile_bits<D>& b, int t0, int end, int r, int g) {
+  unsigned word = b.w;
+  if (MASKED && t0 + 8 * g + (r & 7) >= end) word = 0u;
+  const unsigned theta = word & 15u;
+  const float scale = __builtin_bit_cast(float, word & ~15u);
+  const masks m;
 
   // ---- scores
   f4 z[NR][2];
 #pragma unroll
   for (int a = 0; a < 2; ++a) {
-    // theta of the token that this lane holds as first operand: row r of tile a is token 8 (r / 4) + 4 a + r % 4
-    const unsigned th = (unsigned)__builtin_amdgcn_ds_bpermute((16 * (r >> 2) + 4 * a + (r & 3)) * 4, (int)theta) * 0x10001u;
-    const h2 low = as_h2(th + 0xE400E400u), high = as_h2((th << 4) + 0xD400D400u);
+    h2 low = {}, high = {};
+    if (DIG == 2) {
+      // theta of the token that this lane holds as first operand: row r of tile a is token 8 (r / 4) + 4 a + r % 4
+      const unsigned th = (unsigned)__builtin_amdgcn_ds_bpermute((16 * (r >> 2) + 4 * a + (r & 3)) * 4, (int)theta) * 0x10001u;
+      low = as_h2(th + 0xE400E400u);
+      high = as_h2((th << 4) + 0xD400D400u);
+    }
 #pragma unroll
     for (int n = 0; n < NR; ++n) z[n][a] = (f4){0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
     for (int i = 0; i < D / 32; ++i) {
       frag k;
-      unpack(b.k[a][i], low, high, k.h);
+      if (DIG == 2)
+        spread_less(b.k[a][i], m, low, high, k.u);
+      else
+        spread(b.k[a][i], k.u);
 #pragma unroll
       for (int n = 0; n < NR; ++n)
 #pragma unroll
@@ -168,16 +217,26 @@ __device__ inline void step(state<D, DIG, NR>& s, tile_bits<D> b, int t0, int en
   // ---- exponents; the references move rarely
   const float ks[8] = {row_lane<0>(scale), row_lane<1>(scale), row_lane<2>(scale), row_lane<3>(scale),
                        row_lane<4>(scale), row_lane<5>(scale), row_lane<6>(scale), row_lane<7>(scale)};
-  const int vexp = r >= 8 ? min((int)(b.w >> 23 & 255u), 254) : 0;
-  bool move = (b.w & 0x7f800000u) != 0x7f800000u && min(vexp, 253) > s.vref;
+  if (DIG == 1) {
+    const float t = (float)theta;
+    const float zp[8] = {row_lane<0>(t), row_lane<1>(t), row_lane<2>(t), row_lane<3>(t),
+                         row_lane<4>(t), row_lane<5>(t), row_lane<6>(t), row_lane<7>(t)};
+#pragma unroll
+    for (int n = 0; n < NR; ++n)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) z[n][j >> 2][j & 3] = __builtin_fmaf(zp[j], s.q_sum[n], z[n][j >> 2][j & 3]);
+  }
+  const int vexp = (word & 0x7f800000u) != 0x7f800000u && r >= 8 ? min((int)(word >> 23 & 255u), 253) : 0;
+  bool move = vexp > s.vref;
   float y[NR][8];
 #pragma unroll
   for (int n = 0; n < NR; ++n) {
+    const float base = BOOST - s.m[n];
     float top = -__builtin_inff();
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
       z[n][j >> 2][j & 3] *= ks[j];
-      y[n][j] = __builtin_fmaf(z[n][j >> 2][j & 3], s.factor[n], BOOST - s.m[n]);
+      y[n][j] = exponent<DIG>(z[n][j >> 2][j & 3], s.factor[n], s.factor_lo[n], base);
       if (MASKED) {
         const int t = t0 + 8 * g + j;
         if (t >= end || t > s.limit[n]) y[n][j] = -__builtin_inff();
@@ -187,7 +246,7 @@ __device__ inline void step(state<D, DIG, NR>& s, tile_bits<D> b, int t0, int en
     move |= top > SLACK;
   }
   if (__builtin_expect(__ballot(move) != 0ull, 0)) {
-    int e = (b.w & 0x7f800000u) != 0x7f800000u ? min(vexp, 253) : 0;
+    int e = vexp;
 #pragma unroll
     for (int d = 1; d < 64; d *= 2) e = max(e, __shfl_xor(e, d));
     const int vref = max(s.vref, e);
@@ -195,22 +254,22 @@ __device__ inline void step(state<D, DIG, NR>& s, tile_bits<D> b, int t0, int en
     s.vref = vref;
 #pragma unroll
     for (int n = 0; n < NR; ++n) {
-      float top = -__builtin_inff();
+      float high = -__builtin_inff();
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        const float x = z[n][j >> 2][j & 3] * s.factor[n];
         const int t = t0 + 8 * g + j;
-        top = fmaxf(top, MASKED && (t >= end || t > s.limit[n]) ? -__builtin_inff() : x);
+        const float x = z[n][j >> 2][j & 3] * s.factor[n];
+        high = fmaxf(high, MASKED && (t >= end || t > s.limit[n]) ? -__builtin_inff() : x);
       }
-      const float m = fmaxf(s.m[n], across_max(top));
-      const float f = __builtin_amdgcn_exp2f(s.m[n] - m);
-      s.m[n] = m;
+      const float top = fmaxf(s.m[n], across_max(high));
+      const float f = __builtin_amdgcn_exp2f(s.m[n] - top);
+      s.m[n] = top;
       s.l[n] *= f;
 #pragma unroll
       for (int i = 0; i < D / 16; ++i) s.o[n][i] *= f * shrink;
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        y[n][j] = __builtin_fmaf(z[n][j >> 2][j & 3], s.factor[n], BOOST - m);
+        y[n][j] = exponent<DIG>(z[n][j >> 2][j & 3], s.factor[n], s.factor_lo[n], BOOST - top);
         if (MASKED) {
           const int t = t0 + 8 * g + j;
           if (t >= end || t > s.limit[n]) y[n][j] = -__builtin_inff();
@@ -244,16 +303,18 @@ __device__ inline void step(state<D, DIG, NR>& s, tile_bits<D> b, int t0, int en
   // ---- output.  theta of tokens 2 i and 2 i + 1 in a pair, from the lanes of the row that hold their words
   const unsigned next = (unsigned)__builtin_amdgcn_mov_dpp((int)theta, 0x101, 0xf, 0xf, true);  // row_shl:1
   const unsigned pair = theta | next << 16;
-  const unsigned th[4] = {row_lane<8>(pair), row_lane<10>(pair), row_lane<12>(pair), row_lane<14>(pair)};
+  const unsigned low = pair + 0xE400E400u, high = (pair << 4) + 0xD400D400u;
+  const h2 lows[4] = {as_h2(row_lane<8>(low)), as_h2(row_lane<10>(low)), as_h2(row_lane<12>(low)), as_h2(row_lane<14>(low))};
+  const h2 highs[4] = {as_h2(row_lane<8>(high)), as_h2(row_lane<10>(high)), as_h2(row_lane<12>(high)), as_h2(row_lane<14>(high))};
 #pragma unroll
   for (int i = 0; i < D / 64; ++i) {
     frag v[4];
 #pragma unroll
     for (int t = 0; t < 4; ++t) {
-      h2 x[4];
-      unpack(b.v[i][t], as_h2(th[t] + 0xE400E400u), as_h2((th[t] << 4) + 0xD400D400u), x);
+      unsigned x[4];
+      spread_less(b.v[i][t], m, lows[t], highs[t], x);
 #pragma unroll
-      for (int c = 0; c < 4; ++c) v[c].h[t] = x[c];
+      for (int c = 0; c < 4; ++c) v[c].u[t] = x[c];
     }
 #pragma unroll
     for (int c = 0; c < 4; ++c)
@@ -264,13 +325,13 @@ __device__ inline void step(state<D, DIG, NR>& s, tile_bits<D> b, int t0, int en
   }
 }
 
-// The queries of a lane: row `row` of its column, channels (D/4) g .. of it, as fp16 scaled by a power of two; returns the
-// factor that turns a product with code - theta, times alpha, into log2 units
-template <int D, int DIG, int TYPE>
-__device__ inline float load_q(const void* q, bool there, frag (*out)[D / 32], float scale_log2e, int g) {
+// The queries of a lane: row `row` of its column, channels (D/4) g .. of it, as fp16 scaled by a power of two
+template <int D, int DIG, int NR, int TYPE>
+__device__ inline void load_q(state<D, DIG, NR>& s, int n, const typename qg_elem<TYPE>::t* q, bool there, float scale_log2e,
+                              float scale_log2e_lo, int g) {
   float x[D / 4];
   if (there) {
-    qg_load<TYPE, D / 4>(static_cast<const typename qg_elem<TYPE>::t*>(q) + g * (D / 4), x);
+    qg_load<TYPE, D / 4>(q + g * (D / 4), x);
   } else {
 #pragma unroll
     for (int i = 0; i < D / 4; ++i) x[i] = 0.0f;
@@ -280,18 +341,23 @@ __device__ inline float load_q(const void* q, bool there, frag (*out)[D / 32], f
   for (int i = 0; i < D / 4; ++i) top = max(top, __builtin_bit_cast(unsigned, x[i]) & 0x7fffffffu);
   top = max(top, (unsigned)__shfl_xor((int)top, 16));
   top = max(top, (unsigned)__shfl_xor((int)top, 32));
-  const int shift = top == 0u ? 0 : 14 + 127 - max((int)(top >> 23), 1);  // (an infinity or NaN: the row's scores become NaN)
+  const int shift = top == 0u ? 0 : 14 + 127 - max((int)(top >> 23), 1);
+  float sum = 0.0f;
 #pragma unroll
   for (int i = 0; i < D / 32; ++i)
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      const int c = 8 * i + (j >> 1) + 4 * (j & 1);  // the order in which unpack() leaves the codes
+      const int c = 8 * i + (j >> 1) + 4 * (j & 1);  // the order in which the codes of a dword are spread
+      // (an infinity or NaN: the row's scores become NaN)
       const float y = top < 0x7f800000u ? __builtin_ldexpf(x[c], shift) : __builtin_nanf("");
       const _Float16 hi = (_Float16)y;
-      out[0][i].v[j] = hi;
-      if (DIG == 2) out[DIG - 1][i].v[j] = (_Float16)(y - (float)hi);
+      s.q[n][0][i].v[j] = hi;
+      if (DIG == 2) s.q[n][DIG - 1][i].v[j] = (_Float16)(y - (float)hi);
+      if (DIG == 1) sum += (float)hi;
     }
-  return __builtin_ldexpf(scale_log2e, -shift);
+  if (DIG == 1) s.q_sum[n] = across_sum(sum) * -0x1p-20f;
+  s.factor[n] = __builtin_ldexpf(scale_log2e, (DIG == 1 ? 20 : 0) - shift);
+  s.factor_lo[n] = __builtin_ldexpf(scale_log2e_lo, -shift);
 }
 
 // Four consecutive channels of a finished row
@@ -308,7 +374,7 @@ __device__ inline void hand_in(float* to, float a, float b) {  // past the cache
 
 // TOKENS: the workgroup's waves share the same rows and split its tokens; otherwise they split its rows.
 template <int D, int DIG, int TYPE, int NR, bool TOKENS, bool SMALL>
-__global__ __launch_bounds__(64 * WAVES) void qg_kv4_attention_kernel(qg_kv4_attention_args p) {
+__global__ __launch_bounds__(64 * WAVES, 2) void qg_kv4_attention_kernel(qg_kv4_attention_args p) {
   constexpr int ROWS = 16 * NR * (TOKENS ? 1 : WAVES);  // of the workgroup
   constexpr int PITCH = D + 4;
   __shared__ float part[TOKENS ? WAVES * ROWS * PITCH : 1];
@@ -348,7 +414,7 @@ __global__ __launch_bounds__(64 * WAVES) void qg_kv4_attention_kernel(qg_kv4_att
     const bool there = row < rows;
     const typename qg_elem<TYPE>::t* q = static_cast<const typename qg_elem<TYPE>::t*>(p.q) +
                                          (there ? (int64_t)(q0 + i) * p.q_token + (int64_t)(head * p.group + row - i * p.group) * p.q_head : 0);
-    s.factor[nr] = load_q<D, DIG, TYPE>(q, there, s.q[nr], p.scale_log2e, g);
+    load_q<D, DIG, NR, TYPE>(s, nr, q, there, p.scale_log2e, p.scale_log2e_lo, g);
     s.limit[nr] = !there ? 0x7fffffff : p.causal ? keys - n + i : keys - 1;
     s.m[nr] = START;
     s.l[nr] = 0.0f;
@@ -359,20 +425,26 @@ __global__ __launch_bounds__(64 * WAVES) void qg_kv4_attention_kernel(qg_kv4_att
   const int whole = min(hi, p.causal ? keys - n + wave_row / p.group + 1 : keys);
 
   if (wave_row < rows) {
-    const reader<D, SMALL> in = {p, p.pages + (int64_t)seq * p.pages_stride, head, max((keys - 1) >> p.c.lgp, 0), g, r, g};
+    const reader<D, SMALL> in(p, seq, head, keys, r, g);
     constexpr int STRIDE = TILE * (TOKENS ? WAVES : 1);
     int t0 = lo + (TOKENS ? wave * TILE : 0);
     if (t0 < hi) {
-      tile_bits<D> now, next;
-      in.load(t0, now);
+      // two tiles in turn, each requested while the other one is worked on (past the end: the last one again)
+      const int last = t0 + (hi - 1 - t0) / STRIDE * STRIDE;
+      tile_bits<D> a, b;
+      in.load(t0, a);
+      while (t0 + STRIDE + TILE <= whole) {
+        in.load(min(t0 + STRIDE, last), b);
+        step<D, DIG, NR, false>(s, a, t0, hi, r, g);
+        t0 += STRIDE;
+        in.load(min(t0 + STRIDE, last), a);
+        step<D, DIG, NR, false>(s, b, t0, hi, r, g);
+        t0 += STRIDE;
+      }
       for (; t0 < hi; t0 += STRIDE) {
-        const bool more = t0 + STRIDE < hi;
-        if (more) in.load(t0 + STRIDE, next);
-        if (t0 + TILE <= whole)
-          step<D, DIG, NR, false>(s, now, t0, hi, r, g);
-        else
-          step<D, DIG, NR, true>(s, now, t0, hi, r, g);
-        now = next;
+        in.load(min(t0 + STRIDE, last), b);
+        step<D, DIG, NR, true>(s, a, t0, hi, r, g);
+        a = b;
       }
     }
   }

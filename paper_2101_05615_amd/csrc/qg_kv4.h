@@ -176,7 +176,7 @@ struct qg_kv4_attention_args {
   const int32_t* q_starts;   // null: one query per sequence
   qg_kv4_layout c;
   int tokens, group, batch, pages_stride, max_q_len, max_kv_len, causal;
-  float scale_log2e;
+  float scale_log2e, scale_log2e_lo;  // two parts
   int split, chunk;          // workgroups that share a sequence's keys, and tokens each takes (a multiple of 32)
   int row_blocks;            // workgroups over a KV head's query rows
   int rows_pad;              // rows of a KV head in the workspace
