@@ -43,28 +43,27 @@ int check_rotation(const float* table, int max_pos, int rot, int interleaved, in
 }
 
 // ---- keys of a sequence over workgroups
-// With few sequences a workgroup per (sequence, KV head) leaves most of the 256 CUs idle, and with sequences of different lengths
-// the longest one ends alone.  Keys are dealt in chunks of equal length: as few tokens as fill the CUs FILL times over, but at
-// least LEAST (a workgroup's start and end cost as much as a few hundred tokens) and at most MOST.
-constexpr int FILL = 4, LEAST = 256, MOST = 2048, CUS = 256;
+// With few sequences a workgroup per (sequence, KV head, rows) leaves most of the 256 CUs idle, and with long ones that differ in
+// length the longest ends alone.  Keys are dealt in chunks of equal length, at least LEAST tokens, what a workgroup's start and end
+// cost.  Few rows: chunks that give every CU a workgroup.  More would cost more than it evens out: every share is written, and read by
+// the last one to arrive (131072 keys of 8 KV heads, 8 rows: 34 us in 256 shares, 40 in 512, 49 in 1024).  Many rows: workgroups run for
+// long, so eight times as many (512 queries of four sequences up to 8192 keys: 240 us whole, 203 in 1024 workgroups, 167 in 2048, 164 in
+// 3072).
+constexpr int CUS = 256;
 constexpr size_t COUNTERS = 16384;  // a fixed part of every workspace, so that calls of other extents find it zero
 
 struct share {
   int split, chunk, rows_pad;
 };
 
-share share_of(int kv_heads, int q_heads, int batch, int max_q_len, int max_kv_len) {
-  share s = {1, 0, 0};
-  const long long rows = (long long)max_q_len * (q_heads / kv_heads);
-  const long long tiles = (rows + 15) / 16, blocks = (rows + 63) / 64;
-  s.rows_pad = (int)(tiles * 16);
-  const long long units = (long long)batch * kv_heads * (rows <= 16 ? 1 : blocks);
-  const int padded = (int)(((long long)max_kv_len + 31) / 32 * 32);
-  s.chunk = padded;
-  if ((size_t)((long long)batch * kv_heads * tiles) > COUNTERS) return s;
-  long long chunk = (long long)max_kv_len * units / (FILL * CUS);
-  chunk = (chunk + 31) / 32 * 32;
-  chunk = chunk < LEAST ? LEAST : chunk > MOST && rows <= 16 ? MOST : chunk;
+share share_of(const qg_kv4_cache* c, int q_heads, int batch, int max_q_len, int max_kv_len) {
+  const long long rows = (long long)max_q_len * (q_heads / c->kv_heads), per = qg_kv4_rows_per_workgroup(c->head_dim, rows);
+  share s = {1, (max_kv_len + 63) / 64 * 64, (int)((rows + 15) / 16 * 16)};
+  const long long units = (long long)batch * c->kv_heads * ((rows + per - 1) / per);
+  if ((size_t)((long long)batch * c->kv_heads * ((rows + 15) / 16)) > COUNTERS) return s;  // (workgroups have 16 rows at least)
+  const int least = rows <= QG_KV4_FEW ? 256 : 512, workgroups = rows <= QG_KV4_FEW ? CUS : 8 * CUS;
+  long long chunk = ((long long)max_kv_len * units / workgroups + 63) / 64 * 64;
+  if (chunk < least) chunk = least;
   if (chunk >= max_kv_len) return s;
   s.chunk = (int)chunk;
   s.split = (int)((max_kv_len + chunk - 1) / chunk);
@@ -230,7 +229,7 @@ int qg_kv4_read(const qg_kv4_cache* c, const int64_t* slots, int tokens, int dty
 size_t qg_kv4_attention_workspace_bytes(const qg_kv4_cache* c, int q_heads, int batch, int max_q_len, int max_kv_len) {
   if (!c || qg_kv4_bytes(c->n_pages, c->kv_heads, c->head_dim, c->page_tokens) == 0) return 0;
   if (!extents_ok(c, q_heads, batch, max_q_len, max_kv_len) || batch == 0 || max_q_len == 0 || max_kv_len == 0) return 0;
-  return share_bytes(share_of(c->kv_heads, q_heads, batch, max_q_len, max_kv_len), c->kv_heads, batch, c->head_dim);
+  return share_bytes(share_of(c, q_heads, batch, max_q_len, max_kv_len), c->kv_heads, batch, c->head_dim);
 }
 
 int qg_kv4_attention(const qg_kv4_cache* c, const qg_kv4_attention_params* p, void* stream) {
@@ -247,16 +246,16 @@ int qg_kv4_attention(const qg_kv4_cache* c, const qg_kv4_attention_params* p, vo
   if (!aligned(p->kv_lens, 4) || !aligned(p->pages, 4) || !aligned(p->q_starts, 4)) return QG_EALIGN;
   if ((rc = check_heads(p->q, p->dtype)) != QG_OK || (rc = check_heads(p->out, p->dtype)) != QG_OK) return rc;
   const int max_q = p->q_starts ? p->max_q_len : 1;
-  share s = share_of(c->kv_heads, p->q_heads, p->batch, max_q, p->max_kv_len);
+  share s = share_of(c, p->q_heads, p->batch, max_q, p->max_kv_len);
   if (!p->workspace) {
     s.split = 1;
-    s.chunk = (p->max_kv_len + 31) / 32 * 32;
+    s.chunk = (p->max_kv_len + 63) / 64 * 64;
   }
   if (s.split > 1) {
     if (p->workspace_bytes < share_bytes(s, c->kv_heads, p->batch, c->head_dim)) return QG_EWORKSPACE;
     if (!aligned(p->workspace, 16)) return QG_EALIGN;
   }
-  if (s.chunk == 0) s.chunk = 32;
+  if (s.chunk == 0) s.chunk = 64;
   const long long rows = (long long)max_q * (p->q_heads / c->kv_heads);
   if (((long long)p->batch * c->kv_heads * s.split + 8) * ((rows + 15) / 16) > 0x7fffffffll / 256) return QG_EUNSUPPORTED;
   a.q = p->q.data;
@@ -283,8 +282,8 @@ int qg_kv4_attention(const qg_kv4_cache* c, const qg_kv4_attention_params* p, vo
   a.q_head = p->q.head_stride;
   a.o_token = p->out.token_stride;
   a.o_head = p->out.head_stride;
-  return qg_launch_kv4_attention(a, c->head_dim, p->dtype, (int)rows, static_cast<hipStream_t>(stream)) == hipSuccess ? QG_OK
-                                                                                                                  : QG_ELAUNCH;
+  const auto launch = rows <= QG_KV4_FEW ? qg_launch_kv4_attention_few : qg_launch_kv4_attention_many;
+  return launch(a, c->head_dim, p->dtype, (int)rows, static_cast<hipStream_t>(stream)) == hipSuccess ? QG_OK : QG_ELAUNCH;
 }
 
 }  // extern "C"

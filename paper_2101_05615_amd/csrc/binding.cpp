@@ -13,6 +13,7 @@
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <limits.h>
+#include <math.h>
 
 #include "qgemm.h"
 
@@ -201,6 +202,205 @@ PyObject* gemm_f32s8(PyObject*, PyObject* const* a, Py_ssize_t n) {
     return result.give();)
 }
 
+// ---- positions and the 4-bit key/value cache (kv4.py); as above, anything out of the ordinary gives None
+int element(at::ScalarType t) { return t == at::kFloat ? QG_F32 : t == at::kBFloat16 ? QG_BF16 : t == at::kHalf ? QG_F16 : -1; }
+
+// a tensor [tokens][heads][channels] with unit channel stride
+bool heads(const at::Tensor* t, qg_heads* out) {
+  if (!t || !t->is_cuda() || t->dim() != 3 || (t->stride(2) != 1 && t->size(2) > 1) || element(t->scalar_type()) < 0) return false;
+  out->data = t->data_ptr();
+  out->token_stride = t->stride(0);
+  out->head_stride = t->stride(1);
+  return t->size(0) <= INT_MAX && t->size(1) <= INT_MAX && t->size(2) <= INT_MAX;
+}
+bool same_kind(const at::Tensor& a, const at::Tensor& b) { return a.scalar_type() == b.scalar_type() && a.size(0) == b.size(0) && a.size(2) == b.size(2); }
+
+// a contiguous vector of `n` whole numbers
+template <typename T>
+bool numbers(PyObject* o, at::ScalarType type, int64_t n, const T** out) {
+  const at::Tensor* const t = tensor(o);
+  if (!t || !t->is_cuda() || t->scalar_type() != type || t->dim() != 1 || t->size(0) != n || !t->is_contiguous()) return false;
+  *out = static_cast<const T*>(t->data_ptr());
+  return true;
+}
+bool angles(PyObject* o, const float** table, int* max_pos, int* rot) {
+  const at::Tensor* const t = tensor(o);
+  if (!t || !t->is_cuda() || t->scalar_type() != at::kFloat || t->dim() != 2 || !t->is_contiguous() || t->size(0) > INT_MAX || t->size(1) > INT_MAX)
+    return false;
+  *table = static_cast<const float*>(t->data_ptr());
+  *max_pos = (int)t->size(0);
+  *rot = (int)t->size(1);
+  return true;
+}
+struct cache_handle {
+  const qg_kv4_cache* c;
+};
+bool cache(PyObject* o, cache_handle* out) {  // the address of the descriptor that the object holds
+  PyObject* const t = PyObject_GetAttr(o, g_name_fast);
+  if (!t) return slow();
+  out->c = static_cast<const qg_kv4_cache*>(PyLong_AsVoidPtr(t));
+  Py_DECREF(t);
+  if (PyErr_Occurred()) return slow();
+  return out->c != nullptr;
+}
+// the caller's output, or a new one like `like`; both as a new reference
+PyObject* heads_output(PyObject* given, const at::Tensor& like, at::Tensor* out, qg_heads* h) {
+  if (given == Py_None) {
+    *out = at::empty({like.size(0), like.size(1), like.size(2)}, like.options());
+    if (!heads(out, h)) return nullptr;
+    return THPVariable_Wrap(*out);
+  }
+  const at::Tensor* const t = tensor(given);
+  if (!heads(t, h) || !same_kind(*t, like) || t->size(1) != like.size(1)) return nullptr;
+  *out = *t;
+  return Py_NewRef(given);
+}
+bool truth(PyObject* o, int* out) {
+  *out = PyObject_IsTrue(o);
+  return *out >= 0 || slow();
+}
+
+// (x, positions, table, interleaved, inverse, out or None)
+PyObject* rope(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  if (n != 6) Py_RETURN_NONE;
+  QG_OR_SLOW(
+    const at::Tensor* const x = tensor(a[0]);
+    qg_heads xh = {}; qg_heads yh = {};
+    const int32_t* positions = nullptr; const float* table = nullptr;
+    int max_pos = 0; int rot = 0; int interleaved = 0; int inverse = 0; void* s = nullptr;
+    if (!heads(x, &xh) || !numbers(a[1], at::kInt, x->size(0), &positions) || !angles(a[2], &table, &max_pos, &rot) ||
+        !truth(a[3], &interleaved) || !truth(a[4], &inverse) || !stream(&s))
+      Py_RETURN_NONE;
+    at::Tensor y;
+    reference result{heads_output(a[5], *x, &y, &yh)};
+    if (!result.o) { PyErr_Clear(); Py_RETURN_NONE; }
+    const int type = element(x->scalar_type()); const int T = (int)x->size(0); const int H = (int)x->size(1); const int D = (int)x->size(2);
+    int rc;
+    Py_BEGIN_ALLOW_THREADS
+    rc = qg_rope(&xh, type, T, H, D, positions, table, max_pos, rot, interleaved, inverse, &yh, s);
+    Py_END_ALLOW_THREADS
+    if (rc != QG_OK) Py_RETURN_NONE;
+    return result.give();)
+}
+
+// (cache, k, v, slots, positions or None, table or None, interleaved, q or None, q_out or None) -> q_out, True without queries
+PyObject* kv4_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  if (n != 9) Py_RETURN_NONE;
+  QG_OR_SLOW(
+    cache_handle c = {};
+    qg_kv4_append_params p = {};
+    const at::Tensor* const k = tensor(a[1]);
+    const at::Tensor* const v = tensor(a[2]);
+    void* s = nullptr;
+    if (!cache(a[0], &c) || !heads(k, &p.k) || !heads(v, &p.v) || !same_kind(*k, *v) || k->size(1) != c.c->kv_heads || v->size(1) != c.c->kv_heads ||
+        k->size(2) != c.c->head_dim || !numbers(a[3], at::kLong, k->size(0), &p.slots) || !truth(a[6], &p.interleaved) || !stream(&s))
+      Py_RETURN_NONE;
+    if (a[4] != Py_None && (!numbers(a[4], at::kInt, k->size(0), &p.positions) || !angles(a[5], &p.table, &p.max_pos, &p.rot))) Py_RETURN_NONE;
+    at::Tensor out;
+    reference result{nullptr};
+    if (a[7] != Py_None) {
+      const at::Tensor* const q = tensor(a[7]);
+      if (!heads(q, &p.q) || !same_kind(*q, *k)) Py_RETURN_NONE;
+      p.q_heads = (int)q->size(1);
+      result.o = heads_output(a[8], *q, &out, &p.q_out);
+      if (!result.o) { PyErr_Clear(); Py_RETURN_NONE; }
+    } else if (a[8] != Py_None) {
+      Py_RETURN_NONE;
+    }
+    p.dtype = element(k->scalar_type());
+    p.tokens = (int)k->size(0);
+    int rc;
+    Py_BEGIN_ALLOW_THREADS
+    rc = qg_kv4_append(c.c, &p, s);
+    Py_END_ALLOW_THREADS
+    if (rc != QG_OK) Py_RETURN_NONE;
+    if (!result.o) Py_RETURN_TRUE;
+    return result.give();)
+}
+
+// (cache, q, pages, kv_lens, q_starts or None, max_q_len, max_kv_len or None, scale or None, causal, workspace or None, out or None)
+PyObject* kv4_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  if (n != 11) Py_RETURN_NONE;
+  QG_OR_SLOW(
+    cache_handle c = {};
+    qg_kv4_attention_params p = {};
+    const at::Tensor* const q = tensor(a[1]);
+    const at::Tensor* const pages = tensor(a[2]);
+    void* s = nullptr;
+    if (!cache(a[0], &c) || !heads(q, &p.q) || q->size(2) != c.c->head_dim || !pages || !pages->is_cuda() || pages->scalar_type() != at::kInt ||
+        pages->dim() != 2 || (pages->stride(1) != 1 && pages->size(1) > 1) || pages->size(0) > INT_MAX || pages->size(1) > INT_MAX)
+      Py_RETURN_NONE;
+    const int64_t B = pages->size(0); const int64_t stride = B > 1 ? pages->stride(0) : pages->size(1);
+    if (!numbers(a[3], at::kInt, B, &p.kv_lens) || (a[4] != Py_None && !numbers(a[4], at::kInt, B + 1, &p.q_starts)) ||
+        !integer(a[5], &p.max_q_len) || !truth(a[8], &p.causal) || stride > INT_MAX || stride < INT_MIN || !stream(&s))
+      Py_RETURN_NONE;
+    const int64_t held = pages->size(1) * (int64_t)c.c->page_tokens;
+    if (a[6] == Py_None) {
+      if (held > INT_MAX) Py_RETURN_NONE;
+      p.max_kv_len = (int)held;
+    } else if (!integer(a[6], &p.max_kv_len) || p.max_kv_len > held) {
+      Py_RETURN_NONE;
+    }
+    double scale = 0.0;
+    if (a[7] == Py_None) {
+      scale = 1.0 / sqrt((double)c.c->head_dim);
+    } else {
+      scale = PyFloat_AsDouble(a[7]);
+      if (scale == -1.0 && PyErr_Occurred()) { PyErr_Clear(); Py_RETURN_NONE; }
+    }
+    if (a[9] != Py_None) {
+      const at::Tensor* const w = tensor(a[9]);
+      if (!w || !w->is_cuda() || !w->is_contiguous()) Py_RETURN_NONE;
+      p.workspace = w->data_ptr();
+      p.workspace_bytes = (size_t)w->numel() * w->element_size();
+    }
+    at::Tensor out;
+    reference result{heads_output(a[10], *q, &out, &p.out)};
+    if (!result.o) { PyErr_Clear(); Py_RETURN_NONE; }
+    p.pages = static_cast<const int32_t*>(pages->data_ptr());
+    p.scale = (float)scale;
+    p.dtype = element(q->scalar_type());
+    p.tokens = (int)q->size(0);
+    p.q_heads = (int)q->size(1);
+    p.batch = (int)B;
+    p.pages_stride = (int)stride;
+    int rc;
+    Py_BEGIN_ALLOW_THREADS
+    rc = qg_kv4_attention(c.c, &p, s);
+    Py_END_ALLOW_THREADS
+    if (rc != QG_OK) Py_RETURN_NONE;
+    return result.give();)
+}
+
+// (cache, slots, element type, None, None) -> (k, v)
+PyObject* kv4_read(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  if (n != 5) Py_RETURN_NONE;
+  QG_OR_SLOW(
+    cache_handle c = {};
+    const at::Tensor* const slots = tensor(a[1]);
+    const int64_t* at_slots = nullptr;
+    int type = 0; void* s = nullptr;
+    if (!cache(a[0], &c) || !slots || slots->dim() != 1 || !numbers(a[1], at::kLong, slots->size(0), &at_slots) || slots->size(0) > INT_MAX ||
+        !integer(a[2], &type) || type < QG_F32 || type > QG_F16 || a[3] != Py_None || a[4] != Py_None || !stream(&s))
+      Py_RETURN_NONE;
+    const auto options = slots->options().dtype(type == QG_F32 ? at::kFloat : type == QG_BF16 ? at::kBFloat16 : at::kHalf);
+    const at::Tensor k = at::empty({slots->size(0), c.c->kv_heads, c.c->head_dim}, options);
+    const at::Tensor v = at::empty({slots->size(0), c.c->kv_heads, c.c->head_dim}, options);
+    qg_heads kh = {}; qg_heads vh = {};
+    if (!heads(&k, &kh) || !heads(&v, &vh)) Py_RETURN_NONE;
+    const int T = (int)slots->size(0);
+    int rc;
+    Py_BEGIN_ALLOW_THREADS
+    rc = qg_kv4_read(c.c, at_slots, T, type, &kh, &vh, s);
+    Py_END_ALLOW_THREADS
+    if (rc != QG_OK) Py_RETURN_NONE;
+    reference first{THPVariable_Wrap(k)};
+    reference second{THPVariable_Wrap(v)};
+    PyObject* const both = first.o && second.o ? PyTuple_Pack(2, first.o, second.o) : nullptr;
+    if (!both) { PyErr_Clear(); Py_RETURN_NONE; }
+    return both;)
+}
+
 // ---- a call whose arguments are marshalled once
 enum call_kind { CALL_GEMM, CALL_CONV_GROUP, CALL_CONV_DENSE, CALL_KINDS };
 const char* const call_names[CALL_KINDS] = {"qg_gemm_u8s8_requant", "qg_conv_groupwise_u8s8_requant", "qg_conv_dense_u8s8_requant"};
@@ -295,6 +495,10 @@ PyObject* init(PyObject*, PyObject* args) {
 PyMethodDef methods[] = {
     {"gemm_u8s8_requant", QG_FAST(gemm_u8s8_requant), METH_FASTCALL, nullptr},
     {"gemm_f32s8", QG_FAST(gemm_f32s8), METH_FASTCALL, nullptr},
+    {"rope", QG_FAST(rope), METH_FASTCALL, nullptr},
+    {"kv4_append", QG_FAST(kv4_append), METH_FASTCALL, nullptr},
+    {"kv4_attention", QG_FAST(kv4_attention), METH_FASTCALL, nullptr},
+    {"kv4_read", QG_FAST(kv4_read), METH_FASTCALL, nullptr},
     {"init", init, METH_VARARGS, nullptr},
     {nullptr, nullptr, 0, nullptr},
 };

@@ -189,4 +189,12 @@ hipError_t qg_launch_rope_table(const double* freqs, int rot, int max_pos, doubl
 hipError_t qg_launch_rope(const qg_rope_args& a, int dtype, hipStream_t s);
 hipError_t qg_launch_kv4_append(const qg_kv4_append_args& a, int head_dim, int dtype, hipStream_t s);
 hipError_t qg_launch_kv4_read(const qg_kv4_read_args& a, int head_dim, int dtype, hipStream_t s);
-hipError_t qg_launch_kv4_attention(const qg_kv4_attention_args& a, int head_dim, int dtype, int rows, hipStream_t s);
+// Query rows of a KV head (its query heads times a sequence's queries): up to QG_KV4_FEW a wave has all of them; beyond, the waves
+// of a workgroup share unpacked keys and values.
+#define QG_KV4_FEW 32
+static inline int qg_kv4_rows_per_workgroup(int head_dim, long long rows) {
+  if (rows <= QG_KV4_FEW) return head_dim == 256 || rows <= 16 ? 16 : 32;
+  return 128;  // (fp32 with 128 channels and less: 64; the split of the keys is the same for all types)
+}
+hipError_t qg_launch_kv4_attention_few(const qg_kv4_attention_args& a, int head_dim, int dtype, int rows, hipStream_t s);
+hipError_t qg_launch_kv4_attention_many(const qg_kv4_attention_args& a, int head_dim, int dtype, int rows, hipStream_t s);

@@ -1,0 +1,580 @@
+// What the two kernels of the attention over the 4-bit cache share: codes into operands of the matrix cores, scores into weights,
+// queries, and the joining of results.  Not part of the public interface.
+//
+// A wave owns 16 query rows (the query heads that share a KV head, times the queries of a sequence), or NR times that, and walks
+// over tiles of 32 tokens.  Both products run on v_mfma_f32_16x16x32_f16, transposed:
+//   S^T = K Q^T   first operand 16 tokens x 32 channels, second 32 channels x 16 rows
+//   O^T = V^T P^T first operand 16 channels x 32 tokens, second 32 tokens x 16 rows
+// so that a lane keeps to one query row (its column l % 16) from the scores to the output: the running maximum and sum are a
+// register each, and what a lane gets of S^T, tokens 8g .. 8g+7 (g = l / 16; the rows of the two key tiles are dealt that way),
+// is in place as the second operand of the other product.
+//
+// The codes never become dequantized numbers: the scales go to the other side, a key's onto the score, a value's onto the
+// probability.  The 16 scale-and-theta words of 8 tokens lie in the 16 lanes of a DPP row, where every lane of the row reaches them
+// as an operand.  The zero points:
+//   values  code - theta is a whole number of at most 15 and exact in fp16.  A dword of codes becomes eight of them with one shift,
+//           four and-or (the exponent of 1024 put around a nibble) and four packed additions that take away 1024 + theta.
+//   keys    a nibble alone in bits 4 to 7 of an fp16 is the number code * 2^-20, which the matrix cores take as it is (four ANDs and
+//           three shifts), and theta comes off the sum, sum q (code - theta) = sum q code - theta sum q, with one fused multiply-add
+//           per score.  fp32 results would see the cancellation: there keys go as values do.
+// (Taking theta off the second product's sums as well is 10 % fewer instructions, but where the token that has all the weight is
+// worth 0, 2^-21 of its neighbours' size is left: measured, 6 % of a result that came from the other tokens.  Nibbles in bits 0
+// to 3 would save two shifts, but products of numbers this small are aligned by the exponent 2^-14 that their format gives them:
+// over 32 products code * 2^-24 measured 2e-6 off the sum of their sizes, code * 2^-20 5e-8.)
+//
+// Rounding.  Queries become fp16 after a power of two per row that puts the largest channel near 2^14: exact for fp16 and
+// bf16 channels down to 2^-24 of the largest; fp32 queries take two fp16 (22 bits).  Probabilities times value scale become fp16
+// (two for fp32 results) against a running reference for both, so that they lie below 2^14 and keep 11 bits down to 2^-14.
+// Scores, maxima, sums and outputs are fp32.
+#pragma once
+
+#include "qg_kv4.h"
+
+namespace {
+
+typedef _Float16 h2 __attribute__((ext_vector_type(2)));
+typedef _Float16 h8 __attribute__((ext_vector_type(8)));
+typedef float f4 __attribute__((ext_vector_type(4)));
+typedef unsigned u2 __attribute__((ext_vector_type(2)));
+typedef unsigned u4 __attribute__((ext_vector_type(4)));
+typedef unsigned long long u64;
+
+constexpr int TILE = 32;         // tokens of a wave's step
+constexpr float START = -1e30f;  // the running maximum before the first key
+constexpr float BOOST = 4.0f;    // probabilities are held times 2^BOOST ...
+constexpr float SLACK = 12.0f;   // ... and the reference moves when one would pass 2^SLACK
+
+template <int J>
+__device__ inline float row_lane(float x) {  // lane J of the caller's row of 16
+  return __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, x), 0x150 + J, 0xf, 0xf, true));
+}
+template <int J>
+__device__ inline unsigned row_lane(unsigned x) {
+  return (unsigned)__builtin_amdgcn_mov_dpp((int)x, 0x150 + J, 0xf, 0xf, true);
+}
+
+union frag {
+  unsigned u[4];
+  h2 h[4];
+  h8 v;
+};
+
+__device__ inline h2 as_h2(unsigned x) { return __builtin_bit_cast(h2, x); }
+__device__ inline f4 product(const frag& a, const frag& b, f4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a.v, b.v, c, 0, 0, 0); }
+
+// Eight codes of a dword as four pairs (nibbles 0 4, 1 5, 2 6, 3 7), times 2^-20
+__device__ inline void spread(unsigned x, unsigned* out) {
+  out[0] = x << 4 & 0x00f000f0u;
+  out[1] = x & 0x00f000f0u;
+  out[2] = x >> 4 & 0x00f000f0u;
+  out[3] = x >> 8 & 0x00f000f0u;
+}
+
+// The same less theta, in units of 1: 1024 + c or 1024 + 16 c, whose bits are a nibble under the exponent of 1024, less 1024 + theta.
+// low: -(1024 + theta) twice; high: -(64 + theta).  (The masks live in registers: and-or takes no constants.)
+struct masks {
+  unsigned even, odd, magic;
+  __device__ inline masks() : even(0x000f000fu), odd(0x00f000f0u), magic(0x64006400u) { asm("" : "+s"(even), "+s"(odd), "+v"(magic)); }
+};
+__device__ inline void spread_less(unsigned x, const masks& m, h2 low, h2 high, unsigned* out) {
+  const h2 sixteenth = {(_Float16)0.0625f, (_Float16)0.0625f};
+  const unsigned y = x >> 8;
+  out[0] = __builtin_bit_cast(unsigned, as_h2((x & m.even) | m.magic) + low);
+  out[1] = __builtin_bit_cast(unsigned, __builtin_elementwise_fma(as_h2((x & m.odd) | m.magic), sixteenth, high));
+  out[2] = __builtin_bit_cast(unsigned, as_h2((y & m.even) | m.magic) + low);
+  out[3] = __builtin_bit_cast(unsigned, __builtin_elementwise_fma(as_h2((y & m.odd) | m.magic), sixteenth, high));
+}
+
+// theta and its neighbour's in two forms for spread_less(), a pair from one or two tokens
+struct zero_pair {
+  unsigned low, high;
+  __device__ inline explicit zero_pair(unsigned pair) : low(pair + 0xE400E400u), high((pair << 4) + 0xD400D400u) {}
+};
+
+// For the values of a row's 8 tokens, words in lanes 8 .. 15: tokens 2 i and 2 i + 1
+struct zero_points {
+  h2 low[4], high[4];
+  __device__ inline explicit zero_points(unsigned word) {
+    const unsigned theta = word & 15u;
+    const unsigned next = (unsigned)__builtin_amdgcn_mov_dpp((int)theta, 0x101, 0xf, 0xf, true);  // row_shl:1
+    const zero_pair z(theta | next << 16);
+    low[0] = as_h2(row_lane<8>(z.low));
+    low[1] = as_h2(row_lane<10>(z.low));
+    low[2] = as_h2(row_lane<12>(z.low));
+    low[3] = as_h2(row_lane<14>(z.low));
+    high[0] = as_h2(row_lane<8>(z.high));
+    high[1] = as_h2(row_lane<10>(z.high));
+    high[2] = as_h2(row_lane<12>(z.high));
+    high[3] = as_h2(row_lane<14>(z.high));
+  }
+};
+
+// Four channels of 8 tokens (a dword: two tokens) as the first operands of four products
+__device__ inline void spread_values(const u4& x, const masks& m, const zero_points& z, frag* out) {
+#pragma unroll
+  for (int t = 0; t < 4; ++t) {
+    unsigned y[4];
+    spread_less(x[t], m, z.low[t], z.high[t], y);
+#pragma unroll
+    for (int c = 0; c < 4; ++c) out[c].u[t] = y[c];
+  }
+}
+
+// Where a lane's bytes lie.  Keys: of a token's D/2 bytes lane group g takes KEY_BYTES in each of KEY_LOADS pieces.  Values: of
+// 8 tokens lane r takes 16 bytes, four channels, in each of D/64 pieces.
+template <int D>
+struct lay {
+  static constexpr int KEY_BYTES = D == 64 ? 8 : 16, KEY_LOADS = D / 8 / KEY_BYTES, KEY_WORDS = KEY_BYTES / 4, VALUE_LOADS = D / 64;
+  // first channel of a lane's dword f of keys; of its outputs 4 i .. 4 i + 3 (16 consecutive ones in all)
+  static __device__ constexpr int key_channel(int f, int g) { return f / KEY_WORDS * (8 * KEY_BYTES) + g * (2 * KEY_BYTES) + f % KEY_WORDS * 8; }
+  static __device__ constexpr int out_channel(int i, int g) { return 64 * i + 16 * g; }
+};
+
+// The pages of a sequence.  An entry that is no page of the cache reads as page 0.
+struct page_reader {
+  uint8_t* data;
+  const int32_t* table;
+  int entries, n_pages, lgp;
+  size_t page_bytes, head_bytes;
+  int head;
+  template <int D>
+  __device__ inline void init(const qg_kv4_attention_args& p, int seq, int kv_head) {
+    data = p.c.data;
+    table = p.pages + (int64_t)seq * p.pages_stride;
+    entries = p.pages_stride;
+    n_pages = p.c.n_pages;
+    lgp = p.c.lgp;
+    head_bytes = (size_t)(D + 8) << lgp;
+    page_bytes = head_bytes * p.c.heads;
+    head = kv_head;
+  }
+  __device__ inline unsigned page(int index) const { return (unsigned)table[min(index, entries - 1)]; }
+  __device__ inline const uint8_t* block(unsigned page) const {
+    page = page < (unsigned)n_pages ? page : 0u;
+    return data + page * page_bytes + head * head_bytes;
+  }
+};
+
+// Where a lane finds its part of a tile of 32 tokens.  SMALL: pages of 16 tokens, two to a tile; otherwise a tile lies in one page,
+// whose address is the same for all lanes.
+struct page_ids {
+  unsigned first, second;
+};
+struct spots {
+  const uint8_t *keys, *values, *words;
+};
+template <int D, bool SMALL>
+struct reader : page_reader {
+  typedef lay<D> L;
+  unsigned key_lane, value_lane, word_lane;  // this lane's bytes past the tile's
+  bool key_half, value_half;                 // SMALL: the lane's run of 8 tokens lies in the tile's second page
+
+  __device__ inline reader(const qg_kv4_attention_args& p, int seq, int head, int r, int g) {
+    init<D>(p, seq, head);
+    const int key_run = r >> 2, key_at = SMALL ? key_run & 1 : key_run, value_at = SMALL ? g & 1 : g;
+    key_lane = (unsigned)((8 * key_at + (r & 3)) * (D / 2) + g * L::KEY_BYTES);
+    value_lane = (unsigned)(value_at * (4 * D) + r * 16);
+    word_lane = (unsigned)(value_at * 64 + r * 4);
+    key_half = key_run >= 2;
+    value_half = g >= 2;
+  }
+  __device__ inline page_ids pages(int t0) const {
+    if (SMALL) return {page(t0 >> 4), page((t0 >> 4) + 1)};
+    return {page(t0 >> lgp), 0u};
+  }
+  __device__ inline spots at(int t0, page_ids ids) const {
+    spots s;
+    if (SMALL) {
+      const uint8_t *first = block(ids.first), *second = block(ids.second);
+      s.keys = key_half ? second : first;
+      s.values = (value_half ? second : first) + 16 * (D / 2);
+      s.words = s.values + 16 * (D / 2);
+    } else {
+      const uint8_t* page = block(ids.first);
+      const int P = 1 << lgp, at = t0 & (P - 1);
+      s.keys = page + at * (D / 2);
+      s.values = page + (P + at) * (D / 2);
+      s.words = page + P * D + at * 8;
+    }
+    return s;
+  }
+  // tile a of 16 tokens: row r is token 8 (r / 4) + 4 a + r % 4
+  __device__ inline void load_keys(const spots& s, int a, int i, unsigned* out) const {
+    const uint8_t* from = s.keys + key_lane + a * 4 * (D / 2) + i * 64;
+    if (D == 64) {
+      const u2 x = *reinterpret_cast<const u2*>(from);
+      out[0] = x[0];
+      out[1] = x[1];
+    } else {
+      const u4 x = *reinterpret_cast<const u4*>(from);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) out[j] = x[j];
+    }
+  }
+  __device__ inline u4 load_values(const spots& s, int i) const { return *reinterpret_cast<const u4*>(s.values + value_lane + i * 256); }
+  __device__ inline unsigned load_word(const spots& s) const { return *reinterpret_cast<const unsigned*>(s.words + word_lane); }
+};
+// theta, twice, of the token that this lane holds as first operand of tile a
+__device__ inline unsigned key_zero(unsigned theta, int a, int r) {
+  return (unsigned)__builtin_amdgcn_ds_bpermute((16 * (r >> 2) + 4 * a + (r & 3)) * 4, (int)theta) * 0x10001u;
+}
+
+// What a wave keeps of its NR tiles of 16 rows
+template <int D, int DIG, int NR>
+struct state {
+  f4 o[NR][D / 16];
+  float m[NR], l[NR];              // reference of the exponents (log2), sum (this lane's tokens)
+  float factor[NR], factor_lo[NR]; // log2 score of a product and a key's scale, in two parts (the second: DIG 2)
+  int limit[NR];                   // last token that the row sees
+  int vref;                        // biased exponent of the value scales' reference, 1 .. 253
+  __device__ inline void start() {
+    vref = 1;
+#pragma unroll
+    for (int n = 0; n < NR; ++n) {
+      m[n] = START;
+      l[n] = 0.0f;
+#pragma unroll
+      for (int c = 0; c < D / 16; ++c) o[n][c] = (f4){0.0f, 0.0f, 0.0f, 0.0f};
+    }
+  }
+};
+
+__device__ inline float across_max(float x) {  // over the four lanes of a row of queries
+  x = fmaxf(x, __shfl_xor(x, 16));
+  return fmaxf(x, __shfl_xor(x, 32));
+}
+__device__ inline float across_sum(float x) {
+  x += __shfl_xor(x, 16);
+  return x + __shfl_xor(x, 32);
+}
+
+template <int DIG>
+__device__ inline float exponent(float z, float factor, float factor_lo, float base) {
+  // DIG 2: the factor's own rounding (2^-24 of every score) is more than the rest of an fp32 result's error
+  return DIG == 2 ? __builtin_fmaf(z, factor, __builtin_fmaf(z, factor_lo, base)) : __builtin_fmaf(z, factor, base);
+}
+
+// Products of a tile's 8 tokens (z[n][a][i]: token 8g + 4a + i) into exponents against the running references, which move rarely.
+// MASKED: tokens from `end` on are not there (`word` is 0 for them), and a row may end inside the tile.
+template <int D, int DIG, int NR, bool MASKED>
+__device__ inline void exponents(state<D, DIG, NR>& s, f4 (*z)[2], unsigned word, int t0, int end, int r, int g, float (*y)[8]) {
+  const int vexp = (word & 0x7f800000u) != 0x7f800000u && r >= 8 ? min((int)(word >> 23 & 255u), 253) : 0;
+  bool move = vexp > s.vref;
+  int limit[NR];  // the last of the lane's 8 tokens that the row sees
+  if (MASKED) {
+#pragma unroll
+    for (int n = 0; n < NR; ++n) limit[n] = min(s.limit[n], end - 1) - t0 - 8 * g;
+  }
+#pragma unroll
+  for (int n = 0; n < NR; ++n) {
+    const float scale = __builtin_bit_cast(float, word & ~15u);
+    const float ks[8] = {row_lane<0>(scale), row_lane<1>(scale), row_lane<2>(scale), row_lane<3>(scale),
+                         row_lane<4>(scale), row_lane<5>(scale), row_lane<6>(scale), row_lane<7>(scale)};
+    const float base = BOOST - s.m[n];
+    float top = -__builtin_inff();
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      z[n][j >> 2][j & 3] *= ks[j];
+      y[n][j] = exponent<DIG>(z[n][j >> 2][j & 3], s.factor[n], s.factor_lo[n], base);
+      if (MASKED) y[n][j] = j > limit[n] ? -__builtin_inff() : y[n][j];
+      top = fmaxf(top, y[n][j]);
+    }
+    move |= top > SLACK;
+  }
+  if (__builtin_expect(__ballot(move) != 0ull, 0)) {
+    int e = vexp;
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) e = max(e, __shfl_xor(e, d));
+    const int vref = max(s.vref, e);
+    const float shrink = __builtin_amdgcn_exp2f((float)(s.vref - vref));
+    s.vref = vref;
+#pragma unroll
+    for (int n = 0; n < NR; ++n) {
+      float high = -__builtin_inff();
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const float x = z[n][j >> 2][j & 3] * s.factor[n];
+        high = fmaxf(high, MASKED && j > limit[n] ? -__builtin_inff() : x);
+      }
+      const float top = fmaxf(s.m[n], across_max(high));
+      const float f = __builtin_amdgcn_exp2f(s.m[n] - top);
+      s.m[n] = top;
+      s.l[n] *= f;
+#pragma unroll
+      for (int i = 0; i < D / 16; ++i) s.o[n][i] *= f * shrink;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        y[n][j] = exponent<DIG>(z[n][j >> 2][j & 3], s.factor[n], s.factor_lo[n], BOOST - top);
+        if (MASKED) y[n][j] = j > limit[n] ? -__builtin_inff() : y[n][j];
+      }
+    }
+  }
+}
+
+// ... and those into the second operands of the other product: probability times value scale
+template <int D, int DIG, int NR, bool MASKED>
+__device__ inline void weights(state<D, DIG, NR>& s, const float (*y)[8], unsigned word, frag (*p)[DIG]) {
+#pragma unroll
+  for (int n = 0; n < NR; ++n) {
+    const float scale = __builtin_bit_cast(float, word & ~15u) * __builtin_bit_cast(float, (unsigned)(254 - s.vref) << 23);
+    const float vs[8] = {row_lane<8>(scale),  row_lane<9>(scale),  row_lane<10>(scale), row_lane<11>(scale),
+                         row_lane<12>(scale), row_lane<13>(scale), row_lane<14>(scale), row_lane<15>(scale)};
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const float e = __builtin_amdgcn_exp2f(y[n][j]);
+      s.l[n] += e;
+      float x = e * vs[j];
+      if (MASKED) x = y[n][j] == -__builtin_inff() ? 0.0f : x;  // (a masked value may be NaN)
+      const _Float16 hi = (_Float16)x;
+      p[n][0].v[j] = hi;
+      if (DIG == 2) p[n][DIG - 1].v[j] = (_Float16)(x - (float)hi);
+    }
+  }
+}
+
+// The channels of a query that a lane needs, as they lie in memory
+template <int D, int TYPE>
+struct raw_query {
+  typename qg_elem<TYPE>::t x[D / 4];
+  __device__ inline void load(const typename qg_elem<TYPE>::t* q, bool there, int g) {
+    typedef typename qg_elem<TYPE>::t t;
+    typedef lay<D> L;
+    constexpr int W = 16 / sizeof(t), RUN = 2 * L::KEY_BYTES;
+    typedef t vec __attribute__((ext_vector_type(W)));
+    typedef vec vec_any __attribute__((aligned(sizeof(t))));
+#pragma unroll
+    for (int i = 0; i < D / 4; ++i) x[i] = (t)0.0f;
+    if (!there) return;
+#pragma unroll
+    for (int i = 0; i < D / 4; i += W) {
+      const vec v = *reinterpret_cast<const vec_any*>(q + L::key_channel(i / RUN * L::KEY_WORDS, g) + i % RUN);
+#pragma unroll
+      for (int j = 0; j < W; ++j) x[i + j] = v[j];
+    }
+  }
+};
+
+// ... as fp16 scaled by a power of two; returns the power
+template <int D, int DIG, int TYPE>
+__device__ inline int split_query(const raw_query<D, TYPE>& raw, frag (*q)[D / 32]) {
+  float x[D / 4];
+  unsigned top = 0u;
+#pragma unroll
+  for (int i = 0; i < D / 4; ++i) {
+    x[i] = qg_elem<TYPE>::up(raw.x[i]);
+    top = max(top, __builtin_bit_cast(unsigned, x[i]) & 0x7fffffffu);
+  }
+  top = max(top, (unsigned)__shfl_xor((int)top, 16));
+  top = max(top, (unsigned)__shfl_xor((int)top, 32));
+  const int shift = top == 0u ? 0 : 14 + 127 - max((int)(top >> 23), 1);
+#pragma unroll
+  for (int i = 0; i < D / 32; ++i)
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const int c = 8 * i + (j >> 1) + 4 * (j & 1);  // the order in which the codes of a dword are spread
+      // (an infinity or NaN: the row's scores become NaN)
+      const float y = top < 0x7f800000u ? __builtin_ldexpf(x[c], shift) : __builtin_nanf("");
+      const _Float16 hi = (_Float16)y;
+      q[0][i].v[j] = hi;
+      if (DIG == 2) q[DIG - 1][i].v[j] = (_Float16)(y - (float)hi);
+    }
+  return shift;
+}
+
+// Which rows, keys and workgroups a workgroup deals with
+struct job {
+  int head, seq, slice, slices, rb;
+  int q0, n, keys;           // the sequence's first query, its queries, its keys
+  int rows, row0, last_row;  // of the KV head; this workgroup's first and last
+  int lo, hi;                // its tokens
+  template <int ROWS>
+  __device__ inline bool init(const qg_kv4_attention_args& p) {
+    // Workgroups over the rows of one (sequence, KV head, share of the keys) read the same keys: ids that differ by eight share an
+    // L2.  Heads come first in the numbering of units: with a sequence's shares side by side, shares that only long sequences have
+    // would fall to the same few XCDs.
+    const int units = p.batch * p.c.heads * p.split;
+    const int id = (int)blockIdx.x, unit = (id / (8 * p.row_blocks)) * 8 + id % 8;
+    if (unit >= units) return false;
+    rb = p.row_blocks - 1 - (id / 8) % p.row_blocks;  // (the rows that see the most keys first)
+    head = unit % p.c.heads;
+    seq = (unit / p.c.heads) % p.batch;
+    slice = unit / p.c.heads / p.batch;
+    q0 = seq;
+    n = 1;
+    if (p.q_starts != nullptr) {
+      q0 = min(max(p.q_starts[seq], 0), p.tokens);
+      n = min(max(p.q_starts[seq + 1], q0), p.tokens) - q0;
+    }
+    keys = min(max(p.kv_lens[seq], 0), p.max_kv_len);
+    rows = min(n, p.max_q_len) * p.group;
+    row0 = rb * ROWS;
+    if (row0 >= rows) return false;
+    last_row = min(row0 + ROWS, rows) - 1;
+    const int seen = p.causal ? min(max(keys - n + last_row / p.group + 1, 0), keys) : keys;  // keys that some row sees
+    slices = max((seen + p.chunk - 1) / p.chunk, 1);
+    lo = slice * p.chunk;
+    hi = min(lo + p.chunk, seen);
+    return slice < slices;
+  }
+  // keys that all rows from `row` on see
+  __device__ inline int seen_by(const qg_kv4_attention_args& p, int row) const {
+    return min(hi, p.causal ? keys - n + row / p.group + 1 : keys);
+  }
+  __device__ inline int limit(const qg_kv4_attention_args& p, int row) const {
+    return row >= rows ? 0x7fffffff : p.causal ? keys - n + row / p.group : keys - 1;
+  }
+  template <int TYPE>
+  __device__ inline const typename qg_elem<TYPE>::t* query(const qg_kv4_attention_args& p, int row) const {
+    const int i = row / p.group;
+    return static_cast<const typename qg_elem<TYPE>::t*>(p.q) +
+           (row < rows ? (int64_t)(q0 + i) * p.q_token + (int64_t)(head * p.group + row - i * p.group) * p.q_head : 0);
+  }
+  // consecutive channels of a finished row
+  template <int TYPE, int N>
+  __device__ inline void write(const qg_kv4_attention_args& p, int row, int c, const float* x) const {
+    typedef typename qg_elem<TYPE>::t t;
+    const int i = row / p.group;
+    qg_store<TYPE, N>(static_cast<t*>(p.out) + (int64_t)(q0 + i) * p.o_token + (int64_t)(head * p.group + row - i * p.group) * p.o_head + c, x);
+  }
+};
+
+// A wave's rows divided by their sums; returns the sum's log2 (-infinity: no key)
+template <int D, int DIG, int NR>
+__device__ inline void finish(state<D, DIG, NR>& s, float* lse) {
+#pragma unroll
+  for (int n = 0; n < NR; ++n) {
+    const float l = across_sum(s.l[n]);
+    lse[n] = s.m[n] + __builtin_amdgcn_logf(l);
+    const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+#pragma unroll
+    for (int c = 0; c < D / 16; ++c)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) s.o[n][c][e] = __builtin_ldexpf(s.o[n][c][e] * inv, s.vref - 127);
+  }
+}
+// Between the four lanes of a row of queries: block k of lane g becomes block g of lane k
+__device__ inline void transpose(float* x) {
+  auto swap16 = [](float& a, float& b) {
+    const auto v = __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(unsigned, a), __builtin_bit_cast(unsigned, b), false, false);
+    const unsigned first = v[0], second = v[1];
+    a = __builtin_bit_cast(float, first);
+    b = __builtin_bit_cast(float, second);
+  };
+  auto swap32 = [](float& a, float& b) {
+    const auto v = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(unsigned, a), __builtin_bit_cast(unsigned, b), false, false);
+    const unsigned first = v[0], second = v[1];
+    a = __builtin_bit_cast(float, first);
+    b = __builtin_bit_cast(float, second);
+  };
+#pragma unroll
+  for (int c = 0; c < 4; ++c) {
+    swap32(x[c], x[8 + c]);
+    swap32(x[4 + c], x[12 + c]);
+    swap16(x[c], x[4 + c]);
+    swap16(x[8 + c], x[12 + c]);
+  }
+}
+// The 16 output channels of a lane's run i
+template <int D, int DIG, int NR>
+__device__ inline void run_of(const state<D, DIG, NR>& s, int n, int i, float* x) {
+#pragma unroll
+  for (int c = 0; c < 16; ++c) x[c] = s.o[n][4 * i + c % 4][c / 4];
+}
+
+// Results of a share of the keys, past the caches that other workgroups do not share
+struct shares {
+  float *data, *lse;
+  size_t first;  // the first share's first row
+  int rows_pad;
+  template <int D>
+  __device__ inline void init(const qg_kv4_attention_args& p, const job& j) {
+    first = ((size_t)j.seq * p.c.heads + j.head) * p.split * p.rows_pad;
+    rows_pad = p.rows_pad;
+    data = p.partial;
+    lse = p.partial + (size_t)p.batch * p.c.heads * p.split * p.rows_pad * D;
+  }
+  __device__ inline size_t at(int slice, int row) const { return first + (size_t)slice * rows_pad + row; }
+};
+__device__ inline void hand_in(float* to, f4 x) {  // 16 bytes at once (their registers may not be written to in the next cycle)
+  asm volatile("global_store_dwordx4 %0, %1, off sc1\n\ts_nop 1" ::"v"(to), "v"(x) : "memory");
+}
+__device__ inline void hand_in(float* to, float a) { __hip_atomic_store(to, a, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+
+// Keys split over workgroups: the last one to arrive adds the shares, in their order.  THREADS of the workgroup; scratch: 8 floats a
+// thread, or NULL (many rows: every thread has a row of its own).
+template <int D, int TYPE, int THREADS, int BATCH>
+__device__ inline void join(const qg_kv4_attention_args& p, const job& j, const shares& w, float* scratch, int* ticket) {
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // what this wave handed in has been acknowledged
+  __syncthreads();
+  int* const counter = p.counters + ((size_t)j.seq * p.c.heads + j.head) * p.row_blocks + j.rb;
+  if (threadIdx.x == 0) *ticket = __hip_atomic_fetch_add(counter, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  __syncthreads();
+  if (*ticket != j.slices - 1) return;
+  if (threadIdx.x == 0) __hip_atomic_store(counter, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);  // ready for the next call
+  // BATCH shares are requested together; where there are fewer results than threads, groups of threads take every groups-th batch
+  // and meet in LDS
+  const int items = (j.last_row - j.row0 + 1) * (D / 4);
+  const int groups = scratch != nullptr && items * 2 <= THREADS ? THREADS / items : 1;
+  for (int at = (int)threadIdx.x; at < items * groups; at += THREADS) {
+    const int mine = at / items, item = at - mine * items;
+    const int c = item % (D / 4) * 4, row = j.row0 + item / (D / 4);
+    float top = -__builtin_inff(), total = 0.0f;
+    f4 x = (f4){0.0f, 0.0f, 0.0f, 0.0f};
+    for (int t0 = mine * BATCH; t0 < j.slices; t0 += groups * BATCH) {
+      float lse[BATCH];
+      u64 u[BATCH], v[BATCH];
+#pragma unroll
+      for (int t = 0; t < BATCH; ++t) {
+        const size_t from = w.at(min(t0 + t, j.slices - 1), row);
+        lse[t] = __hip_atomic_load(w.lse + from, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        const u64* data = reinterpret_cast<const u64*>(w.data + from * D + c);
+        u[t] = __hip_atomic_load(data, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        v[t] = __hip_atomic_load(data + 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      }
+      float high = top;
+#pragma unroll
+      for (int t = 0; t < BATCH; ++t) high = fmaxf(high, lse[t]);
+      const float base = high == -__builtin_inff() ? 0.0f : high;
+      const float f = __builtin_amdgcn_exp2f(top - base);
+      top = high;
+      total *= f;
+      x *= f;
+#pragma unroll
+      for (int t = 0; t < BATCH; ++t) {
+        const float e = t0 + t < j.slices ? __builtin_amdgcn_exp2f(lse[t] - base) : 0.0f;
+        total += e;
+        x[0] += e * __builtin_bit_cast(float, (unsigned)u[t]);
+        x[1] += e * __builtin_bit_cast(float, (unsigned)(u[t] >> 32));
+        x[2] += e * __builtin_bit_cast(float, (unsigned)v[t]);
+        x[3] += e * __builtin_bit_cast(float, (unsigned)(v[t] >> 32));
+      }
+    }
+    if (groups > 1) {  // (every thread comes here once)
+      float* to = scratch + at * 8;
+      *reinterpret_cast<f4*>(to) = x;
+      to[4] = top;
+      to[5] = total;
+    } else {
+      x *= total == 0.0f ? 0.0f : 1.0f / total;
+      j.write<TYPE, 4>(p, row, c, reinterpret_cast<const float*>(&x));
+    }
+  }
+  if (groups == 1) return;
+  __syncthreads();
+  const int item = (int)threadIdx.x;
+  if (item >= items) return;
+  float top = -__builtin_inff(), total = 0.0f;
+  for (int k = 0; k < groups; ++k) top = fmaxf(top, scratch[(k * items + item) * 8 + 4]);
+  const float base = top == -__builtin_inff() ? 0.0f : top;
+  f4 x = (f4){0.0f, 0.0f, 0.0f, 0.0f};
+  for (int k = 0; k < groups; ++k) {
+    const float* from = scratch + (k * items + item) * 8;
+    const float e = __builtin_amdgcn_exp2f(from[4] - base);
+    total += e * from[5];
+    x += e * *reinterpret_cast<const f4*>(from);
+  }
+  x *= total == 0.0f ? 0.0f : 1.0f / total;
+  j.write<TYPE, 4>(p, j.row0 + item / (D / 4), item % (D / 4) * 4, reinterpret_cast<const float*>(&x));
+}
+
+}  // namespace

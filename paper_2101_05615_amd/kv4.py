@@ -6,14 +6,15 @@
     o = kv4.attention(q, cache, pages, kv_lens)                            # one query token per sequence
 
 Tensors of heads are [tokens, heads, head_dim] in float32, bfloat16 or float16 with any strides but a unit stride of channels:
-views of a fused projection's rows are taken as they are.  Argument marshalling only, like qgemm.py.
+views of a fused projection's rows are taken as they are.  Argument marshalling only, like qgemm.py: the calls that a program
+repeats first go through the extension module, and only a call that it declines is marshalled, and its error named, here.
 """
 import ctypes
 import math
 
 import torch
 
-from .qgemm import QGemmError, _check, _stream, lib
+from .qgemm import QGemmError, _binding, _check, _stream, lib
 
 F32, BF16, F16 = 0, 1, 2
 _TYPES = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}
@@ -93,6 +94,9 @@ def rope_table(max_pos, rot, base=10000.0, scaling="plain", factor=1.0, low=1.0,
 def rope(x, positions, table, interleaved=False, inverse=False, out=None):
     """x [tokens, heads, head_dim] with the first table.shape[1] channels of every head turned by the token's position (int32
     [tokens]); inverse: turned back, the gradient.  `out` may be x."""
+    done = _binding.rope(x, positions, table, interleaved, inverse, out)
+    if done is not None:
+        return done
     _check_heads(x)
     _check_table(table)
     T, H, D = x.shape
@@ -123,7 +127,7 @@ class Cache:
         self.data, self.n_pages = data, data.numel() // per
         self.kv_heads, self.head_dim, self.page_tokens = kv_heads, head_dim, page_tokens
         self._desc = CacheDesc(data.data_ptr(), self.n_pages, kv_heads, head_dim, page_tokens)
-        self._ref = ctypes.byref(self._desc)
+        self._ref, self._fast = ctypes.byref(self._desc), ctypes.addressof(self._desc)
 
 
 def new_cache(n_pages, kv_heads, head_dim, page_tokens, device="cuda"):
@@ -137,6 +141,9 @@ def append(cache, k, v, slots, positions=None, table=None, interleaved=False, q=
     """Stores k and v [tokens, kv_heads, head_dim] in the slots (int64 [tokens]; -1: not stored) in 4 bits, k rotated by its
     position if `positions` (int32 [tokens]) and `table` are given.  q [tokens, heads, head_dim] is rotated in the same pass into
     q_out (new; may be q), which is returned (None without q)."""
+    done = _binding.kv4_append(cache, k, v, slots, positions, table, interleaved, q, q_out)
+    if done is not None:
+        return None if done is True else done
     _check_heads(k, None, cache.kv_heads, cache.head_dim)
     _check_heads(v, k, cache.kv_heads, cache.head_dim)
     T = k.shape[0]
@@ -163,6 +170,9 @@ def append(cache, k, v, slots, positions=None, table=None, interleaved=False, q=
 
 def read(cache, slots, dtype=torch.float32, k=None, v=None):
     """What the slots (int64 [tokens]) hold: (keys, values) [tokens, kv_heads, head_dim] of `dtype`; outside the cache: zeros."""
+    done = _binding.kv4_read(cache, slots, _TYPES[dtype], k, v)
+    if done is not None:
+        return done
     T = slots.shape[0]
     _check_ints(slots, torch.int64, T)
     shape = (T, cache.kv_heads, cache.head_dim)
@@ -195,6 +205,9 @@ def attention(q, cache, pages, kv_lens, q_starts=None, max_q_len=1, max_kv_len=N
     pages of a sequence in order; kv_lens int32 [batch] its tokens.  q_starts int32 [batch + 1]: the rows of q that belong to a
     sequence, its last tokens (causal: query i of n sees the keys up to kv_len - n + i); None: one row each.  max_q_len,
     max_kv_len: the most of any sequence (default for the latter: what the page table holds).  scale: 1 / sqrt(head_dim)."""
+    done = _binding.kv4_attention(cache, q, pages, kv_lens, q_starts, max_q_len, max_kv_len, scale, causal, workspace, out)
+    if done is not None:
+        return done
     _check_heads(q, None, None, cache.head_dim)
     T, H, D = q.shape
     B, W = pages.shape
@@ -215,5 +228,6 @@ def attention(q, cache, pages, kv_lens, q_starts=None, max_q_len=1, max_kv_len=N
     p.scale = 1.0 / math.sqrt(D) if scale is None else scale
     p.dtype, p.tokens, p.q_heads, p.batch, p.pages_stride = _TYPES[q.dtype], T, H, B, pages.stride(0) if B > 1 else W
     p.max_q_len, p.max_kv_len, p.causal = max_q_len, W * cache.page_tokens if max_kv_len is None else max_kv_len, int(bool(causal))
+    assert p.max_kv_len <= W * cache.page_tokens
     _check(lib.qg_kv4_attention(cache._ref, ctypes.byref(p), _stream()), "qg_kv4_attention")
     return out
