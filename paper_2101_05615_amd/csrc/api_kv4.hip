@@ -44,11 +44,11 @@ int check_rotation(const float* table, int max_pos, int rot, int interleaved, in
 
 // ---- keys of a sequence over workgroups
 // With few sequences a workgroup per (sequence, KV head, rows) leaves most of the 256 CUs idle, and with long ones that differ in
-// length the longest ends alone.  Keys are dealt in chunks of equal length, at least LEAST tokens, what a workgroup's start and end
-// cost.  Few rows: chunks that give every CU a workgroup.  More would cost more than it evens out: every share is written, and read by
+// length the longest ends alone.  Keys are dealt in chunks of equal length, at least what a workgroup's start and end cost, and not
+// at all up to twice that (777 keys of 8 KV heads: 9.0 us in four shares, 9.1 whole).  Few rows: chunks that give every CU a workgroup.  More would cost more than it evens out: every share is written, and read by
 // the last one to arrive (131072 keys of 8 KV heads, 8 rows: 34 us in 256 shares, 40 in 512, 49 in 1024).  Many rows: workgroups run for
-// long, so eight times as many (512 queries of four sequences up to 8192 keys: 240 us whole, 203 in 1024 workgroups, 167 in 2048, 164 in
-// 3072).
+// long, so eight times as many (512 queries of four sequences up to 8192 keys: 240 us whole, 203 in 1024 workgroups, 165 in 2048, 161 in
+// 3072, 176 in 4096).
 constexpr int CUS = 256;
 constexpr size_t COUNTERS = 16384;  // a fixed part of every workspace, so that calls of other extents find it zero
 
@@ -64,7 +64,7 @@ share share_of(const qg_kv4_cache* c, int q_heads, int batch, int max_q_len, int
   const int least = rows <= QG_KV4_FEW ? 256 : 512, workgroups = rows <= QG_KV4_FEW ? CUS : 8 * CUS;
   long long chunk = ((long long)max_kv_len * units / workgroups + 63) / 64 * 64;
   if (chunk < least) chunk = least;
-  if (chunk >= max_kv_len) return s;
+  if (chunk >= max_kv_len || max_kv_len <= 2 * least) return s;
   s.chunk = (int)chunk;
   s.split = (int)((max_kv_len + chunk - 1) / chunk);
   return s;

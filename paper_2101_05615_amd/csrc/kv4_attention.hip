@@ -8,7 +8,7 @@
 
 namespace {
 
-constexpr int WAVES = 4;  // of a workgroup
+constexpr int WAVES = 4;  // of a workgroup; eight (64 KiB of LDS, one workgroup a CU) measured the same or a few per cent more
 
 template <int D>
 struct tile_bits {
@@ -206,7 +206,11 @@ __global__ __launch_bounds__(64 * WAVES, waves_per_simd(D, NR)) void qg_kv4_atte
       if (c == 0) hand_in(w.lse + w.at(j.slice, row), base + __builtin_amdgcn_logf(total));
     }
   }
-  if (j.slices > 1) join<D, TYPE, 64 * WAVES, D == 128 && DIG == 1 ? 16 : 8>(p, j, w, part, &ticket);
+  if (j.slices == 1) return;
+  if (D == 256 && (j.last_row - j.row0 + 1) * (D / 4) > 2 * 64 * WAVES)
+    join<D, TYPE, 64 * WAVES, 4, 4>(p, j, w, nullptr, &ticket);
+  else
+    join<D, TYPE, 64 * WAVES, 1, D == 128 && DIG == 1 ? 16 : 8>(p, j, w, part, &ticket);
 }
 
 template <int D, int TYPE, int NR>

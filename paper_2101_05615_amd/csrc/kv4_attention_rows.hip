@@ -237,7 +237,7 @@ __global__ __launch_bounds__(64 * waves_of(D), 2) void qg_kv4_attention_rows_ker
     }
     if (j.slices > 1 && g == 0 && row < j.rows) hand_in(w.lse + w.at(j.slice, row), lse[n]);
   }
-  if (j.slices > 1) join<D, TYPE, 64 * WAVES, 4>(p, j, w, nullptr, &ticket);
+  if (j.slices > 1) join<D, TYPE, 64 * WAVES, 4, 4>(p, j, w, nullptr, &ticket);
 }
 
 template <int D, int TYPE>

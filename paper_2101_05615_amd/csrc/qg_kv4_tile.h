@@ -500,9 +500,11 @@ __device__ inline void hand_in(float* to, f4 x) {  // 16 bytes at once (their re
 }
 __device__ inline void hand_in(float* to, float a) { __hip_atomic_store(to, a, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
 
-// Keys split over workgroups: the last one to arrive adds the shares, in their order.  THREADS of the workgroup; scratch: 8 floats a
-// thread, or NULL (many rows: every thread has a row of its own).
-template <int D, int TYPE, int THREADS, int BATCH>
+// Keys split over workgroups: the last one to arrive adds the shares, in their order.  THREADS of the workgroup.  An item is four
+// channels of a row; a thread requests BATCH shares of ITEMS items together, since a request past the caches takes more than a
+// microsecond.  scratch: 8 floats a thread, or NULL; with it, where there are fewer items than threads, groups of threads take every
+// groups-th batch of shares and meet there.
+template <int D, int TYPE, int THREADS, int ITEMS, int BATCH>
 __device__ inline void join(const qg_kv4_attention_args& p, const job& j, const shares& w, float* scratch, int* ticket) {
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // what this wave handed in has been acknowledged
   __syncthreads();
@@ -511,55 +513,69 @@ __device__ inline void join(const qg_kv4_attention_args& p, const job& j, const 
   __syncthreads();
   if (*ticket != j.slices - 1) return;
   if (threadIdx.x == 0) __hip_atomic_store(counter, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);  // ready for the next call
-  // BATCH shares are requested together; where there are fewer results than threads, groups of threads take every groups-th batch
-  // and meet in LDS
   const int items = (j.last_row - j.row0 + 1) * (D / 4);
   const int groups = scratch != nullptr && items * 2 <= THREADS ? THREADS / items : 1;
-  for (int at = (int)threadIdx.x; at < items * groups; at += THREADS) {
-    const int mine = at / items, item = at - mine * items;
-    const int c = item % (D / 4) * 4, row = j.row0 + item / (D / 4);
-    float top = -__builtin_inff(), total = 0.0f;
-    f4 x = (f4){0.0f, 0.0f, 0.0f, 0.0f};
+  for (int at = (int)threadIdx.x; at < items * groups; at += THREADS * ITEMS) {
+    const int mine = groups > 1 ? at / items : 0;
+    int item[ITEMS];
+    float top[ITEMS], total[ITEMS];
+    f4 x[ITEMS];
+#pragma unroll
+    for (int k = 0; k < ITEMS; ++k) {
+      item[k] = min(at - mine * items + k * THREADS, items - 1);  // (past the end: the last one again, not written)
+      top[k] = -__builtin_inff();
+      total[k] = 0.0f;
+      x[k] = (f4){0.0f, 0.0f, 0.0f, 0.0f};
+    }
     for (int t0 = mine * BATCH; t0 < j.slices; t0 += groups * BATCH) {
-      float lse[BATCH];
-      u64 u[BATCH], v[BATCH];
+      float lse[ITEMS][BATCH];
+      u64 u[ITEMS][BATCH], v[ITEMS][BATCH];
 #pragma unroll
-      for (int t = 0; t < BATCH; ++t) {
-        const size_t from = w.at(min(t0 + t, j.slices - 1), row);
-        lse[t] = __hip_atomic_load(w.lse + from, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        const u64* data = reinterpret_cast<const u64*>(w.data + from * D + c);
-        u[t] = __hip_atomic_load(data, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        v[t] = __hip_atomic_load(data + 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-      }
-      float high = top;
+      for (int k = 0; k < ITEMS; ++k)
 #pragma unroll
-      for (int t = 0; t < BATCH; ++t) high = fmaxf(high, lse[t]);
-      const float base = high == -__builtin_inff() ? 0.0f : high;
-      const float f = __builtin_amdgcn_exp2f(top - base);
-      top = high;
-      total *= f;
-      x *= f;
+        for (int t = 0; t < BATCH; ++t) {
+          const size_t from = w.at(min(t0 + t, j.slices - 1), j.row0 + item[k] / (D / 4));
+          lse[k][t] = __hip_atomic_load(w.lse + from, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+          const u64* data = reinterpret_cast<const u64*>(w.data + from * D + item[k] % (D / 4) * 4);
+          u[k][t] = __hip_atomic_load(data, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+          v[k][t] = __hip_atomic_load(data + 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        }
 #pragma unroll
-      for (int t = 0; t < BATCH; ++t) {
-        const float e = t0 + t < j.slices ? __builtin_amdgcn_exp2f(lse[t] - base) : 0.0f;
-        total += e;
-        x[0] += e * __builtin_bit_cast(float, (unsigned)u[t]);
-        x[1] += e * __builtin_bit_cast(float, (unsigned)(u[t] >> 32));
-        x[2] += e * __builtin_bit_cast(float, (unsigned)v[t]);
-        x[3] += e * __builtin_bit_cast(float, (unsigned)(v[t] >> 32));
+      for (int k = 0; k < ITEMS; ++k) {
+        float high = top[k];
+#pragma unroll
+        for (int t = 0; t < BATCH; ++t) high = fmaxf(high, lse[k][t]);
+        const float base = high == -__builtin_inff() ? 0.0f : high;
+        const float f = __builtin_amdgcn_exp2f(top[k] - base);
+        top[k] = high;
+        total[k] *= f;
+        x[k] *= f;
+#pragma unroll
+        for (int t = 0; t < BATCH; ++t) {
+          const float e = t0 + t < j.slices ? __builtin_amdgcn_exp2f(lse[k][t] - base) : 0.0f;
+          total[k] += e;
+          x[k][0] += e * __builtin_bit_cast(float, (unsigned)u[k][t]);
+          x[k][1] += e * __builtin_bit_cast(float, (unsigned)(u[k][t] >> 32));
+          x[k][2] += e * __builtin_bit_cast(float, (unsigned)v[k][t]);
+          x[k][3] += e * __builtin_bit_cast(float, (unsigned)(v[k][t] >> 32));
+        }
       }
     }
-    if (groups > 1) {  // (every thread comes here once)
+    if (ITEMS == 1 && groups > 1) {  // (every thread comes here once)
       float* to = scratch + at * 8;
-      *reinterpret_cast<f4*>(to) = x;
-      to[4] = top;
-      to[5] = total;
+      *reinterpret_cast<f4*>(to) = x[0];
+      to[4] = top[0];
+      to[5] = total[0];
     } else {
-      x *= total == 0.0f ? 0.0f : 1.0f / total;
-      j.write<TYPE, 4>(p, row, c, reinterpret_cast<const float*>(&x));
+#pragma unroll
+      for (int k = 0; k < ITEMS; ++k) {
+        if (at + k * THREADS >= items) break;
+        x[k] *= total[k] == 0.0f ? 0.0f : 1.0f / total[k];
+        j.write<TYPE, 4>(p, j.row0 + item[k] / (D / 4), item[k] % (D / 4) * 4, reinterpret_cast<const float*>(&x[k]));
+      }
     }
   }
-  if (groups == 1) return;
+  if (ITEMS > 1 || groups == 1) return;
   __syncthreads();
   const int item = (int)threadIdx.x;
   if (item >= items) return;
