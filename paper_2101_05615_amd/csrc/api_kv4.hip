@@ -17,6 +17,9 @@ int check_heads(const qg_heads& h, int dtype) {
   return aligned(h.data, ELEM[dtype]) ? QG_OK : QG_EALIGN;
 }
 
+// A launch's threads along one axis; the kernels over tokens number them so
+bool too_many(long long tokens, long long heads, int head_dim) { return tokens * heads * (head_dim / 16) > 0x7fff0000ll; }
+
 int lg_of_page(int page_tokens) {
   for (int l = 4; l <= 8; ++l)
     if (page_tokens == 1 << l) return l;
@@ -171,6 +174,7 @@ int qg_kv4_append(const qg_kv4_cache* c, const qg_kv4_append_params* p, void* st
     if (p->rot % 16 != 0) return QG_EUNSUPPORTED;
     if (!aligned(p->positions, 4)) return QG_EALIGN;
   }
+  if (too_many(p->tokens, 2 * c->kv_heads + p->q_heads, c->head_dim)) return QG_EUNSUPPORTED;
   if (p->tokens == 0) return QG_OK;
   if (!p->slots) return QG_ENULL;
   if (!aligned(p->slots, 8)) return QG_EALIGN;
@@ -210,6 +214,7 @@ int qg_kv4_read(const qg_kv4_cache* c, const int64_t* slots, int tokens, int dty
   int rc = check_cache(c, &a.c);
   if (rc != QG_OK) return rc;
   if (!known(dtype) || tokens < 0 || tokens > QG_KV4_MAX_TOKENS) return QG_EINVAL;
+  if (too_many(tokens, 2 * c->kv_heads, c->head_dim)) return QG_EUNSUPPORTED;
   if (tokens == 0) return QG_OK;
   if (!slots) return QG_ENULL;
   if (!aligned(slots, 8)) return QG_EALIGN;

@@ -37,7 +37,7 @@ struct rows_of_wave : state<D, DIG, NR> {
   float q_sum[NR];  // DIG 1: less the sum of the queries, times 2^-20
 };
 
-template <int D, int DIG, int NR, bool MASKED>
+template <int D, int DIG, int NR, int PARTS, bool MASKED>
 __device__ inline void step(rows_of_wave<D, DIG, NR>& s, const tile_bits<D>& b, int t0, int end, int r, int g) {
   unsigned word = b.w;
   if (MASKED && t0 + 8 * g + (r & 7) >= end) word = 0u;
@@ -79,10 +79,10 @@ __device__ inline void step(rows_of_wave<D, DIG, NR>& s, const tile_bits<D>& b, 
       for (int j = 0; j < 8; ++j) z[n][j >> 2][j & 3] = __builtin_fmaf(zp[j], s.q_sum[n], z[n][j >> 2][j & 3]);
   }
 
-  frag p[NR][DIG];
+  frag p[NR][PARTS];
   float y[NR][8];
   exponents<D, DIG, NR, MASKED>(s, z, word, t0, end, r, g, y);
-  weights<D, DIG, NR, MASKED>(s, y, word, p);
+  weights<D, DIG, NR, PARTS, MASKED>(s, y, word, p);
 
   const zero_points zp(word);
 #pragma unroll
@@ -94,7 +94,7 @@ __device__ inline void step(rows_of_wave<D, DIG, NR>& s, const tile_bits<D>& b, 
 #pragma unroll
       for (int n = 0; n < NR; ++n)
 #pragma unroll
-        for (int d = 0; d < DIG; ++d) s.o[n][4 * i + c] = product(v[c], p[n][d], s.o[n][4 * i + c]);
+        for (int d = 0; d < PARTS; ++d) s.o[n][4 * i + c] = product(v[c], p[n][d], s.o[n][4 * i + c]);
   }
 }
 
@@ -102,7 +102,7 @@ constexpr int waves_per_simd(int D, int NR) { return NR == 2 || D == 256 ? 2 : 3
 
 template <int D, int DIG, int TYPE, int NR, bool SMALL>
 __global__ __launch_bounds__(64 * WAVES, waves_per_simd(D, NR)) void qg_kv4_attention_kernel(qg_kv4_attention_args p) {
-  constexpr int ROWS = 16 * NR, PITCH = D + 4, STRIDE = TILE * WAVES;
+  constexpr int ROWS = 16 * NR, PITCH = D + 4, STRIDE = TILE * WAVES, PARTS = TYPE == QG_BF16 ? 1 : 2;
   __shared__ float part[WAVES * ROWS * PITCH];
   __shared__ float part_lse[WAVES * ROWS];
   __shared__ int ticket;
@@ -151,17 +151,17 @@ __global__ __launch_bounds__(64 * WAVES, waves_per_simd(D, NR)) void qg_kv4_atte
     while (t0 + STRIDE + TILE <= whole) {
       load_tile(in, min(t0 + STRIDE, last), next, b);
       next = in.pages(min(t0 + 2 * STRIDE, last));
-      step<D, DIG, NR, false>(s, a, t0, j.hi, r, g);
+      step<D, DIG, NR, PARTS, false>(s, a, t0, j.hi, r, g);
       t0 += STRIDE;
       load_tile(in, min(t0 + STRIDE, last), next, a);
       next = in.pages(min(t0 + 2 * STRIDE, last));
-      step<D, DIG, NR, false>(s, b, t0, j.hi, r, g);
+      step<D, DIG, NR, PARTS, false>(s, b, t0, j.hi, r, g);
       t0 += STRIDE;
     }
     for (; t0 < j.hi; t0 += STRIDE) {
       load_tile(in, min(t0 + STRIDE, last), next, b);
       next = in.pages(min(t0 + 2 * STRIDE, last));
-      step<D, DIG, NR, true>(s, a, t0, j.hi, r, g);
+      step<D, DIG, NR, PARTS, true>(s, a, t0, j.hi, r, g);
       a = b;
     }
   }

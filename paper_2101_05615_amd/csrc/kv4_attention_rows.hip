@@ -133,10 +133,10 @@ __device__ inline void stage(rows_of_wave<D, DIG, NR>& s, const stage_lds<D>& in
   between();
   exponents<D, DIG, NR, MASKED>(s, z[0], w[0], t0, end, r, g, y);
   scores(s, in, 1, lane, z[1]);
-  weights<D, DIG, NR, MASKED>(s, y, w[0], p);
+  weights<D, DIG, NR, DIG, MASKED>(s, y, w[0], p);
   outputs(s, in, 0, lane, p);
   exponents<D, DIG, NR, MASKED>(s, z[1], w[1], t0 + TILE, end, r, g, y);
-  weights<D, DIG, NR, MASKED>(s, y, w[1], p);
+  weights<D, DIG, NR, DIG, MASKED>(s, y, w[1], p);
   outputs(s, in, 1, lane, p);
 }
 
