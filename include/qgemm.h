@@ -577,7 +577,7 @@ int qg_kv4_read(const qg_kv4_cache* c, const int64_t* slots, int tokens, int dty
  * for query i of n of a sequence with m keys over the keys j < m, and with causal
  * = 1 over j <= m - n + i only (the queries are the last n tokens, their own keys
  * stored).  Query head h reads KV head h / (q_heads / kv_heads).  A query with no
- * key to see gives 0.  Sums and softmax statistics are fp32; the codes enter the
+ * key to see gives 0.  Scores may be up to 2^28 in size.  Sums and softmax statistics are fp32; the codes enter the
  * matrix cores exactly, queries as fp16 numbers scaled by row (two per channel for
  * QG_F32), probabilities as fp16 (two for QG_F32).
  *   pages     dev int32 [batch][pages_stride]; entry i names the page of tokens

@@ -42,7 +42,6 @@ typedef unsigned u4 __attribute__((ext_vector_type(4)));
 typedef unsigned long long u64;
 
 constexpr int TILE = 32;         // tokens of a wave's step
-constexpr float START = -1e30f;  // the running maximum before the first key
 constexpr float BOOST = 4.0f;    // probabilities are held times 2^BOOST ...
 constexpr float SLACK = 12.0f;   // ... and the reference moves when one would pass 2^SLACK
 
@@ -143,7 +142,7 @@ struct page_reader {
   __device__ inline void init(const qg_kv4_attention_args& p, int seq, int kv_head) {
     data = p.c.data;
     table = p.pages + (int64_t)seq * p.pages_stride;
-    entries = p.pages_stride;
+    entries = max((p.max_kv_len + (1 << p.c.lgp) - 1) >> p.c.lgp, 1);  // (that a call may read)
     n_pages = p.c.n_pages;
     lgp = p.c.lgp;
     head_bytes = (size_t)(D + 8) << lgp;
@@ -233,7 +232,7 @@ struct state {
     vref = 1;
 #pragma unroll
     for (int n = 0; n < NR; ++n) {
-      m[n] = START;
+      m[n] = -__builtin_inff();  // (before the first key every exponent is +infinity, and the reference moves)
       l[n] = 0.0f;
 #pragma unroll
       for (int c = 0; c < D / 16; ++c) o[n][c] = (f4){0.0f, 0.0f, 0.0f, 0.0f};
@@ -299,7 +298,7 @@ __device__ inline void exponents(state<D, DIG, NR>& s, f4 (*z)[2], unsigned word
         high = fmaxf(high, MASKED && j > limit[n] ? -__builtin_inff() : x);
       }
       const float top = fmaxf(s.m[n], across_max(high));
-      const float f = __builtin_amdgcn_exp2f(s.m[n] - top);
+      const float f = top == s.m[n] ? 1.0f : __builtin_amdgcn_exp2f(s.m[n] - top);  // (both -infinity: no key yet)
       s.m[n] = top;
       s.l[n] *= f;
 #pragma unroll

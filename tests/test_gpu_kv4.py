@@ -403,6 +403,22 @@ def test_scores_of_all_sizes(env, dtype):
     b.check(b.run())
 
 
+@pytest.mark.parametrize("q_lens", [[1], [3], [20]])
+def test_scores_far_below_zero(env, q_lens):
+    """All scores between -4e6 and -4e8: the least negative one takes all."""
+    kv4, torch, dev = env
+    b = Batch(env, [100], 4, 2, 64, 16, "float32", seed=2, q_lens=q_lens)
+    slots = torch.from_numpy(b.slots[0]).to(dev)
+    k = (torch.arange(100, device=dev).flip(0) + 1.0)[:, None, None].repeat(1, 2, 64)
+    v = torch.randn(100, 2, 64, device=dev)
+    kv4.append(b.cache, k, v, slots)
+    b.q.fill_(-(2.0 ** 16))
+    got, held = b.run(scale=1.0), kv4.read(b.cache, slots)[1]
+    for i in range(q_lens[0]):
+        want = held[99 - (q_lens[0] - 1 - i)].repeat_interleave(2, 0)
+        assert ((got[i] - want).abs() <= 2.0 ** -20 * want.abs()).all()
+
+
 def test_value_scales_of_all_sizes(env):
     """Values 2^60 apart between tokens: the small ones count where the large ones have no weight."""
     kv4, torch, dev = env
