@@ -82,9 +82,6 @@ __device__ inline void unpack(const parts<D>& b, int wave, int lane, stage_lds<D
   }
 }
 
-// Operands are read four at a time: requested all at once, they would push queries and outputs out of the registers
-__device__ inline void few_at_once() { asm volatile("" ::: "memory"); }
-
 // Step `which` of a stage: products of queries and keys; of weights and values
 template <int D, int DIG, int NR>
 __device__ inline void scores(const rows_of_wave<D, DIG, NR>& s, const stage_lds<D>& in, int which, int lane, f4 (*z)[2]) {
@@ -94,7 +91,6 @@ __device__ inline void scores(const rows_of_wave<D, DIG, NR>& s, const stage_lds
     for (int n = 0; n < NR; ++n) z[n][a] = (f4){0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
     for (int i = 0; i < D / 32; ++i) {
-      if (i % 4 == 0) few_at_once();
       const frag k = in.keys[2 * which + a][i][lane];
 #pragma unroll
       for (int n = 0; n < NR; ++n)
@@ -107,7 +103,6 @@ template <int D, int DIG, int NR>
 __device__ inline void outputs(rows_of_wave<D, DIG, NR>& s, const stage_lds<D>& in, int which, int lane, const frag (*p)[DIG]) {
 #pragma unroll
   for (int c = 0; c < D / 16; ++c) {
-    if (c % 4 == 0) few_at_once();
     const frag v = in.values[which][c][lane];
 #pragma unroll
     for (int n = 0; n < NR; ++n)
