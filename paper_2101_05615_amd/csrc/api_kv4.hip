@@ -75,7 +75,7 @@ share share_of(const qg_kv4_cache* c, int q_heads, int batch, int max_q_len, int
 
 size_t share_bytes(const share& s, int kv_heads, int batch, int head_dim) {
   if (s.split == 1) return 0;
-  return COUNTERS * 4 + (size_t)batch * kv_heads * s.split * s.rows_pad * (head_dim + 1) * 4;
+  return COUNTERS * 4 + (size_t)batch * kv_heads * s.split * s.rows_pad * (head_dim + 2) * 4;
 }
 
 bool extents_ok(const qg_kv4_cache* c, int q_heads, int batch, int max_q_len, int max_kv_len) {

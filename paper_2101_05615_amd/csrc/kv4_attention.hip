@@ -104,7 +104,7 @@ template <int D, int DIG, int TYPE, int NR, bool SMALL>
 __global__ __launch_bounds__(64 * WAVES, waves_per_simd(D, NR)) void qg_kv4_attention_kernel(qg_kv4_attention_args p) {
   constexpr int ROWS = 16 * NR, PITCH = D + 4, STRIDE = TILE * WAVES, PARTS = TYPE == QG_BF16 ? 1 : 2;
   __shared__ float part[WAVES * ROWS * PITCH];
-  __shared__ float part_lse[WAVES * ROWS];
+  __shared__ float part_m[WAVES * ROWS], part_sum[WAVES * ROWS];
   __shared__ int ticket;
   const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   const int r = lane & 15, g = lane >> 4;
@@ -167,8 +167,8 @@ __global__ __launch_bounds__(64 * WAVES, waves_per_simd(D, NR)) void qg_kv4_atte
   }
 
   // ---- the waves' results meet in LDS, weighted by their sums
-  float lse[NR];
-  finish(s, lse);
+  float sum[NR];
+  finish(s, sum);
 #pragma unroll
   for (int n = 0; n < NR; ++n) {
     float* to = part + (wave * ROWS + n * 16 + r) * PITCH;
@@ -179,7 +179,10 @@ __global__ __launch_bounds__(64 * WAVES, waves_per_simd(D, NR)) void qg_kv4_atte
 #pragma unroll
       for (int c = 0; c < 16; c += 4) *reinterpret_cast<f4*>(to + lay<D>::out_channel(i, g) + c) = (f4){x[c], x[c + 1], x[c + 2], x[c + 3]};
     }
-    if (g == 0) part_lse[wave * ROWS + n * 16 + r] = lse[n];
+    if (g == 0) {
+      part_m[wave * ROWS + n * 16 + r] = s.m[n];
+      part_sum[wave * ROWS + n * 16 + r] = sum[n];
+    }
   }
   __syncthreads();
   shares w;
@@ -188,13 +191,12 @@ __global__ __launch_bounds__(64 * WAVES, waves_per_simd(D, NR)) void qg_kv4_atte
     const int local = at / (D / 4), c = at % (D / 4) * 4, row = j.row0 + local;
     float top = -__builtin_inff();
 #pragma unroll
-    for (int k = 0; k < WAVES; ++k) top = fmaxf(top, part_lse[k * ROWS + local]);
-    const float base = top == -__builtin_inff() ? 0.0f : top;
+    for (int k = 0; k < WAVES; ++k) top = fmaxf(top, part_m[k * ROWS + local]);
     float total = 0.0f;
     f4 x = (f4){0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
     for (int k = 0; k < WAVES; ++k) {
-      const float e = __builtin_amdgcn_exp2f(part_lse[k * ROWS + local] - base);
+      const float e = weight(part_m[k * ROWS + local], part_sum[k * ROWS + local], top);
       total += e;
       x += e * *reinterpret_cast<const f4*>(part + (k * ROWS + local) * PITCH + c);
     }
@@ -203,7 +205,7 @@ __global__ __launch_bounds__(64 * WAVES, waves_per_simd(D, NR)) void qg_kv4_atte
       j.write<TYPE, 4>(p, row, c, reinterpret_cast<const float*>(&x));
     } else {
       hand_in(w.data + w.at(j.slice, row) * D + c, x);
-      if (c == 0) hand_in(w.lse + w.at(j.slice, row), base + __builtin_amdgcn_logf(total));
+      if (c == 0) hand_in(w.sums + 2 * w.at(j.slice, row), top, total);
     }
   }
   if (j.slices == 1) return;

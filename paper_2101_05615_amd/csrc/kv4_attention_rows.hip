@@ -209,8 +209,8 @@ __global__ __launch_bounds__(64 * waves_of(D), 2) void qg_kv4_attention_rows_ker
     }
   }
 
-  float lse[NR];
-  finish(s, lse);
+  float sum[NR];
+  finish(s, sum);
   shares w;
   w.init<D>(p, j);
 #pragma unroll
@@ -230,7 +230,7 @@ __global__ __launch_bounds__(64 * waves_of(D), 2) void qg_kv4_attention_rows_ker
           if (row < j.rows) hand_in(to + 16 * k, (f4){x[4 * k], x[4 * k + 1], x[4 * k + 2], x[4 * k + 3]});
       }
     }
-    if (j.slices > 1 && g == 0 && row < j.rows) hand_in(w.lse + w.at(j.slice, row), lse[n]);
+    if (j.slices > 1 && g == 0 && row < j.rows) hand_in(w.sums + 2 * w.at(j.slice, row), s.m[n], sum[n]);
   }
   if (j.slices > 1) join<D, TYPE, 64 * WAVES, 4, 4>(p, j, w, nullptr, &ticket);
 }

@@ -181,7 +181,7 @@ struct qg_kv4_attention_args {
   int row_blocks;            // workgroups over a KV head's query rows
   int rows_pad;              // rows of a KV head in the workspace
   int* counters;             // one per (sequence, KV head, row block), zero before and after
-  float* partial;            // [sequence][KV head][split][rows_pad][D], then the row's log2 sum
+  float* partial;            // [sequence][KV head][split][rows_pad][D], then reference and sum of each row
   int64_t q_token, q_head, o_token, o_head;
 };
 

@@ -224,7 +224,7 @@ __device__ inline unsigned key_zero(unsigned theta, int a, int r) {
 template <int D, int DIG, int NR>
 struct state {
   f4 o[NR][D / 16];
-  float m[NR], l[NR];              // reference of the exponents (log2), sum (this lane's tokens)
+  float m[NR], l[NR];              // reference of the exponents (log2, a whole number), sum (this lane's tokens)
   float factor[NR], factor_lo[NR]; // log2 score of a product and a key's scale, in two parts (the second: DIG 2)
   int limit[NR];                   // last token that the row sees
   int vref;                        // biased exponent of the value scales' reference, 1 .. 253
@@ -249,10 +249,12 @@ __device__ inline float across_sum(float x) {
   return x + __shfl_xor(x, 32);
 }
 
+// z factor + base, where base is a whole number near -z factor: the sum is small and loses nothing of it.  DIG 2: the factor's own
+// rounding (2^-25 of every score) is more than the rest of an fp32 result's error.
 template <int DIG>
 __device__ inline float exponent(float z, float factor, float factor_lo, float base) {
-  // DIG 2: the factor's own rounding (2^-24 of every score) is more than the rest of an fp32 result's error
-  return DIG == 2 ? __builtin_fmaf(z, factor, __builtin_fmaf(z, factor_lo, base)) : __builtin_fmaf(z, factor, base);
+  const float y = __builtin_fmaf(z, factor, base);
+  return DIG == 2 ? __builtin_fmaf(z, factor_lo, y) : y;
 }
 
 // Products of a tile's 8 tokens (z[n][a][i]: token 8g + 4a + i) into exponents against the running references, which move rarely.
@@ -297,7 +299,7 @@ __device__ inline void exponents(state<D, DIG, NR>& s, f4 (*z)[2], unsigned word
         const float x = z[n][j >> 2][j & 3] * s.factor[n];
         high = fmaxf(high, MASKED && j > limit[n] ? -__builtin_inff() : x);
       }
-      const float top = fmaxf(s.m[n], across_max(high));
+      const float top = fmaxf(s.m[n], rintf(across_max(high)));  // (whole: references differ by powers of two)
       const float f = top == s.m[n] ? 1.0f : __builtin_amdgcn_exp2f(s.m[n] - top);  // (both -infinity: no key yet)
       s.m[n] = top;
       s.l[n] *= f;
@@ -326,6 +328,10 @@ __device__ inline void weights(state<D, DIG, NR>& s, const float (*y)[8], unsign
       s.l[n] += e;
       float x = e * vs[j];
       if (MASKED) x = y[n][j] == -__builtin_inff() ? 0.0f : x;  // (a masked value may be NaN)
+      // The product as 32 bits: left to itself the compiler rounds it to fp16 twice, once from the exact product and once from
+      // this one, and where the two differ the second part makes up for the wrong first part (one token in some thousands; an
+      // fp32 result then loses half its digits).
+      if (PARTS == 2) asm("" : "+v"(x));
       const _Float16 hi = (_Float16)x;
       p[n][0].v[j] = hi;
       if (PARTS == 2) p[n][PARTS - 1].v[j] = (_Float16)(x - (float)hi);
@@ -439,13 +445,14 @@ struct job {
   }
 };
 
-// A wave's rows divided by their sums; returns the sum's log2 (-infinity: no key)
+// A wave's rows divided by their sums, and those: what a part of the keys weighs is sum 2^m, kept as the two numbers (a logarithm of
+// a large sum would lose what an fp32 result shows).  No key: sum 0, m -infinity.
 template <int D, int DIG, int NR>
-__device__ inline void finish(state<D, DIG, NR>& s, float* lse) {
+__device__ inline void finish(state<D, DIG, NR>& s, float* sum) {
 #pragma unroll
   for (int n = 0; n < NR; ++n) {
     const float l = across_sum(s.l[n]);
-    lse[n] = s.m[n] + __builtin_amdgcn_logf(l);
+    sum[n] = l;
     const float inv = l == 0.0f ? 0.0f : 1.0f / l;
 #pragma unroll
     for (int c = 0; c < D / 16; ++c)
@@ -453,6 +460,9 @@ __device__ inline void finish(state<D, DIG, NR>& s, float* lse) {
       for (int e = 0; e < 4; ++e) s.o[n][c][e] = __builtin_ldexpf(s.o[n][c][e] * inv, s.vref - 127);
   }
 }
+// Weights relative to the largest reference `top` among the parts
+__device__ inline float weight(float m, float sum, float top) { return sum * __builtin_amdgcn_exp2f(m - (top == -__builtin_inff() ? 0.0f : top)); }
+
 // Between the four lanes of a row of queries: block k of lane g becomes block g of lane k
 __device__ inline void transpose(float* x) {
   auto swap16 = [](float& a, float& b) {
@@ -484,7 +494,7 @@ __device__ inline void run_of(const state<D, DIG, NR>& s, int n, int i, float* x
 
 // Results of a share of the keys, past the caches that other workgroups do not share
 struct shares {
-  float *data, *lse;
+  float *data, *sums;  // rows of D; (m, sum) of each
   size_t first;  // the first share's first row
   int rows_pad;
   template <int D>
@@ -492,14 +502,22 @@ struct shares {
     first = ((size_t)j.seq * p.c.heads + j.head) * p.split * p.rows_pad;
     rows_pad = p.rows_pad;
     data = p.partial;
-    lse = p.partial + (size_t)p.batch * p.c.heads * p.split * p.rows_pad * D;
+    sums = p.partial + (size_t)p.batch * p.c.heads * p.split * p.rows_pad * D;
   }
   __device__ inline size_t at(int slice, int row) const { return first + (size_t)slice * rows_pad + row; }
 };
 __device__ inline void hand_in(float* to, f4 x) {  // 16 bytes at once (their registers may not be written to in the next cycle)
   asm volatile("global_store_dwordx4 %0, %1, off sc1\n\ts_nop 1" ::"v"(to), "v"(x) : "memory");
 }
-__device__ inline void hand_in(float* to, float a) { __hip_atomic_store(to, a, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+__device__ inline void hand_in(float* to, float a, float b) {
+  __hip_atomic_store(reinterpret_cast<u64*>(to), (u64)__builtin_bit_cast(unsigned, a) | (u64)__builtin_bit_cast(unsigned, b) << 32,
+                     __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ inline float low(u64 x) { return __builtin_bit_cast(float, (unsigned)x); }
+__device__ inline float high(u64 x) { return __builtin_bit_cast(float, (unsigned)(x >> 32)); }
+__device__ inline u64 fetch(const float* from) {
+  return __hip_atomic_load(reinterpret_cast<const u64*>(from), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
 
 // Keys split over workgroups: the last one to arrive adds the shares, in their order.  THREADS of the workgroup.  An item is four
 // channels of a row; a thread requests BATCH shares of ITEMS items together, since a request past the caches takes more than a
@@ -529,36 +547,34 @@ __device__ inline void join(const qg_kv4_attention_args& p, const job& j, const 
       x[k] = (f4){0.0f, 0.0f, 0.0f, 0.0f};
     }
     for (int t0 = mine * BATCH; t0 < j.slices; t0 += groups * BATCH) {
-      float lse[ITEMS][BATCH];
-      u64 u[ITEMS][BATCH], v[ITEMS][BATCH];
+      u64 ms[ITEMS][BATCH], u[ITEMS][BATCH], v[ITEMS][BATCH];
 #pragma unroll
       for (int k = 0; k < ITEMS; ++k)
 #pragma unroll
         for (int t = 0; t < BATCH; ++t) {
           const size_t from = w.at(min(t0 + t, j.slices - 1), j.row0 + item[k] / (D / 4));
-          lse[k][t] = __hip_atomic_load(w.lse + from, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-          const u64* data = reinterpret_cast<const u64*>(w.data + from * D + item[k] % (D / 4) * 4);
-          u[k][t] = __hip_atomic_load(data, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-          v[k][t] = __hip_atomic_load(data + 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+          ms[k][t] = fetch(w.sums + 2 * from);
+          const float* data = w.data + from * D + item[k] % (D / 4) * 4;
+          u[k][t] = fetch(data);
+          v[k][t] = fetch(data + 2);
         }
 #pragma unroll
       for (int k = 0; k < ITEMS; ++k) {
-        float high = top[k];
+        float most = top[k];
 #pragma unroll
-        for (int t = 0; t < BATCH; ++t) high = fmaxf(high, lse[k][t]);
-        const float base = high == -__builtin_inff() ? 0.0f : high;
-        const float f = __builtin_amdgcn_exp2f(top[k] - base);
-        top[k] = high;
+        for (int t = 0; t < BATCH; ++t) most = fmaxf(most, low(ms[k][t]));
+        const float f = weight(top[k], 1.0f, most);
+        top[k] = most;
         total[k] *= f;
         x[k] *= f;
 #pragma unroll
         for (int t = 0; t < BATCH; ++t) {
-          const float e = t0 + t < j.slices ? __builtin_amdgcn_exp2f(lse[k][t] - base) : 0.0f;
+          const float e = t0 + t < j.slices ? weight(low(ms[k][t]), high(ms[k][t]), most) : 0.0f;
           total[k] += e;
-          x[k][0] += e * __builtin_bit_cast(float, (unsigned)u[k][t]);
-          x[k][1] += e * __builtin_bit_cast(float, (unsigned)(u[k][t] >> 32));
-          x[k][2] += e * __builtin_bit_cast(float, (unsigned)v[k][t]);
-          x[k][3] += e * __builtin_bit_cast(float, (unsigned)(v[k][t] >> 32));
+          x[k][0] += e * low(u[k][t]);
+          x[k][1] += e * high(u[k][t]);
+          x[k][2] += e * low(v[k][t]);
+          x[k][3] += e * high(v[k][t]);
         }
       }
     }
@@ -582,11 +598,10 @@ __device__ inline void join(const qg_kv4_attention_args& p, const job& j, const 
   if (item >= items) return;
   float top = -__builtin_inff(), total = 0.0f;
   for (int k = 0; k < groups; ++k) top = fmaxf(top, scratch[(k * items + item) * 8 + 4]);
-  const float base = top == -__builtin_inff() ? 0.0f : top;
   f4 x = (f4){0.0f, 0.0f, 0.0f, 0.0f};
   for (int k = 0; k < groups; ++k) {
     const float* from = scratch + (k * items + item) * 8;
-    const float e = __builtin_amdgcn_exp2f(from[4] - base);
+    const float e = weight(from[4], 1.0f, top);
     total += e * from[5];
     x += e * *reinterpret_cast<const f4*>(from);
   }

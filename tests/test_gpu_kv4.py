@@ -419,6 +419,25 @@ def test_scores_far_below_zero(env, q_lens):
         assert ((got[i] - want).abs() <= 2.0 ** -20 * want.abs()).all()
 
 
+@pytest.mark.parametrize("D,n_q", [(64, 1), (64, 20), (128, 1), (128, 40), (256, 1), (256, 40)])
+@pytest.mark.parametrize("n", [1, 64])
+def test_keys_all_alike_give_their_value(env, D, n_q, n):
+    """n tokens alike: each has a probability of 1 / n whatever the score, and an fp32 result is the value they hold.  Over 2^16 rows
+    of scores of all fractions: 2^-22 of the two fp16 numbers for a probability and 2^-24 n each for its two sums."""
+    kv4, torch, dev = env
+    Hq, Hkv, P, B = 16, 2, 64, 4096 // n_q
+    g = torch.Generator(device=dev).manual_seed(D + n_q)
+    cache = kv4.new_cache(B, Hkv, D, P, device=dev)
+    k, v = (torch.randn(B, Hkv, D, device=dev, generator=g).repeat_interleave(n, 0) for _ in range(2))
+    kv4.append(cache, k, v, (torch.arange(B, device=dev)[:, None] * P + torch.arange(n, device=dev)).flatten())
+    held = kv4.read(cache, torch.arange(B, device=dev) * P)[1].repeat_interleave(n_q, 0).repeat_interleave(Hq // Hkv, 1)
+    q = torch.randn(B * n_q, Hq, D, device=dev, generator=g)
+    got = kv4.attention(q, cache, torch.arange(B, device=dev, dtype=torch.int32)[:, None], torch.full((B,), n, dtype=torch.int32, device=dev),
+                        q_starts=torch.arange(B + 1, dtype=torch.int32, device=dev) * n_q, max_q_len=n_q, max_kv_len=n, causal=False)
+    off = ((got - held).abs() / held.abs().clamp(min=1e-30)).max()
+    assert off <= 2.0 ** -21 + 2 * (n + 4) * 2.0 ** -24, f"{float(off):.1e}"
+
+
 def test_value_scales_of_all_sizes(env):
     """Values 2^60 apart between tokens: the small ones count where the large ones have no weight."""
     kv4, torch, dev = env
