@@ -45,38 +45,50 @@ int check_rotation(const float* table, int max_pos, int rot, int interleaved, in
   return aligned(table, 16) ? QG_OK : QG_EALIGN;
 }
 
-// ---- keys of a sequence over workgroups
+// ---- keys over workgroups
 // With few sequences a workgroup per (sequence, KV head, rows) leaves most of the 256 CUs idle, and with long ones that differ in
-// length the longest ends alone.  Keys are dealt in chunks of equal length, at least what a workgroup's start and end cost, and not
-// at all up to twice that (777 keys of 8 KV heads: 9.0 us in four shares, 9.1 whole).  Few rows: chunks that give every CU a workgroup.  More would cost more than it evens out: every share is written, and read by
-// the last one to arrive (131072 keys of 8 KV heads, 8 rows: 34 us in 256 shares, 40 in 512, 49 in 1024).  Many rows: workgroups run for
-// long, so eight times as many (512 queries of four sequences up to 8192 keys: 240 us whole, 203 in 1024 workgroups, 165 in 2048, 161 in
-// 3072, 176 in 4096).
-constexpr int CUS = 256;
+// length the longest ends alone.  A share is at least what a workgroup's start and end cost, and keys are not dealt at all up to
+// twice that (777 keys of 8 KV heads: 9.0 us in four shares, 9.1 whole).
+//   Few rows: shares of equal length, so many that every CU has a workgroup if all sequences are as long as the longest may be.  More
+//   would cost more than it evens out: every share is written, and read by the last one to arrive (131072 keys of 8 KV heads, 8 rows:
+//   34 us in 256 shares, 40 in 512, 49 in 1024), and so would shares by the lengths there are, as below (64 sequences of up to 8192
+//   keys: 69.3 us for 69.0; 16 of up to 4096, 5 queries: 27.9 for 25.6).
+//   Many rows: workgroups run for long, so the kernel deals the keys by the lengths that it finds (512 queries of four sequences of
+//   8192, 1981, 1766 and 1310 keys: 154 us with 512 workgroups, 152 with 768, 145 with 1024, 168 with 1536; 240 whole, 164 in
+//   shares of equal length).
+constexpr int FEW_SHARES = 256, MANY_SHARES = 1024;
 constexpr size_t COUNTERS = 16384;  // a fixed part of every workspace, so that calls of other extents find it zero
 
 struct share {
-  int split, chunk, rows_pad;
+  int split, piece, shares, least;
+  long long rows;  // of results in the workspace; 0: keys not split
 };
 
 share share_of(const qg_kv4_cache* c, int q_heads, int batch, int max_q_len, int max_kv_len) {
   const long long rows = (long long)max_q_len * (q_heads / c->kv_heads), per = qg_kv4_rows_per_workgroup(c->head_dim, rows);
-  share s = {1, (max_kv_len + 63) / 64 * 64, (int)((rows + 15) / 16 * 16)};
-  const long long units = (long long)batch * c->kv_heads * ((rows + per - 1) / per);
-  if ((size_t)((long long)batch * c->kv_heads * ((rows + 15) / 16)) > COUNTERS) return s;  // (workgroups have 16 rows at least)
-  const int least = rows <= QG_KV4_FEW ? 256 : 512, workgroups = rows <= QG_KV4_FEW ? CUS : 8 * CUS;
-  long long chunk = ((long long)max_kv_len * units / workgroups + 63) / 64 * 64;
-  if (chunk < least) chunk = least;
-  if (chunk >= max_kv_len || max_kv_len <= 2 * least) return s;
-  s.chunk = (int)chunk;
-  s.split = (int)((max_kv_len + chunk - 1) / chunk);
+  const long long heads = (long long)batch * c->kv_heads, blocks = (rows + per - 1) / per;
+  const long long most = heads * ((rows + 15) / 16);  // workgroups have 16 rows at least
+  const bool few = rows <= QG_KV4_FEW;
+  const int least = few ? 256 : 512;
+  share s = {1, 0x40000000, 0, 0, 0};
+  if (max_kv_len <= 2 * least) return s;
+  if (few) {
+    const long long piece = ((long long)max_kv_len * heads * blocks / FEW_SHARES + 63) / 64 * 64;
+    if (piece >= max_kv_len || most + 16 > (long long)COUNTERS) return s;
+    s.piece = (int)(piece < least ? least : piece);
+    s.split = (max_kv_len + s.piece - 1) / s.piece;
+    s.rows = heads * blocks * s.split * per;
+  } else {
+    // (the kernel adds up workgroups, and the stages of all, in 32 bits)
+    if (MANY_SHARES + most > (long long)COUNTERS || most * ((max_kv_len + 63) / 64) > 0x7fff0000ll) return s;
+    s.shares = MANY_SHARES;
+    s.least = least / 64;
+    s.rows = (MANY_SHARES + heads * blocks) * per;
+  }
   return s;
 }
 
-size_t share_bytes(const share& s, int kv_heads, int batch, int head_dim) {
-  if (s.split == 1) return 0;
-  return COUNTERS * 4 + (size_t)batch * kv_heads * s.split * s.rows_pad * (head_dim + 2) * 4;
-}
+size_t share_bytes(const share& s, int head_dim) { return s.rows == 0 ? 0 : COUNTERS * 4 + (size_t)s.rows * (head_dim + 2) * 4; }
 
 bool extents_ok(const qg_kv4_cache* c, int q_heads, int batch, int max_q_len, int max_kv_len) {
   if (q_heads < 1 || q_heads % c->kv_heads != 0 || batch < 0 || max_q_len < 0 || max_kv_len < 0) return false;
@@ -234,7 +246,7 @@ int qg_kv4_read(const qg_kv4_cache* c, const int64_t* slots, int tokens, int dty
 size_t qg_kv4_attention_workspace_bytes(const qg_kv4_cache* c, int q_heads, int batch, int max_q_len, int max_kv_len) {
   if (!c || qg_kv4_bytes(c->n_pages, c->kv_heads, c->head_dim, c->page_tokens) == 0) return 0;
   if (!extents_ok(c, q_heads, batch, max_q_len, max_kv_len) || batch == 0 || max_q_len == 0 || max_kv_len == 0) return 0;
-  return share_bytes(share_of(c, q_heads, batch, max_q_len, max_kv_len), c->kv_heads, batch, c->head_dim);
+  return share_bytes(share_of(c, q_heads, batch, max_q_len, max_kv_len), c->head_dim);
 }
 
 int qg_kv4_attention(const qg_kv4_cache* c, const qg_kv4_attention_params* p, void* stream) {
@@ -252,17 +264,13 @@ int qg_kv4_attention(const qg_kv4_cache* c, const qg_kv4_attention_params* p, vo
   if ((rc = check_heads(p->q, p->dtype)) != QG_OK || (rc = check_heads(p->out, p->dtype)) != QG_OK) return rc;
   const int max_q = p->q_starts ? p->max_q_len : 1;
   share s = share_of(c, p->q_heads, p->batch, max_q, p->max_kv_len);
-  if (!p->workspace) {
-    s.split = 1;
-    s.chunk = (p->max_kv_len + 63) / 64 * 64;
-  }
-  if (s.split > 1) {
-    if (p->workspace_bytes < share_bytes(s, c->kv_heads, p->batch, c->head_dim)) return QG_EWORKSPACE;
+  if (!p->workspace) s = {1, 0x40000000, 0, 0, 0};
+  if (s.rows > 0) {
+    if (p->workspace_bytes < share_bytes(s, c->head_dim)) return QG_EWORKSPACE;
     if (!aligned(p->workspace, 16)) return QG_EALIGN;
   }
-  if (s.chunk == 0) s.chunk = 64;
   const long long rows = (long long)max_q * (p->q_heads / c->kv_heads);
-  if (((long long)p->batch * c->kv_heads * s.split + 8) * ((rows + 15) / 16) > 0x7fffffffll / 256) return QG_EUNSUPPORTED;
+  if ((long long)p->batch * c->kv_heads * s.split * ((rows + 15) / 16) > 0x7fffffffll / 512) return QG_EUNSUPPORTED;
   a.q = p->q.data;
   a.out = p->out.data;
   a.pages = p->pages;
@@ -279,10 +287,14 @@ int qg_kv4_attention(const qg_kv4_cache* c, const qg_kv4_attention_params* p, vo
   a.scale_log2e = (float)to_log2;
   a.scale_log2e_lo = (float)(to_log2 - (double)a.scale_log2e);
   a.split = s.split;
-  a.chunk = s.chunk;
-  a.rows_pad = s.rows_pad;
-  a.counters = static_cast<int*>(p->workspace);
-  a.partial = reinterpret_cast<float*>(static_cast<char*>(p->workspace) + (p->workspace ? COUNTERS * 4 : 0));
+  a.piece = s.piece;
+  a.shares = s.shares;
+  a.least = s.least;
+  if (s.rows > 0) {
+    a.counters = static_cast<int*>(p->workspace);
+    a.partial = reinterpret_cast<float*>(a.counters + COUNTERS);
+    a.sums = a.partial + (size_t)s.rows * c->head_dim;
+  }
   a.q_token = p->q.token_stride;
   a.q_head = p->q.head_stride;
   a.o_token = p->out.token_stride;

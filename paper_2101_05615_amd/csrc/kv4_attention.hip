@@ -109,7 +109,7 @@ __global__ __launch_bounds__(64 * WAVES, waves_per_simd(D, NR)) void qg_kv4_atte
   const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   const int r = lane & 15, g = lane >> 4;
   job j;
-  if (!j.init<ROWS>(p)) return;
+  if (!j.init<ROWS, false>(p)) return;
   const reader<D, SMALL> in(p, j.seq, j.head, r, g);
   int t0 = j.lo + wave * TILE;
   page_ids next = {0u, 0u};
@@ -185,8 +185,7 @@ __global__ __launch_bounds__(64 * WAVES, waves_per_simd(D, NR)) void qg_kv4_atte
     }
   }
   __syncthreads();
-  shares w;
-  w.init<D>(p, j);
+  const shares<ROWS> w(p, j);
   for (int at = (int)threadIdx.x; at < (j.last_row - j.row0 + 1) * (D / 4); at += 64 * WAVES) {
     const int local = at / (D / 4), c = at % (D / 4) * 4, row = j.row0 + local;
     float top = -__builtin_inff();
@@ -219,8 +218,7 @@ template <int D, int TYPE, int NR>
 void go(qg_kv4_attention_args a, int rows, hipStream_t s) {
   constexpr int DIG = TYPE == QG_F32 ? 2 : 1;
   a.row_blocks = (rows + 16 * NR - 1) / (16 * NR);
-  const long long units = (long long)a.batch * a.c.heads * a.split;
-  const dim3 grid((unsigned)((units + 7) / 8 * 8 * a.row_blocks));
+  const dim3 grid((unsigned)(a.batch * a.c.heads * a.split * a.row_blocks));
   if (a.c.lgp == 4)
     hipLaunchKernelGGL((qg_kv4_attention_kernel<D, DIG, TYPE, NR, true>), grid, dim3(64 * WAVES), 0, s, a);
   else

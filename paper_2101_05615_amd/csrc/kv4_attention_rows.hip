@@ -143,7 +143,7 @@ __global__ __launch_bounds__(64 * waves_of(D), 2) void qg_kv4_attention_rows_ker
   const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   const int r = lane & 15, g = lane >> 4;
   job j;
-  if (!j.init<ROWS>(p)) return;
+  if (!j.init<ROWS, true>(p)) return;
   const reader<D, SMALL> in(p, j.seq, j.head, r, g);
   const int wave_row = j.row0 + wave * 16 * NR;
 
@@ -211,8 +211,7 @@ __global__ __launch_bounds__(64 * waves_of(D), 2) void qg_kv4_attention_rows_ker
 
   float sum[NR];
   finish(s, sum);
-  shares w;
-  w.init<D>(p, j);
+  const shares<ROWS> w(p, j);
 #pragma unroll
   for (int n = 0; n < NR; ++n) {
     const int row = wave_row + n * 16 + r;
@@ -239,8 +238,7 @@ template <int D, int TYPE>
 void go(qg_kv4_attention_args a, int rows, hipStream_t s) {
   constexpr int DIG = TYPE == QG_F32 ? 2 : 1, NR = D == 256 || DIG == 2 ? 1 : 2, WAVES = waves_of(D), ROWS = 16 * NR * WAVES;
   a.row_blocks = (rows + ROWS - 1) / ROWS;
-  const long long units = (long long)a.batch * a.c.heads * a.split;
-  const dim3 grid((unsigned)((units + 7) / 8 * 8 * a.row_blocks));
+  const dim3 grid((unsigned)(a.shares + a.batch * a.c.heads * a.row_blocks));  // (shares of a sequence: one more than it fills)
   if (a.c.lgp == 4)
     hipLaunchKernelGGL((qg_kv4_attention_rows_kernel<D, DIG, TYPE, NR, true>), grid, dim3(64 * WAVES), 0, s, a);
   else

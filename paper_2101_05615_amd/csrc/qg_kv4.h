@@ -177,11 +177,11 @@ struct qg_kv4_attention_args {
   qg_kv4_layout c;
   int tokens, group, batch, pages_stride, max_q_len, max_kv_len, causal;
   float scale_log2e, scale_log2e_lo;  // two parts
-  int split, chunk;          // workgroups that share a sequence's keys, and tokens each takes (a multiple of 32)
+  int split, piece;          // workgroups that share a sequence's keys, and tokens each takes (a multiple of 64); or, many rows:
+  int shares, least;         // workgroups that the keys of the whole batch are dealt to (0: split 1), stages of 64 tokens each has at least
   int row_blocks;            // workgroups over a KV head's query rows
-  int rows_pad;              // rows of a KV head in the workspace
-  int* counters;             // one per (sequence, KV head, row block), zero before and after
-  float* partial;            // [sequence][KV head][split][rows_pad][D], then reference and sum of each row
+  int* counters;             // one a workgroup, zero before and after
+  float *partial, *sums;     // [workgroup][rows of a workgroup][D]; reference and sum of each row
   int64_t q_token, q_head, o_token, o_head;
 };
 

@@ -388,39 +388,104 @@ __device__ inline int split_query(const raw_query<D, TYPE>& raw, frag (*q)[D / 3
   return shift;
 }
 
+// Running sums over the lanes of a wave (lane 63: of all)
+__device__ inline int running(int x) {
+  x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, true);   // row_shr:1, 2, 4, 8
+  x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, true);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, true);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, true);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);  // row_bcast:15, :31
+  x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);
+  return x;
+}
+
 // Which rows, keys and workgroups a workgroup deals with
 struct job {
-  int head, seq, slice, slices, rb;
+  int head, seq, slice, slices;
   int q0, n, keys;           // the sequence's first query, its queries, its keys
   int rows, row0, last_row;  // of the KV head; this workgroup's first and last
   int lo, hi;                // its tokens
-  template <int ROWS>
-  __device__ inline bool init(const qg_kv4_attention_args& p) {
-    // Workgroups over the rows of one (sequence, KV head, share of the keys) read the same keys: ids that differ by eight share an
-    // L2.  Heads come first in the numbering of units: with a sequence's shares side by side, shares that only long sequences have
-    // would fall to the same few XCDs.
-    const int units = p.batch * p.c.heads * p.split;
-    const int id = (int)blockIdx.x, unit = (id / (8 * p.row_blocks)) * 8 + id % 8;
-    if (unit >= units) return false;
-    rb = p.row_blocks - 1 - (id / 8) % p.row_blocks;  // (the rows that see the most keys first)
-    head = unit % p.c.heads;
-    seq = (unit / p.c.heads) % p.batch;
-    slice = unit / p.c.heads / p.batch;
-    q0 = seq;
+  int first, units, blocks, block;  // units of a (sequence, KV head, share of the keys) numbered together, `blocks` workgroups each, from `first` on
+  int unit0, unit_step;             // those of this one's first share, from share to share
+  __device__ inline void look(const qg_kv4_attention_args& p, int b) {
+    q0 = b;
     n = 1;
     if (p.q_starts != nullptr) {
-      q0 = min(max(p.q_starts[seq], 0), p.tokens);
-      n = min(max(p.q_starts[seq + 1], q0), p.tokens) - q0;
+      q0 = min(max(p.q_starts[b], 0), p.tokens);
+      n = min(max(p.q_starts[b + 1], q0), p.tokens) - q0;
     }
-    keys = min(max(p.kv_lens[seq], 0), p.max_kv_len);
+    keys = min(max(p.kv_lens[b], 0), p.max_kv_len);
     rows = min(n, p.max_q_len) * p.group;
-    row0 = rb * ROWS;
+  }
+  // A unit's workgroups, which differ in their rows, read the same keys: ids that differ by eight share an L2.  The first
+  // units / 8 * 8 units go by eights, what is left spreads.
+  __device__ inline int id_of(int share) const {
+    const int unit = unit0 + share * unit_step, whole = units & ~7;
+    return first + (unit < whole ? (unit >> 3) * 8 * blocks + block * 8 + (unit & 7) : whole * blocks + block * (units - whole) + unit - whole);
+  }
+  template <int ROWS, bool MANY>
+  __device__ inline bool init(const qg_kv4_attention_args& p) {
+    const int id = (int)blockIdx.x;
+    int unit, piece = p.piece;
+    if (!MANY || p.shares == 0) {  // heads first: shares that only long sequences have would fall to the same few XCDs otherwise
+      units = p.batch * p.c.heads * p.split;
+      blocks = p.row_blocks;
+      first = 0;
+    } else {
+      // Every wave deals the keys for itself: shares of one length for the whole batch (in stages of 64 tokens), so many as there are
+      // to be workgroups, then of one length within each sequence.
+      const int lane = (int)threadIdx.x & 63;
+      int total = 0;
+      for (int b0 = 0; b0 < p.batch; b0 += 64) {
+        look(p, min(b0 + lane, p.batch - 1));
+        const int work = b0 + lane < p.batch ? (keys + 63) / 64 * ((rows + ROWS - 1) / ROWS) * p.c.heads : 0;
+        total += __builtin_amdgcn_readlane(running(work), 63);
+      }
+      const int stages = max(p.least, (total + p.shares - 1) / p.shares);
+      first = 0;
+      bool found = false;
+      for (int b0 = 0; b0 < p.batch && !found; b0 += 64) {
+        if (p.batch > 64) look(p, min(b0 + lane, p.batch - 1));
+        const int all = (keys + 63) / 64, about = max((all + stages - 1) / stages, 1);
+        const int mine = max((all + about - 1) / about, 1), n_shares = max((all + mine - 1) / mine, 1);
+        const int n_blocks = b0 + lane < p.batch ? (rows + ROWS - 1) / ROWS : 0;
+        const int upto = first + running(n_shares * n_blocks * p.c.heads);
+        const unsigned long long here = __ballot(id < upto);
+        found = here != 0ull;
+        const int l = found ? __builtin_ctzll(here) : 63;
+        first = __builtin_amdgcn_readlane(upto - (found ? n_shares * n_blocks * p.c.heads : 0), l);
+        seq = b0 + l;
+        units = __builtin_amdgcn_readlane(n_shares, l) * p.c.heads;
+        blocks = __builtin_amdgcn_readlane(n_blocks, l);
+        piece = __builtin_amdgcn_readlane(mine, l) * 64;
+      }
+      if (!found) return false;
+    }
+    const int local = id - first, whole = units & ~7, rest = units - whole;
+    if (local < whole * blocks) {
+      unit = local / (8 * blocks) * 8 + (local & 7);
+      block = local / 8 % blocks;
+    } else {
+      unit = whole + (local - whole * blocks) % rest;
+      block = (local - whole * blocks) / rest;
+    }
+    head = unit % p.c.heads;
+    slice = unit / p.c.heads;
+    unit_step = p.c.heads;
+    if (!MANY || p.shares == 0) {
+      seq = slice % p.batch;
+      slice /= p.batch;
+      unit_step *= p.batch;
+    }
+    unit0 = unit - slice * unit_step;
+    look(p, seq);
+    row0 = (blocks - 1 - block) * ROWS;  // (the rows that see the most keys first)
     if (row0 >= rows) return false;
     last_row = min(row0 + ROWS, rows) - 1;
     const int seen = p.causal ? min(max(keys - n + last_row / p.group + 1, 0), keys) : keys;  // keys that some row sees
-    slices = max((seen + p.chunk - 1) / p.chunk, 1);
-    lo = slice * p.chunk;
-    hi = min(lo + p.chunk, seen);
+    slices = max((seen + piece - 1) / piece, 1);
+    lo = slice * piece;
+    hi = min(lo + piece, seen);
     return slice < slices;
   }
   // keys that all rows from `row` on see
@@ -492,19 +557,13 @@ __device__ inline void run_of(const state<D, DIG, NR>& s, int n, int i, float* x
   for (int c = 0; c < 16; ++c) x[c] = s.o[n][4 * i + c % 4][c / 4];
 }
 
-// Results of a share of the keys, past the caches that other workgroups do not share
+// Results of a share of the keys, past the caches that other workgroups do not share: a workgroup's rows under its number
+template <int ROWS>
 struct shares {
   float *data, *sums;  // rows of D; (m, sum) of each
-  size_t first;  // the first share's first row
-  int rows_pad;
-  template <int D>
-  __device__ inline void init(const qg_kv4_attention_args& p, const job& j) {
-    first = ((size_t)j.seq * p.c.heads + j.head) * p.split * p.rows_pad;
-    rows_pad = p.rows_pad;
-    data = p.partial;
-    sums = p.partial + (size_t)p.batch * p.c.heads * p.split * p.rows_pad * D;
-  }
-  __device__ inline size_t at(int slice, int row) const { return first + (size_t)slice * rows_pad + row; }
+  const job& j;
+  __device__ inline shares(const qg_kv4_attention_args& p, const job& j) : data(p.partial), sums(p.sums), j(j) {}
+  __device__ inline size_t at(int slice, int row) const { return (size_t)j.id_of(slice) * ROWS + (row - j.row0); }
 };
 __device__ inline void hand_in(float* to, f4 x) {  // 16 bytes at once (their registers may not be written to in the next cycle)
   asm volatile("global_store_dwordx4 %0, %1, off sc1\n\ts_nop 1" ::"v"(to), "v"(x) : "memory");
@@ -523,11 +582,11 @@ __device__ inline u64 fetch(const float* from) {
 // channels of a row; a thread requests BATCH shares of ITEMS items together, since a request past the caches takes more than a
 // microsecond.  scratch: 8 floats a thread, or NULL; with it, where there are fewer items than threads, groups of threads take every
 // groups-th batch of shares and meet there.
-template <int D, int TYPE, int THREADS, int ITEMS, int BATCH>
-__device__ inline void join(const qg_kv4_attention_args& p, const job& j, const shares& w, float* scratch, int* ticket) {
+template <int D, int TYPE, int THREADS, int ITEMS, int BATCH, int ROWS>
+__device__ inline void join(const qg_kv4_attention_args& p, const job& j, const shares<ROWS>& w, float* scratch, int* ticket) {
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // what this wave handed in has been acknowledged
   __syncthreads();
-  int* const counter = p.counters + ((size_t)j.seq * p.c.heads + j.head) * p.row_blocks + j.rb;
+  int* const counter = p.counters + j.id_of(0);
   if (threadIdx.x == 0) *ticket = __hip_atomic_fetch_add(counter, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
   __syncthreads();
   if (*ticket != j.slices - 1) return;

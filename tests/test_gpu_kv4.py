@@ -350,6 +350,27 @@ def test_many_queries_split(env, dtype):
     b.check(b.run(None))
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("D,Hq,Hkv", [(64, 10, 5), (128, 6, 3), (256, 2, 1)])
+def test_keys_dealt_over_a_batch(env, dtype, D, Hq, Hkv):
+    """More sequences than a wave has lanes, of all lengths, some without queries or keys: keys are dealt by what is there."""
+    kv4, torch, dev = env
+    rng = np.random.default_rng(D)
+    lens = [int(x) for x in np.exp(rng.uniform(0, math.log(1500), 70))] + [0, 1500, 1281, 1]
+    q_lens = [int(x) for x in rng.integers(0, 6, 70)] + [3, 140, 33, 2]
+    b = Batch(env, lens, Hq, Hkv, D, 32, dtype, seed=D, q_lens=q_lens)
+    ws = kv4.attention_workspace(b.cache, Hq, len(lens), max_q_len=140, max_kv_len=1500)
+    assert ws is not None
+    got = b.run(ws)
+    b.check(got)
+    assert torch.equal(got, b.run(ws)) and (ws[:65536] == 0).all()
+    b.check(b.run(ws, causal=False), causal=False)
+    short = [min(m, 700) for m in lens]                # other lengths in the same workspace
+    b.lens, b.slots = short, [s[:m] for s, m in zip(b.slots, short)]
+    b.kv_lens.copy_(torch.tensor(short, dtype=torch.int32))
+    b.check(b.run(ws, max_kv_len=1500))
+
+
 def test_rows_without_keys_are_zero(env):
     kv4, torch, dev = env
     b = Batch(env, [0, 2], 4, 2, 64, 16, "float32", q_lens=[3, 4])
