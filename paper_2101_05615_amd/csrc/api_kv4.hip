@@ -53,10 +53,11 @@ int check_rotation(const float* table, int max_pos, int rot, int interleaved, in
 //   would cost more than it evens out: every share is written, and read by the last one to arrive (131072 keys of 8 KV heads, 8 rows:
 //   34 us in 256 shares, 40 in 512, 49 in 1024), and so would shares by the lengths there are, as below (64 sequences of up to 8192
 //   keys: 69.3 us for 69.0; 16 of up to 4096, 5 queries: 27.9 for 25.6).
-//   Many rows: workgroups run for long, so the kernel deals the keys by the lengths that it finds (512 queries of four sequences of
-//   8192, 1981, 1766 and 1310 keys: 154 us with 512 workgroups, 152 with 768, 145 with 1024, 168 with 1536; 240 whole, 164 in
-//   shares of equal length).
-constexpr int FEW_SHARES = 256, MANY_SHARES = 1024;
+//   Many rows: workgroups run for long, so the kernel deals the keys by the lengths that it finds, in one or two rounds of the
+//   workgroups that run at once (three a CU with 64 channels, two with 128, one with 256).  512 queries of four sequences of 8192,
+//   1981, 1766 and 1310 keys, 32 heads over 8 of 128 channels: 150 us (equal shares 164, whole 240); four of 4096 keys: 171, as whole
+//   (two rounds 200); one of 8192, 8 heads over one: 56 (in as many shares as run at once 64).
+constexpr int FEW_SHARES = 256;
 constexpr size_t COUNTERS = 16384;  // a fixed part of every workspace, so that calls of other extents find it zero
 
 struct share {
@@ -79,11 +80,12 @@ share share_of(const qg_kv4_cache* c, int q_heads, int batch, int max_q_len, int
     s.split = (max_kv_len + s.piece - 1) / s.piece;
     s.rows = heads * blocks * s.split * per;
   } else {
-    // (the kernel adds up workgroups, and the stages of all, in 32 bits)
-    if (MANY_SHARES + most > (long long)COUNTERS || most * ((max_kv_len + 63) / 64) > 0x7fff0000ll) return s;
-    s.shares = MANY_SHARES;
+    const int at_once = c->head_dim == 64 ? 768 : c->head_dim == 128 ? 512 : 256;
+    // (more than two rounds even out by themselves; the kernel adds up workgroups, and the stages of all, in 32 bits)
+    if (heads * blocks > 2 * at_once || most + 16 > (long long)COUNTERS || most * ((max_kv_len + 63) / 64) > 0x7fff0000ll) return s;
+    s.shares = at_once;
     s.least = least / 64;
-    s.rows = (MANY_SHARES + heads * blocks) * per;
+    s.rows = 4ll * at_once * per;  // 2 at_once and one more per (sequence, head, block of rows); with blocks of 64 rows, 6 at_once of 64
   }
   return s;
 }

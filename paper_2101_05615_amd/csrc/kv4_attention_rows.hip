@@ -238,7 +238,7 @@ template <int D, int TYPE>
 void go(qg_kv4_attention_args a, int rows, hipStream_t s) {
   constexpr int DIG = TYPE == QG_F32 ? 2 : 1, NR = D == 256 || DIG == 2 ? 1 : 2, WAVES = waves_of(D), ROWS = 16 * NR * WAVES;
   a.row_blocks = (rows + ROWS - 1) / ROWS;
-  const dim3 grid((unsigned)(a.shares + a.batch * a.c.heads * a.row_blocks));  // (shares of a sequence: one more than it fills)
+  const dim3 grid((unsigned)(2 * a.shares + a.batch * a.c.heads * a.row_blocks));  // (a sequence has one more share than it fills at most)
   if (a.c.lgp == 4)
     hipLaunchKernelGGL((qg_kv4_attention_rows_kernel<D, DIG, TYPE, NR, true>), grid, dim3(64 * WAVES), 0, s, a);
   else

@@ -178,7 +178,7 @@ struct qg_kv4_attention_args {
   int tokens, group, batch, pages_stride, max_q_len, max_kv_len, causal;
   float scale_log2e, scale_log2e_lo;  // two parts
   int split, piece;          // workgroups that share a sequence's keys, and tokens each takes (a multiple of 64); or, many rows:
-  int shares, least;         // workgroups that the keys of the whole batch are dealt to (0: split 1), stages of 64 tokens each has at least
+  int shares, least;         // workgroups that run at once, to whom the kernel deals the keys (0: split 1), and stages of 64 tokens each has at least
   int row_blocks;            // workgroups over a KV head's query rows
   int* counters;             // one a workgroup, zero before and after
   float *partial, *sums;     // [workgroup][rows of a workgroup][D]; reference and sum of each row

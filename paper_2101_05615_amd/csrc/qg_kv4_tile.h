@@ -432,31 +432,55 @@ struct job {
       blocks = p.row_blocks;
       first = 0;
     } else {
-      // Every wave deals the keys for itself: shares of one length for the whole batch (in stages of 64 tokens), so many as there are
-      // to be workgroups, then of one length within each sequence.
-      const int lane = (int)threadIdx.x & 63;
-      int total = 0;
-      for (int b0 = 0; b0 < p.batch; b0 += 64) {
+      // Every wave deals the keys for itself: shares of at most `stages` of 64 tokens, of one length within a sequence.  Three ways: the
+      // fewest stages that make no more workgroups than there are CUs, or than run at once, or half of what each of those
+      // would have on average.  A round costs its stages and about four (queries in, results out; four fifths of it for a workgroup
+      // that has a CU to itself), the join one a share; the cheapest way is taken.
+      const int lane = (int)threadIdx.x & 63, longest = (p.max_kv_len + 63) / 64;
+      int all, wide;  // of the lane's sequence: stages, workgroups of a share
+      auto measure = [&](int b0) {
         look(p, min(b0 + lane, p.batch - 1));
-        const int work = b0 + lane < p.batch ? (keys + 63) / 64 * ((rows + ROWS - 1) / ROWS) * p.c.heads : 0;
-        total += __builtin_amdgcn_readlane(running(work), 63);
+        all = (keys + 63) / 64;
+        wide = b0 + lane < p.batch ? (rows + ROWS - 1) / ROWS * p.c.heads : 0;
+      };
+      measure(0);
+      int work = 0;
+      for (int b0 = 0; b0 < p.batch; b0 += 64) {
+        if (b0 > 0) measure(b0);
+        work += __builtin_amdgcn_readlane(running(all * wide), 63);
       }
-      const int stages = max(p.least, (total + p.shares - 1) / p.shares);
+      auto fit = [&](int workgroups) {  // (a share more or less does no harm: the quotients need not be exact)
+        int x = max(p.least, (work + workgroups - 1) / workgroups);
+        for (; x < longest; x += max(x >> 3, 1)) {
+          const float inv = __builtin_amdgcn_rcpf((float)x);
+          int n = 0;
+          for (int b0 = 0; b0 < p.batch; b0 += 64) {
+            if (p.batch > 64) measure(b0);
+            n += __builtin_amdgcn_readlane(running(max((int)__builtin_ceilf((float)all * inv), 1) * wide), 63);
+          }
+          if (n <= workgroups) break;
+        }
+        return min(x, longest);
+      };
+      const int alone = fit(min(p.shares, 256)), once = fit(p.shares), twice = max(p.least, (work + 2 * p.shares - 1) / (2 * p.shares));
+      const float cost_alone = 0.8f * (float)(alone + 4) + (float)longest / (float)alone;
+      const float cost_once = (float)(once + 4) + (float)longest / (float)once;
+      const float cost_twice = 2.0f * (float)(twice + 4) + (float)longest / (float)twice;
+      const int chosen = cost_twice < fminf(cost_alone, cost_once) ? twice : cost_alone < cost_once ? alone : once;
       first = 0;
       bool found = false;
       for (int b0 = 0; b0 < p.batch && !found; b0 += 64) {
-        if (p.batch > 64) look(p, min(b0 + lane, p.batch - 1));
-        const int all = (keys + 63) / 64, about = max((all + stages - 1) / stages, 1);
-        const int mine = max((all + about - 1) / about, 1), n_shares = max((all + mine - 1) / mine, 1);
-        const int n_blocks = b0 + lane < p.batch ? (rows + ROWS - 1) / ROWS : 0;
-        const int upto = first + running(n_shares * n_blocks * p.c.heads);
+        if (p.batch > 64) measure(b0);
+        const int about = max((all + chosen - 1) / chosen, 1), mine = max((all + about - 1) / about, 1);
+        const int n_shares = max((all + mine - 1) / mine, 1);
+        const int upto = first + running(n_shares * wide);
         const unsigned long long here = __ballot(id < upto);
         found = here != 0ull;
         const int l = found ? __builtin_ctzll(here) : 63;
-        first = __builtin_amdgcn_readlane(upto - (found ? n_shares * n_blocks * p.c.heads : 0), l);
+        first = __builtin_amdgcn_readlane(upto - (found ? n_shares * wide : 0), l);
         seq = b0 + l;
         units = __builtin_amdgcn_readlane(n_shares, l) * p.c.heads;
-        blocks = __builtin_amdgcn_readlane(n_blocks, l);
+        blocks = __builtin_amdgcn_readlane(wide, l) / p.c.heads;
         piece = __builtin_amdgcn_readlane(mine, l) * 64;
       }
       if (!found) return false;
@@ -478,7 +502,7 @@ struct job {
       unit_step *= p.batch;
     }
     unit0 = unit - slice * unit_step;
-    look(p, seq);
+    look(p, seq);  // (again where the kernel dealt: broadcasting the lane's figures instead cost registers, and 64 channels 12 us of 62)
     row0 = (blocks - 1 - block) * ROWS;  // (the rows that see the most keys first)
     if (row0 >= rows) return false;
     last_row = min(row0 + ROWS, rows) - 1;
