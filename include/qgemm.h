@@ -485,7 +485,9 @@ typedef struct {
  *   QG_ROPE_LINEAR    f_i / factor (positions interpolated)
  *   QG_ROPE_BY_INDEX  f_i * (1 - w) + f_i / factor * w, w rising linearly with i
  *                     from the pair that makes `high` turns in `context` positions
- *                     to the one that makes `low`
+ *                     (rounded down) to the one that makes `low` (rounded up), both
+ *                     kept within 0 .. rot-1: the latter may lie behind the last pair,
+ *                     rot/2-1, whose w is below 1 then
  *   QG_ROPE_BY_TURNS  the same with w falling linearly with the number of turns
  *                     t_i = context * f_i / (2 pi) itself, 0 from `high` turns up
  *                     and 1 up to `low`

@@ -117,11 +117,11 @@ int qg_rope_table(const qg_rope_params* p, float* table_dev, void* stream) {
   auto pair_of = [&](double turns) { return p->rot * log(p->context / (two_pi * turns)) / (2.0 * log(p->base)); };
   const int pairs = p->rot / 2;
   double from = 0.0, to = 1.0;
-  if (p->scaling == QG_ROPE_BY_INDEX) {
+  if (p->scaling == QG_ROPE_BY_INDEX) {  // (the far end may lie behind the last pair: then no pair is interpolated in full)
     from = floor(pair_of(p->high));
     to = ceil(pair_of(p->low));
     from = from < 0.0 ? 0.0 : from;
-    to = to > pairs - 1 ? pairs - 1 : to;
+    to = to < 0.0 ? 0.0 : to > p->rot - 1 ? p->rot - 1 : to;
     if (to <= from) to = from + 0.001;
   }
   double f[128];
