@@ -80,9 +80,9 @@ __device__ inline void step(rows_of_wave<D, DIG, NR>& s, const tile_bits<D>& b, 
   }
 
   frag p[NR][PARTS];
-  float y[NR][8];
-  exponents<D, DIG, NR, MASKED>(s, z, word, t0, end, r, g, y);
-  weights<D, DIG, NR, PARTS, MASKED>(s, y, word, p);
+  float x[NR][8];
+  weigh<D, DIG, NR, MASKED>(s, z, word, t0, end, r, g, x);
+  halves<NR, PARTS>(x, p);
 
   const zero_points zp(word);
 #pragma unroll

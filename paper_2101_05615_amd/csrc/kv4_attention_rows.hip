@@ -13,6 +13,8 @@ constexpr int STAGE = 64;
 // Waves of a workgroup.  Eight share the unpacking better, but wait for each other (chunk of 512 queries, 128 channels, keys not
 // split: 291 us where four took 240); with 256 channels two workgroups of four do not fit the LDS.
 constexpr int waves_of(int D) { return D == 256 ? 8 : 4; }
+// Waves of a SIMD that have registers: as many workgroups as the LDS takes (64 channels on two: 512 queries of four sequences, 62 -> 76 us)
+constexpr int waves_per_simd(int D) { return D == 64 ? 3 : 2; }
 
 template <int D, int DIG, int NR>
 struct rows_of_wave : state<D, DIG, NR> {
@@ -112,7 +114,8 @@ __device__ inline void outputs(rows_of_wave<D, DIG, NR>& s, const stage_lds<D>& 
 }
 
 // A stage.  The second step's scores stand beside the first one's weights, and the first one's outputs beside the second one's
-// exponents, so that the matrix cores have work while the vector unit has; `between` is what the first scores cover.
+// weights, so that the matrix cores have work while the vector unit has; `between` is what the first scores cover.  (The second scores
+// behind the test that the first weights end in: 149 us where this order takes 147.)
 template <int D, int DIG, int NR, bool MASKED, typename F>
 __device__ inline void stage(rows_of_wave<D, DIG, NR>& s, const stage_lds<D>& in, const unsigned* word, int t0, int end, int lane, F between) {
   const int r = lane & 15, g = lane >> 4;
@@ -122,21 +125,21 @@ __device__ inline void stage(rows_of_wave<D, DIG, NR>& s, const stage_lds<D>& in
     if (t0 + TILE + 8 * g + (r & 7) >= end) w[1] = 0u;
   }
   f4 z[2][NR][2];
-  float y[NR][8];
+  float x[NR][8];
   frag p[NR][DIG];
   scores(s, in, 0, lane, z[0]);
   between();
-  exponents<D, DIG, NR, MASKED>(s, z[0], w[0], t0, end, r, g, y);
   scores(s, in, 1, lane, z[1]);
-  weights<D, DIG, NR, DIG, MASKED>(s, y, w[0], p);
+  weigh<D, DIG, NR, MASKED>(s, z[0], w[0], t0, end, r, g, x);
+  halves<NR, DIG>(x, p);
   outputs(s, in, 0, lane, p);
-  exponents<D, DIG, NR, MASKED>(s, z[1], w[1], t0 + TILE, end, r, g, y);
-  weights<D, DIG, NR, DIG, MASKED>(s, y, w[1], p);
+  weigh<D, DIG, NR, MASKED>(s, z[1], w[1], t0 + TILE, end, r, g, x);
+  halves<NR, DIG>(x, p);
   outputs(s, in, 1, lane, p);
 }
 
 template <int D, int DIG, int TYPE, int NR, bool SMALL>
-__global__ __launch_bounds__(64 * waves_of(D), 2) void qg_kv4_attention_rows_kernel(qg_kv4_attention_args p) {
+__global__ __launch_bounds__(64 * waves_of(D), waves_per_simd(D)) void qg_kv4_attention_rows_kernel(qg_kv4_attention_args p) {
   constexpr int WAVES = waves_of(D), ROWS = 16 * NR * WAVES;
   __shared__ stage_lds<D> lds[2];
   __shared__ int ticket;

@@ -24,10 +24,17 @@
 //
 // Rounding.  Queries become fp16 after a power of two per row that puts the largest channel near 2^14: exact for fp16 and
 // bf16 channels down to 2^-24 of the largest; fp32 queries take two fp16 (22 bits).  Probabilities times value scale become fp16
-// against a running reference for both, so that they lie below 2^14 and keep 11 bits down to 2^-14: well below the rounding of a bf16
+// against a reference of their own row, the largest such product that it has met, so that they lie below 2^12 and keep 11 bits
+// down to 2^-18 of that: well below the rounding of a bf16
 // result, and as much as that of an fp16 one where one key has all the weight, so fp16 results take two fp16 where that costs
 // little (few rows, bound by memory: 34.4 -> 36.1 us for 131072 keys of 8 heads) and fp32 results always.
 // Scores, maxima, sums and outputs are fp32.
+//
+// References.  With alpha the value scale and S a power of two that all rows of a wave share, a row holds
+//   l = sum 2^(score - m),  o = sum 2^(score - m) alpha / S (code - theta)
+// where m + log2 S is the largest score + log2 alpha of the keys that it sees: what a row does not see, or gives no weight, takes
+// nothing from its products however large its values are.  One exponential serves both sums; S only keeps 2^(score - m) within fp32
+// and near 1, where the exponent itself is rounded least (values 2^60 apart: 2^-18 of a probability, below 2^-20 within 2^12).
 #pragma once
 
 #include "qg_kv4.h"
@@ -42,8 +49,11 @@ typedef unsigned u4 __attribute__((ext_vector_type(4)));
 typedef unsigned long long u64;
 
 constexpr int TILE = 32;         // tokens of a wave's step
-constexpr float BOOST = 4.0f;    // probabilities are held times 2^BOOST ...
-constexpr float SLACK = 12.0f;   // ... and the reference moves when one would pass 2^SLACK
+constexpr int BOOST = 4;             // weights (probability times value scale) are held times 2^BOOST under their largest ...
+constexpr float MOST = 0x1p12f;      // ... and the reference moves when one would pass this
+constexpr int LAG = 16;              // a value scale may pass the common reference by 2^LAG before that moves
+constexpr float SPREAD = 80.0f;      // exponents pass the row's scores by this at most ...
+constexpr float SUMS = 0x1p96f;      // ... and their sum this
 
 template <int J>
 __device__ inline float row_lane(float x) {  // lane J of the caller's row of 16
@@ -224,10 +234,10 @@ __device__ inline unsigned key_zero(unsigned theta, int a, int r) {
 template <int D, int DIG, int NR>
 struct state {
   f4 o[NR][D / 16];
-  float m[NR], l[NR];              // reference of the exponents (log2, a whole number), sum (this lane's tokens)
+  float m[NR], l[NR];              // reference of the exponents (log2, a whole number), sum of 2^(log2 score - m) (this lane's tokens)
   float factor[NR], factor_lo[NR]; // log2 score of a product and a key's scale, in two parts (the second: DIG 2)
   int limit[NR];                   // last token that the row sees
-  int vref;                        // biased exponent of the value scales' reference, 1 .. 253
+  int vref;                        // biased exponent of the value scales' reference
   __device__ inline void start() {
     vref = 1;
 #pragma unroll
@@ -257,86 +267,105 @@ __device__ inline float exponent(float z, float factor, float factor_lo, float b
   return DIG == 2 ? __builtin_fmaf(z, factor_lo, y) : y;
 }
 
-// Products of a tile's 8 tokens (z[n][a][i]: token 8g + 4a + i) into exponents against the running references, which move rarely.
-// MASKED: tokens from `end` on are not there (`word` is 0 for them), and a row may end inside the tile.
+// Products of a tile's 8 tokens (z[n][a][i]: token 8g + 4a + i) into weights x, probability times value scale, against the running
+// references, which move rarely.  MASKED: tokens from `end` on are not there (`word` is 0 for them), and a row may end inside the tile.
 template <int D, int DIG, int NR, bool MASKED>
-__device__ inline void exponents(state<D, DIG, NR>& s, f4 (*z)[2], unsigned word, int t0, int end, int r, int g, float (*y)[8]) {
-  const int vexp = (word & 0x7f800000u) != 0x7f800000u && r >= 8 ? min((int)(word >> 23 & 255u), 253) : 0;
-  bool move = vexp > s.vref;
+__device__ inline void weigh(state<D, DIG, NR>& s, f4 (*z)[2], unsigned word, int t0, int end, int r, int g, float (*x)[8]) {
+  const float scale = __builtin_bit_cast(float, word & ~15u);
   int limit[NR];  // the last of the lane's 8 tokens that the row sees
-  if (MASKED) {
-#pragma unroll
-    for (int n = 0; n < NR; ++n) limit[n] = min(s.limit[n], end - 1) - t0 - 8 * g;
-  }
 #pragma unroll
   for (int n = 0; n < NR; ++n) {
-    const float scale = __builtin_bit_cast(float, word & ~15u);
+    limit[n] = MASKED ? min(s.limit[n], end - 1) - t0 - 8 * g : 7;
     const float ks[8] = {row_lane<0>(scale), row_lane<1>(scale), row_lane<2>(scale), row_lane<3>(scale),
                          row_lane<4>(scale), row_lane<5>(scale), row_lane<6>(scale), row_lane<7>(scale)};
-    const float base = BOOST - s.m[n];
-    float top = -__builtin_inff();
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      z[n][j >> 2][j & 3] *= ks[j];
-      y[n][j] = exponent<DIG>(z[n][j >> 2][j & 3], s.factor[n], s.factor_lo[n], base);
-      if (MASKED) y[n][j] = j > limit[n] ? -__builtin_inff() : y[n][j];
-      top = fmaxf(top, y[n][j]);
-    }
-    move |= top > SLACK;
+    for (int j = 0; j < 8; ++j) z[n][j >> 2][j & 3] *= ks[j];
   }
-  if (__builtin_expect(__ballot(move) != 0ull, 0)) {
-    int e = vexp;
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) e = max(e, __shfl_xor(e, d));
-    const int vref = max(s.vref, e);
-    const float shrink = __builtin_amdgcn_exp2f((float)(s.vref - vref));
-    s.vref = vref;
+  float sum[NR], top[NR];
+  auto all = [&]() {
+    const float scaled = __builtin_ldexpf(scale, 127 + BOOST - s.vref);
+    const float vs[8] = {row_lane<8>(scaled),  row_lane<9>(scaled),  row_lane<10>(scaled), row_lane<11>(scaled),
+                         row_lane<12>(scaled), row_lane<13>(scaled), row_lane<14>(scaled), row_lane<15>(scaled)};
 #pragma unroll
     for (int n = 0; n < NR; ++n) {
-      float high = -__builtin_inff();
+      sum[n] = 0.0f;
+      top[n] = 0.0f;
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        const float x = z[n][j >> 2][j & 3] * s.factor[n];
-        high = fmaxf(high, MASKED && j > limit[n] ? -__builtin_inff() : x);
-      }
-      const float top = fmaxf(s.m[n], rintf(across_max(high)));  // (whole: references differ by powers of two)
-      const float f = top == s.m[n] ? 1.0f : __builtin_amdgcn_exp2f(s.m[n] - top);  // (both -infinity: no key yet)
-      s.m[n] = top;
-      s.l[n] *= f;
-#pragma unroll
-      for (int i = 0; i < D / 16; ++i) s.o[n][i] *= f * shrink;
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        y[n][j] = exponent<DIG>(z[n][j >> 2][j & 3], s.factor[n], s.factor_lo[n], BOOST - top);
-        if (MASKED) y[n][j] = j > limit[n] ? -__builtin_inff() : y[n][j];
+        float y = exponent<DIG>(z[n][j >> 2][j & 3], s.factor[n], s.factor_lo[n], -s.m[n]);
+        if (MASKED) y = j > limit[n] ? -__builtin_inff() : y;
+        const float e = __builtin_amdgcn_exp2f(y);
+        sum[n] += e;
+        x[n][j] = e * vs[j];
+        if (MASKED) x[n][j] = j > limit[n] ? 0.0f : x[n][j];  // (a masked value may be NaN)
+        top[n] = fmaxf(top[n], x[n][j]);
       }
     }
-  }
-}
-
-// ... and those into the second operands of the other product: probability times value scale, in PARTS fp16 numbers
-template <int D, int DIG, int NR, int PARTS, bool MASKED>
-__device__ inline void weights(state<D, DIG, NR>& s, const float (*y)[8], unsigned word, frag (*p)[PARTS]) {
+  };
+  all();
+  bool move[NR], any = false;
 #pragma unroll
   for (int n = 0; n < NR; ++n) {
-    const float scale = __builtin_bit_cast(float, word & ~15u) * __builtin_bit_cast(float, (unsigned)(254 - s.vref) << 23);
-    const float vs[8] = {row_lane<8>(scale),  row_lane<9>(scale),  row_lane<10>(scale), row_lane<11>(scale),
-                         row_lane<12>(scale), row_lane<13>(scale), row_lane<14>(scale), row_lane<15>(scale)};
+    move[n] = top[n] > MOST || s.l[n] + sum[n] > SUMS;
+    any |= move[n];
+  }
+  if (__builtin_expect(__ballot(any) != 0ull, 0)) {
+    const int e = (word & 0x7f800000u) != 0x7f800000u && r >= 8 ? (int)(word >> 23 & 255u) : 0;  // (zero and NaN: 0)
+    int most = e;
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) most = max(most, __shfl_xor(most, d));
+    const int vref = most > s.vref + LAG ? most : s.vref;
+    const float ve = e > 0 ? (float)e : -__builtin_inff();
+    const float ves[8] = {row_lane<8>(ve),  row_lane<9>(ve),  row_lane<10>(ve), row_lane<11>(ve),
+                          row_lane<12>(ve), row_lane<13>(ve), row_lane<14>(ve), row_lane<15>(ve)};
+#pragma unroll
+    for (int n = 0; n < NR; ++n) {
+      float score = -__builtin_inff(), weight = -__builtin_inff();
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        float y = z[n][j >> 2][j & 3] * s.factor[n];
+        if (MASKED) y = j > limit[n] ? -__builtin_inff() : y;
+        score = fmaxf(score, y);
+        weight = fmaxf(weight, y + ves[j]);
+      }
+      u64 rows = __ballot(move[n]);  // (a row's four lanes move together, and no other row moves with it)
+      rows |= rows >> 32;
+      rows |= rows >> 16;
+      weight = rintf(across_max(weight)) - (float)vref;  // (whole: references differ by powers of two)
+      float m = s.m[n] + (float)(s.vref - vref);
+      if (rows >> r & 1) m = fmaxf(m, weight);
+      const int held = __builtin_amdgcn_frexp_expf(across_sum(s.l[n]));
+      m = fmaxf(m, fmaxf(rintf(across_max(score)) - SPREAD, s.m[n] + (float)held - SPREAD));
+      const float by = m == s.m[n] ? 0.0f : fminf(fmaxf(s.m[n] - m, -300.0f), 300.0f);  // (both -infinity: no key yet)
+      s.m[n] = m;
+      s.l[n] = __builtin_ldexpf(s.l[n], (int)by);
+      const float f = __builtin_ldexpf(1.0f, (int)by + s.vref - vref);
+#pragma unroll
+      for (int i = 0; i < D / 16; ++i) s.o[n][i] *= f;
+    }
+    s.vref = vref;
+    all();
+  }
+#pragma unroll
+  for (int n = 0; n < NR; ++n) s.l[n] += sum[n];
+}
+
+// ... and those as second operands of the other product, in PARTS fp16 numbers
+template <int NR, int PARTS>
+__device__ inline void halves(const float (*x)[8], frag (*p)[PARTS]) {
+#pragma unroll
+  for (int n = 0; n < NR; ++n)
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      const float e = __builtin_amdgcn_exp2f(y[n][j]);
-      s.l[n] += e;
-      float x = e * vs[j];
-      if (MASKED) x = y[n][j] == -__builtin_inff() ? 0.0f : x;  // (a masked value may be NaN)
+      float w = x[n][j];
       // The product as 32 bits: left to itself the compiler rounds it to fp16 twice, once from the exact product and once from
       // this one, and where the two differ the second part makes up for the wrong first part (one token in some thousands; an
       // fp32 result then loses half its digits).
-      if (PARTS == 2) asm("" : "+v"(x));
-      const _Float16 hi = (_Float16)x;
+      if (PARTS == 2) asm("" : "+v"(w));
+      const _Float16 hi = (_Float16)w;
       p[n][0].v[j] = hi;
-      if (PARTS == 2) p[n][PARTS - 1].v[j] = (_Float16)(x - (float)hi);
+      if (PARTS == 2) p[n][PARTS - 1].v[j] = (_Float16)(w - (float)hi);
     }
-  }
 }
 
 // The channels of a query that a lane needs, as they lie in memory
@@ -535,18 +564,21 @@ struct job {
 };
 
 // A wave's rows divided by their sums, and those: what a part of the keys weighs is sum 2^m, kept as the two numbers (a logarithm of
-// a large sum would lose what an fp32 result shows).  No key: sum 0, m -infinity.
+// a large sum would lose what an fp32 result shows), the sum below 1 where m is small enough to take up its exponent exactly, so that
+// parts compare by m.  No key: sum 0, m -infinity.
 template <int D, int DIG, int NR>
 __device__ inline void finish(state<D, DIG, NR>& s, float* sum) {
 #pragma unroll
   for (int n = 0; n < NR; ++n) {
     const float l = across_sum(s.l[n]);
-    sum[n] = l;
+    const int e = __builtin_fabsf(s.m[n]) < 0x1p22f ? __builtin_amdgcn_frexp_expf(l) : 0;
+    sum[n] = __builtin_ldexpf(l, -e);
+    s.m[n] += (float)e;
     const float inv = l == 0.0f ? 0.0f : 1.0f / l;
 #pragma unroll
     for (int c = 0; c < D / 16; ++c)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) s.o[n][c][e] = __builtin_ldexpf(s.o[n][c][e] * inv, s.vref - 127);
+      for (int i = 0; i < 4; ++i) s.o[n][c][i] = __builtin_ldexpf(s.o[n][c][i] * inv, s.vref - 127 - BOOST);
   }
 }
 // Weights relative to the largest reference `top` among the parts
