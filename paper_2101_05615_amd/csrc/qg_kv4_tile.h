@@ -35,6 +35,9 @@
 // where m + log2 S is the largest score + log2 alpha of the keys that it sees: what a row does not see, or gives no weight, takes
 // nothing from its products however large its values are.  One exponential serves both sums; S only keeps 2^(score - m) within fp32
 // and near 1, where the exponent itself is rounded least (values 2^60 apart: 2^-18 of a probability, below 2^-20 within 2^12).
+// Scores from 2^24 on are whole numbers in fp32, up to 32 apart: a reference cannot take up the value scale there and is the largest
+// score, S the largest value scale, and the exponent the difference of the rounded scores.  (The exact one, up to 16 on either side
+// of 0 for the largest score itself, passes fp16's range.)  Every tile is then weighed twice.
 #pragma once
 
 #include "qg_kv4.h"
@@ -54,6 +57,7 @@ constexpr float MOST = 0x1p12f;      // ... and the reference moves when one wou
 constexpr int LAG = 16;              // a value scale may pass the common reference by 2^LAG before that moves
 constexpr float SPREAD = 80.0f;      // exponents pass the row's scores by this at most ...
 constexpr float SUMS = 0x1p96f;      // ... and their sum this
+constexpr float FINE = 0x1p24f;      // fp32 numbers below this take up whole ones
 
 template <int J>
 __device__ inline float row_lane(float x) {  // lane J of the caller's row of 16
@@ -238,8 +242,10 @@ struct state {
   float factor[NR], factor_lo[NR]; // log2 score of a product and a key's scale, in two parts (the second: DIG 2)
   int limit[NR];                   // last token that the row sees
   int vref;                        // biased exponent of the value scales' reference
+  bool huge;                       // some score was beyond FINE
   __device__ inline void start() {
     vref = 1;
+    huge = false;
 #pragma unroll
     for (int n = 0; n < NR; ++n) {
       m[n] = -__builtin_inff();  // (before the first key every exponent is +infinity, and the reference moves)
@@ -250,13 +256,29 @@ struct state {
   }
 };
 
-__device__ inline float across_max(float x) {  // over the four lanes of a row of queries
-  x = fmaxf(x, __shfl_xor(x, 16));
-  return fmaxf(x, __shfl_xor(x, 32));
+// Over the four lanes of a row of queries: every lane gets the result, by swaps between the rows of 16 (no trip through the LDS)
+template <typename F>
+__device__ inline float across(float x, F f) {
+  const auto a = __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(unsigned, x), __builtin_bit_cast(unsigned, x), false, false);
+  const unsigned a0 = a[0], a1 = a[1];
+  x = f(__builtin_bit_cast(float, a0), __builtin_bit_cast(float, a1));
+  const auto b = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(unsigned, x), __builtin_bit_cast(unsigned, x), false, false);
+  const unsigned b0 = b[0], b1 = b[1];
+  return f(__builtin_bit_cast(float, b0), __builtin_bit_cast(float, b1));
+}
+__device__ inline float across_max(float x) {
+  return across(x, [](float a, float b) { return fmaxf(a, b); });
 }
 __device__ inline float across_sum(float x) {
-  x += __shfl_xor(x, 16);
-  return x + __shfl_xor(x, 32);
+  return across(x, [](float a, float b) { return a + b; });
+}
+// The largest over all lanes
+__device__ inline float wave_max(float x) {
+  x = fmaxf(x, __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, x), 0x128, 0xf, 0xf, true)));  // row_ror:8, 4, 2, 1
+  x = fmaxf(x, __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, x), 0x124, 0xf, 0xf, true)));
+  x = fmaxf(x, __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, x), 0x122, 0xf, 0xf, true)));
+  x = fmaxf(x, __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, x), 0x121, 0xf, 0xf, true)));
+  return across_max(x);
 }
 
 // z factor + base, where base is a whole number near -z factor: the sum is small and loses nothing of it.  DIG 2: the factor's own
@@ -282,7 +304,7 @@ __device__ inline void weigh(state<D, DIG, NR>& s, f4 (*z)[2], unsigned word, in
     for (int j = 0; j < 8; ++j) z[n][j >> 2][j & 3] *= ks[j];
   }
   float sum[NR], top[NR];
-  auto all = [&]() {
+  auto all = [&](const float* factor, const float* factor_lo) {
     const float scaled = __builtin_ldexpf(scale, 127 + BOOST - s.vref);
     const float vs[8] = {row_lane<8>(scaled),  row_lane<9>(scaled),  row_lane<10>(scaled), row_lane<11>(scaled),
                          row_lane<12>(scaled), row_lane<13>(scaled), row_lane<14>(scaled), row_lane<15>(scaled)};
@@ -292,7 +314,7 @@ __device__ inline void weigh(state<D, DIG, NR>& s, f4 (*z)[2], unsigned word, in
       top[n] = 0.0f;
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        float y = exponent<DIG>(z[n][j >> 2][j & 3], s.factor[n], s.factor_lo[n], -s.m[n]);
+        float y = exponent<DIG>(z[n][j >> 2][j & 3], factor[n], factor_lo[n], -s.m[n]);
         if (MASKED) y = j > limit[n] ? -__builtin_inff() : y;
         const float e = __builtin_amdgcn_exp2f(y);
         sum[n] += e;
@@ -302,19 +324,35 @@ __device__ inline void weigh(state<D, DIG, NR>& s, f4 (*z)[2], unsigned word, in
       }
     }
   };
-  all();
+  all(s.factor, s.factor_lo);
   bool move[NR], any = false;
 #pragma unroll
   for (int n = 0; n < NR; ++n) {
-    move[n] = top[n] > MOST || s.l[n] + sum[n] > SUMS;
+    move[n] = top[n] > MOST || s.l[n] + sum[n] > SUMS || s.huge;
     any |= move[n];
   }
   if (__builtin_expect(__ballot(any) != 0ull, 0)) {
-    const int e = (word & 0x7f800000u) != 0x7f800000u && r >= 8 ? (int)(word >> 23 & 255u) : 0;  // (zero and NaN: 0)
-    int most = e;
+    float far = 0.0f;
 #pragma unroll
-    for (int d = 1; d < 64; d *= 2) most = max(most, __shfl_xor(most, d));
-    const int vref = most > s.vref + LAG ? most : s.vref;
+    for (int n = 0; n < NR; ++n) {
+      float most = 0.0f;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) most = fmaxf(most, __builtin_fabsf(z[n][j >> 2][j & 3]));
+      far = fmaxf(far, most * __builtin_fabsf(s.factor[n]));
+    }
+    const bool huge = s.huge || __ballot(far >= FINE) != 0ull;
+    s.huge = huge;
+    float factor[NR], factor_lo[NR];
+#pragma unroll
+    for (int n = 0; n < NR; ++n) {
+      const float now = huge ? s.factor[n] : 1.0f;  // (then z becomes the rounded score itself)
+      factor[n] = huge ? 1.0f : s.factor[n];
+      factor_lo[n] = huge ? 0.0f : s.factor_lo[n];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) z[n][j >> 2][j & 3] *= now;
+    }
+    const int e = (word & 0x7f800000u) != 0x7f800000u && r >= 8 ? (int)(word >> 23 & 255u) : 0;  // (zero and NaN: 0)
+    const int most = (int)wave_max((float)e), vref = most > s.vref + (huge ? 0 : LAG) ? most : s.vref;
     const float ve = e > 0 ? (float)e : -__builtin_inff();
     const float ves[8] = {row_lane<8>(ve),  row_lane<9>(ve),  row_lane<10>(ve), row_lane<11>(ve),
                           row_lane<12>(ve), row_lane<13>(ve), row_lane<14>(ve), row_lane<15>(ve)};
@@ -323,19 +361,23 @@ __device__ inline void weigh(state<D, DIG, NR>& s, f4 (*z)[2], unsigned word, in
       float score = -__builtin_inff(), weight = -__builtin_inff();
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        float y = z[n][j >> 2][j & 3] * s.factor[n];
-        if (MASKED) y = j > limit[n] ? -__builtin_inff() : y;
-        score = fmaxf(score, y);
-        weight = fmaxf(weight, y + ves[j]);
+        const float y = z[n][j >> 2][j & 3] * factor[n];
+        if (!MASKED || j <= limit[n]) {
+          score = fmaxf(score, y);
+          weight = fmaxf(weight, y + ves[j]);
+        }
       }
+      score = rintf(across_max(score));  // (whole: references differ by powers of two)
+      weight = rintf(across_max(weight)) - (float)vref;
       u64 rows = __ballot(move[n]);  // (a row's four lanes move together, and no other row moves with it)
       rows |= rows >> 32;
       rows |= rows >> 16;
-      weight = rintf(across_max(weight)) - (float)vref;  // (whole: references differ by powers of two)
-      float m = s.m[n] + (float)(s.vref - vref);
-      if (rows >> r & 1) m = fmaxf(m, weight);
       const int held = __builtin_amdgcn_frexp_expf(across_sum(s.l[n]));
-      m = fmaxf(m, fmaxf(rintf(across_max(score)) - SPREAD, s.m[n] + (float)held - SPREAD));
+      float m = s.m[n] + (float)(s.vref - vref);
+      if (huge || (rows >> r & 1)) m = fmaxf(m, weight);
+      m = fmaxf(m, fmaxf(score, s.m[n] + (float)held) - SPREAD);
+      score = fmaxf(score, s.m[n]);
+      if (__builtin_fabsf(score) >= FINE) m = score;
       const float by = m == s.m[n] ? 0.0f : fminf(fmaxf(s.m[n] - m, -300.0f), 300.0f);  // (both -infinity: no key yet)
       s.m[n] = m;
       s.l[n] = __builtin_ldexpf(s.l[n], (int)by);
@@ -344,7 +386,7 @@ __device__ inline void weigh(state<D, DIG, NR>& s, f4 (*z)[2], unsigned word, in
       for (int i = 0; i < D / 16; ++i) s.o[n][i] *= f;
     }
     s.vref = vref;
-    all();
+    all(factor, factor_lo);
   }
 #pragma unroll
   for (int n = 0; n < NR; ++n) s.l[n] += sum[n];
@@ -571,7 +613,7 @@ __device__ inline void finish(state<D, DIG, NR>& s, float* sum) {
 #pragma unroll
   for (int n = 0; n < NR; ++n) {
     const float l = across_sum(s.l[n]);
-    const int e = __builtin_fabsf(s.m[n]) < 0x1p22f ? __builtin_amdgcn_frexp_expf(l) : 0;
+    const int e = __builtin_fabsf(s.m[n]) < 0.5f * FINE ? __builtin_amdgcn_frexp_expf(l) : 0;
     sum[n] = __builtin_ldexpf(l, -e);
     s.m[n] += (float)e;
     const float inv = l == 0.0f ? 0.0f : 1.0f / l;
