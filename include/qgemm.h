@@ -581,7 +581,8 @@ int qg_kv4_read(const qg_kv4_cache* c, const int64_t* slots, int tokens, int dty
  * stored).  Query head h reads KV head h / (q_heads / kv_heads).  A query with no
  * key to see gives 0.  Scores may be up to 2^28 in size.  Sums and softmax statistics are fp32; the codes enter the
  * matrix cores exactly, queries as fp16 numbers scaled by row (two per channel for
- * QG_F32), probabilities times value scale as fp16 (two for QG_F32) relative to the
+ * QG_F32), probabilities times value scale as fp16 (one number for QG_BF16, two for
+ * QG_F16 and QG_F32, however many rows there are) relative to the
  * largest such product of the row, of which each key may lose 2^-28; keys that a row
  * does not see, or gives no weight, take nothing from it while scores are below 2^24
  * and their value scales less than 2^80 times those of the keys that carry it.

@@ -101,22 +101,22 @@ __device__ inline void scores(const rows_of_wave<D, DIG, NR>& s, const stage_lds
     }
   }
 }
-template <int D, int DIG, int NR>
-__device__ inline void outputs(rows_of_wave<D, DIG, NR>& s, const stage_lds<D>& in, int which, int lane, const frag (*p)[DIG]) {
+template <int D, int DIG, int NR, int PARTS>
+__device__ inline void outputs(rows_of_wave<D, DIG, NR>& s, const stage_lds<D>& in, int which, int lane, const frag (*p)[PARTS]) {
 #pragma unroll
   for (int c = 0; c < D / 16; ++c) {
     const frag v = in.values[which][c][lane];
 #pragma unroll
     for (int n = 0; n < NR; ++n)
 #pragma unroll
-      for (int d = 0; d < DIG; ++d) s.o[n][c] = product(v, p[n][d], s.o[n][c]);
+      for (int d = 0; d < PARTS; ++d) s.o[n][c] = product(v, p[n][d], s.o[n][c]);
   }
 }
 
 // A stage.  The second step's scores stand beside the first one's weights, and the first one's outputs beside the second one's
 // weights, so that the matrix cores have work while the vector unit has; `between` is what the first scores cover.  (The second scores
 // behind the test that the first weights end in: 149 us where this order takes 147.)
-template <int D, int DIG, int NR, bool MASKED, typename F>
+template <int D, int DIG, int NR, int PARTS, bool MASKED, typename F>
 __device__ inline void stage(rows_of_wave<D, DIG, NR>& s, const stage_lds<D>& in, const unsigned* word, int t0, int end, int lane, F between) {
   const int r = lane & 15, g = lane >> 4;
   unsigned w[2] = {word[0], word[1]};
@@ -126,21 +126,21 @@ __device__ inline void stage(rows_of_wave<D, DIG, NR>& s, const stage_lds<D>& in
   }
   f4 z[2][NR][2];
   float x[NR][8];
-  frag p[NR][DIG];
+  frag p[NR][PARTS];
   scores(s, in, 0, lane, z[0]);
   between();
   scores(s, in, 1, lane, z[1]);
   weigh<D, DIG, NR, MASKED>(s, z[0], w[0], t0, end, r, g, x);
-  halves<NR, DIG>(x, p);
+  halves<NR, PARTS>(x, p);
   outputs(s, in, 0, lane, p);
   weigh<D, DIG, NR, MASKED>(s, z[1], w[1], t0 + TILE, end, r, g, x);
-  halves<NR, DIG>(x, p);
+  halves<NR, PARTS>(x, p);
   outputs(s, in, 1, lane, p);
 }
 
 template <int D, int DIG, int TYPE, int NR, bool SMALL>
 __global__ __launch_bounds__(64 * waves_of(D), waves_per_simd(D)) void qg_kv4_attention_rows_kernel(qg_kv4_attention_args p) {
-  constexpr int WAVES = waves_of(D), ROWS = 16 * NR * WAVES;
+  constexpr int WAVES = waves_of(D), ROWS = 16 * NR * WAVES, PARTS = TYPE == QG_BF16 ? 1 : 2;
   __shared__ stage_lds<D> lds[2];
   __shared__ int ticket;
   const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
@@ -197,14 +197,14 @@ __global__ __launch_bounds__(64 * waves_of(D), waves_per_simd(D)) void qg_kv4_at
     };
     for (; t0 + STAGE <= whole; t0 += STAGE) {
       const unsigned now[2] = {word[0], word[1]};
-      stage<D, DIG, NR, false>(s, lds[which], now, t0, j.hi, lane, prepare);
+      stage<D, DIG, NR, PARTS, false>(s, lds[which], now, t0, j.hi, lane, prepare);
       which ^= 1;
       __syncthreads();
     }
     for (; t0 < j.hi; t0 += STAGE) {
       const unsigned now[2] = {word[0], word[1]};
       if (t0 < mine)
-        stage<D, DIG, NR, true>(s, lds[which], now, t0, j.hi, lane, prepare);
+        stage<D, DIG, NR, PARTS, true>(s, lds[which], now, t0, j.hi, lane, prepare);
       else
         prepare();
       which ^= 1;
