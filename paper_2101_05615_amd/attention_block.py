@@ -50,7 +50,7 @@ class AttentionBlock:
     def workspace(self, batch, max_q_len, max_kv_len):
         return kv4.attention_workspace(self.cache, self.heads, batch, max_q_len=max_q_len, max_kv_len=max_kv_len)
 
-    def __call__(self, x, positions, slots, pages, kv_lens, q_starts=None, max_q_len=1, max_kv_len=None, workspace=None):
+    def __call__(self, x, positions, slots, pages, kv_lens, q_starts=None, max_q_len=None, max_kv_len=None, workspace=None):
         """x [tokens, hidden] of new tokens, their positions and cache slots; the rest as kv4.attention (kv_lens counts the new ones)."""
         qh, kh, vh = self.project_in(x)
         kv4.append(self.cache, kh, vh, slots, positions=positions, table=self.table, q=qh, q_out=qh)

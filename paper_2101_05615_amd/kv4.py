@@ -200,11 +200,14 @@ def attention_workspace(cache, q_heads, batch, max_q_len=1, max_kv_len=0):
     return ws
 
 
-def attention(q, cache, pages, kv_lens, q_starts=None, max_q_len=1, max_kv_len=None, scale=None, causal=True, workspace=None, out=None):
+def attention(q, cache, pages, kv_lens, q_starts=None, max_q_len=None, max_kv_len=None, scale=None, causal=True, workspace=None, out=None):
     """softmax(scale q k) v over the cached tokens of every sequence: q [tokens, heads, head_dim]; pages int32 [batch, n] names the
     pages of a sequence in order; kv_lens int32 [batch] its tokens.  q_starts int32 [batch + 1]: the rows of q that belong to a
     sequence, its last tokens (causal: query i of n sees the keys up to kv_len - n + i); None: one row each.  max_q_len,
-    max_kv_len: the most of any sequence (default for the latter: what the page table holds).  scale: 1 / sqrt(head_dim)."""
+    max_kv_len: the most of any sequence (default: the rows of q, or one without q_starts; what the page table holds), near bounds are
+    faster.  Rows of q that no sequence has are not written: in a new result they hold anything.  scale: 1 / sqrt(head_dim)."""
+    if max_q_len is None:
+        max_q_len = 1 if q_starts is None else q.shape[0]
     done = _binding.kv4_attention(cache, q, pages, kv_lens, q_starts, max_q_len, max_kv_len, scale, causal, workspace, out)
     if done is not None:
         return done
