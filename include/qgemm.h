@@ -596,12 +596,14 @@ int qg_kv4_read(const qg_kv4_cache* c, const int64_t* slots, int tokens, int dty
  *             one query each.
  *   max_q_len, max_kv_len  the most that any sequence has, <= pages_stride * page_tokens
  *             for the latter (the grid is sized by them: near bounds are faster)
- *   workspace dev, 16-byte aligned, qg_kv4_attention_workspace_bytes() bytes for the same extents,
+ *   workspace dev, 16-byte aligned, qg_kv4_attention_workspace_bytes() bytes for the same
+ *             extents, its first QG_KV4_COUNTER_BYTES
  *             zeroed once by qg_gemm_workspace_init before its first use; every call leaves
  *             it ready for the next one on the stream.  Calls that may overlap in time need one
  *             each.  NULL is allowed: the keys of a sequence are then never split over
  *             workgroups, which long sequences in small batches need.
  * The result of a call is the same every time it is made. */
+#define QG_KV4_COUNTER_BYTES 65536
 typedef struct {
   qg_heads q, out;        /* [tokens][q_heads][head_dim]                      */
   const int32_t* pages;

@@ -58,19 +58,26 @@ int check_rotation(const float* table, int max_pos, int rot, int interleaved, in
 //   1981, 1766 and 1310 keys, 32 heads over 8 of 128 channels: 150 us (equal shares 164, whole 240); four of 4096 keys: 171, as whole
 //   (two rounds 200); one of 8192, 8 heads over one: 56 (in as many shares as run at once 64).
 constexpr int FEW_SHARES = 256;
-constexpr size_t COUNTERS = 16384;  // a fixed part of every workspace, so that calls of other extents find it zero
+constexpr size_t COUNTERS = QG_KV4_COUNTER_BYTES / 4;  // a fixed part of every workspace, so that calls of other extents find it zero
+constexpr int LEAST_FEW = 256, LEAST_MANY = 512;       // tokens of a share; up to twice that keys are not split
 
 struct share {
   int split, piece, shares, least;
   long long rows;  // of results in the workspace; 0: keys not split
 };
 
+int at_once_of(int head_dim) { return head_dim == 64 ? 768 : head_dim == 128 ? 512 : 256; }
+
+// Workgroups that the kernel deals keys to at most, for so many (sequence, head, block of rows): what two rounds take and one more for
+// each, and no more than shares of the least length make
+long long dealt_most(long long units, int at_once, int max_kv_len) { return qg_kv4_dealt(units, at_once, max_kv_len, LEAST_MANY / 64); }
+
 share share_of(const qg_kv4_cache* c, int q_heads, int batch, int max_q_len, int max_kv_len) {
   const long long rows = (long long)max_q_len * (q_heads / c->kv_heads), per = qg_kv4_rows_per_workgroup(c->head_dim, rows);
   const long long heads = (long long)batch * c->kv_heads, blocks = (rows + per - 1) / per;
   const long long most = heads * ((rows + 15) / 16);  // workgroups have 16 rows at least
   const bool few = rows <= QG_KV4_FEW;
-  const int least = few ? 256 : 512;
+  const int least = few ? LEAST_FEW : LEAST_MANY;
   share s = {1, 0x40000000, 0, 0, 0};
   if (max_kv_len <= 2 * least) return s;
   if (few) {
@@ -80,17 +87,17 @@ share share_of(const qg_kv4_cache* c, int q_heads, int batch, int max_q_len, int
     s.split = (max_kv_len + s.piece - 1) / s.piece;
     s.rows = heads * blocks * s.split * per;
   } else {
-    const int at_once = c->head_dim == 64 ? 768 : c->head_dim == 128 ? 512 : 256;
+    const int at_once = at_once_of(c->head_dim);
     // (more than two rounds even out by themselves; the kernel adds up workgroups, and the stages of all, in 32 bits)
     if (heads * blocks > 2 * at_once || most + 16 > (long long)COUNTERS || most * ((max_kv_len + 63) / 64) > 0x7fff0000ll) return s;
     s.shares = at_once;
     s.least = least / 64;
-    s.rows = 4ll * at_once * per;  // 2 at_once and one more per (sequence, head, block of rows); with blocks of 64 rows, 6 at_once of 64
+    s.rows = dealt_most(heads * blocks, at_once, max_kv_len) * per;  // (blocks of 64 rows: at most twice the heads * blocks, half the rows each)
   }
   return s;
 }
 
-size_t share_bytes(const share& s, int head_dim) { return s.rows == 0 ? 0 : COUNTERS * 4 + (size_t)s.rows * (head_dim + 2) * 4; }
+size_t share_bytes(long long rows, int head_dim) { return rows == 0 ? 0 : COUNTERS * 4 + (size_t)rows * (head_dim + 2) * 4; }
 
 bool extents_ok(const qg_kv4_cache* c, int q_heads, int batch, int max_q_len, int max_kv_len) {
   if (q_heads < 1 || q_heads % c->kv_heads != 0 || batch < 0 || max_q_len < 0 || max_kv_len < 0) return false;
@@ -248,7 +255,7 @@ int qg_kv4_read(const qg_kv4_cache* c, const int64_t* slots, int tokens, int dty
 size_t qg_kv4_attention_workspace_bytes(const qg_kv4_cache* c, int q_heads, int batch, int max_q_len, int max_kv_len) {
   if (!c || qg_kv4_bytes(c->n_pages, c->kv_heads, c->head_dim, c->page_tokens) == 0) return 0;
   if (!extents_ok(c, q_heads, batch, max_q_len, max_kv_len) || batch == 0 || max_q_len == 0 || max_kv_len == 0) return 0;
-  return share_bytes(share_of(c, q_heads, batch, max_q_len, max_kv_len), c->head_dim);
+  return share_bytes(share_of(c, q_heads, batch, max_q_len, max_kv_len).rows, c->head_dim);
 }
 
 int qg_kv4_attention(const qg_kv4_cache* c, const qg_kv4_attention_params* p, void* stream) {
@@ -268,7 +275,7 @@ int qg_kv4_attention(const qg_kv4_cache* c, const qg_kv4_attention_params* p, vo
   share s = share_of(c, p->q_heads, p->batch, max_q, p->max_kv_len);
   if (!p->workspace) s = {1, 0x40000000, 0, 0, 0};
   if (s.rows > 0) {
-    if (p->workspace_bytes < share_bytes(s, c->head_dim)) return QG_EWORKSPACE;
+    if (p->workspace_bytes < share_bytes(s.rows, c->head_dim)) return QG_EWORKSPACE;
     if (!aligned(p->workspace, 16)) return QG_EALIGN;
   }
   const long long rows = (long long)max_q * (p->q_heads / c->kv_heads);

@@ -241,7 +241,8 @@ template <int D, int TYPE>
 void go(qg_kv4_attention_args a, int rows, hipStream_t s) {
   constexpr int DIG = TYPE == QG_F32 ? 2 : 1, NR = D == 256 || DIG == 2 ? 1 : 2, WAVES = waves_of(D), ROWS = 16 * NR * WAVES;
   a.row_blocks = (rows + ROWS - 1) / ROWS;
-  const dim3 grid((unsigned)(2 * a.shares + a.batch * a.c.heads * a.row_blocks));  // (a sequence has one more share than it fills at most)
+  const long long units = (long long)a.batch * a.c.heads * a.row_blocks;
+  const dim3 grid((unsigned)(a.shares == 0 ? units : qg_kv4_dealt(units, a.shares, a.max_kv_len, a.least)));
   if (a.c.lgp == 4)
     hipLaunchKernelGGL((qg_kv4_attention_rows_kernel<D, DIG, TYPE, NR, true>), grid, dim3(64 * WAVES), 0, s, a);
   else

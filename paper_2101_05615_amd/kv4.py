@@ -17,6 +17,7 @@ import torch
 from .qgemm import QGemmError, _binding, _check, _stream, lib
 
 F32, BF16, F16 = 0, 1, 2
+COUNTER_BYTES = 65536   # QG_KV4_COUNTER_BYTES
 _TYPES = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}
 ROPE_PLAIN, ROPE_LINEAR, ROPE_BY_INDEX, ROPE_BY_TURNS = 0, 1, 2, 3
 _SCALINGS = {"plain": ROPE_PLAIN, "linear": ROPE_LINEAR, "by_index": ROPE_BY_INDEX, "by_turns": ROPE_BY_TURNS}
@@ -196,7 +197,7 @@ def attention_workspace(cache, q_heads, batch, max_q_len=1, max_kv_len=0):
     if n == 0:
         return None
     ws = torch.empty(n, dtype=torch.uint8, device=cache.data.device)
-    _check(lib.qg_gemm_workspace_init(ws.data_ptr(), n, _stream()), "qg_gemm_workspace_init")
+    _check(lib.qg_gemm_workspace_init(ws.data_ptr(), min(n, COUNTER_BYTES), _stream()), "qg_gemm_workspace_init")
     return ws
 
 
