@@ -596,8 +596,8 @@ int qg_kv4_read(const qg_kv4_cache* c, const int64_t* slots, int tokens, int dty
  *             one query each.
  *   max_q_len, max_kv_len  the most that any sequence has, <= pages_stride * page_tokens
  *             for the latter (the grid is sized by them: near bounds are faster)
- *   workspace dev, 16-byte aligned, qg_kv4_attention_workspace_bytes() bytes for the same
- *             extents, its first QG_KV4_COUNTER_BYTES
+ *   workspace dev, 16-byte aligned, qg_kv4_attention_workspace_bytes() bytes for these extents
+ *             or larger ones of the same cache and q_heads, its first QG_KV4_COUNTER_BYTES
  *             zeroed once by qg_gemm_workspace_init before its first use; every call leaves
  *             it ready for the next one on the stream.  Calls that may overlap in time need one
  *             each.  NULL is allowed: the keys of a sequence are then never split over
@@ -614,6 +614,7 @@ typedef struct {
   float scale;            /* finite                                           */
   int32_t dtype, tokens, q_heads, batch, pages_stride, max_q_len, max_kv_len, causal;
 } qg_kv4_attention_params;
+/* What calls with at most these extents want; 0: none of them splits keys. */
 size_t qg_kv4_attention_workspace_bytes(const qg_kv4_cache* c, int q_heads, int batch, int max_q_len,
                                         int max_kv_len);
 int qg_kv4_attention(const qg_kv4_cache* c, const qg_kv4_attention_params* p, void* stream);

@@ -97,6 +97,29 @@ share share_of(const qg_kv4_cache* c, int q_heads, int batch, int max_q_len, int
   return s;
 }
 
+// Rows of results that calls with at most these extents may want.  More sequences, queries or keys can mean fewer shares, so this
+// is no call's own figure: few rows, `split` is at most FEW_SHARES / units + 1 and at most the keys' number of least pieces, and units
+// number less than FEW_SHARES; many rows as in share_of.
+long long most_rows_of(const qg_kv4_cache* c, int q_heads, int batch, int max_q_len, int max_kv_len) {
+  const long long rows = (long long)max_q_len * (q_heads / c->kv_heads), heads = (long long)batch * c->kv_heads;
+  long long most = 0;
+  if (max_kv_len > 2 * LEAST_FEW) {
+    const long long some = rows < QG_KV4_FEW ? rows : QG_KV4_FEW, per = qg_kv4_rows_per_workgroup(c->head_dim, some);
+    long long units = heads * ((some + per - 1) / per);
+    if (units >= FEW_SHARES) units = FEW_SHARES - 1;
+    const long long pieces = units * ((max_kv_len + LEAST_FEW - 1) / LEAST_FEW);
+    most = (pieces < FEW_SHARES + units ? pieces : FEW_SHARES + units) * per;
+  }
+  if (rows > QG_KV4_FEW && max_kv_len > 2 * LEAST_MANY) {
+    const long long per = qg_kv4_rows_per_workgroup(c->head_dim, rows), at_once = at_once_of(c->head_dim);
+    long long units = heads * ((rows + per - 1) / per);
+    if (units > 2 * at_once) units = 2 * at_once;
+    const long long here = dealt_most(units, (int)at_once, max_kv_len) * per;
+    if (here > most) most = here;
+  }
+  return most;
+}
+
 size_t share_bytes(long long rows, int head_dim) { return rows == 0 ? 0 : COUNTERS * 4 + (size_t)rows * (head_dim + 2) * 4; }
 
 bool extents_ok(const qg_kv4_cache* c, int q_heads, int batch, int max_q_len, int max_kv_len) {
@@ -255,7 +278,7 @@ int qg_kv4_read(const qg_kv4_cache* c, const int64_t* slots, int tokens, int dty
 size_t qg_kv4_attention_workspace_bytes(const qg_kv4_cache* c, int q_heads, int batch, int max_q_len, int max_kv_len) {
   if (!c || qg_kv4_bytes(c->n_pages, c->kv_heads, c->head_dim, c->page_tokens) == 0) return 0;
   if (!extents_ok(c, q_heads, batch, max_q_len, max_kv_len) || batch == 0 || max_q_len == 0 || max_kv_len == 0) return 0;
-  return share_bytes(share_of(c, q_heads, batch, max_q_len, max_kv_len).rows, c->head_dim);
+  return share_bytes(most_rows_of(c, q_heads, batch, max_q_len, max_kv_len), c->head_dim);
 }
 
 int qg_kv4_attention(const qg_kv4_cache* c, const qg_kv4_attention_params* p, void* stream) {

@@ -192,7 +192,7 @@ def attention_workspace_bytes(cache, q_heads, batch, max_q_len=1, max_kv_len=0):
 
 
 def attention_workspace(cache, q_heads, batch, max_q_len=1, max_kv_len=0):
-    """A workspace for attention() with these extents (None where it needs none); one per stream that calls run on."""
+    """A workspace for attention() with at most these extents (None where it needs none); one per stream that calls run on."""
     n = attention_workspace_bytes(cache, q_heads, batch, max_q_len, max_kv_len)
     if n == 0:
         return None
