@@ -18,6 +18,7 @@ from .qgemm import QGemmError, _binding, _check, _stream, lib
 
 F32, BF16, F16 = 0, 1, 2
 COUNTER_BYTES = 65536   # QG_KV4_COUNTER_BYTES
+MAX_KV_LEN = 1 << 30    # of a call
 _TYPES = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}
 ROPE_PLAIN, ROPE_LINEAR, ROPE_BY_INDEX, ROPE_BY_TURNS = 0, 1, 2, 3
 _SCALINGS = {"plain": ROPE_PLAIN, "linear": ROPE_LINEAR, "by_index": ROPE_BY_INDEX, "by_turns": ROPE_BY_TURNS}
@@ -187,12 +188,15 @@ def read(cache, slots, dtype=torch.float32, k=None, v=None):
     return k, v
 
 
-def attention_workspace_bytes(cache, q_heads, batch, max_q_len=1, max_kv_len=0):
+def attention_workspace_bytes(cache, q_heads, batch, max_q_len=1, max_kv_len=None):
+    """Bytes that attention() with at most these extents wants (max_kv_len by default: any length); 0: no call splits its keys."""
+    max_kv_len = MAX_KV_LEN if max_kv_len is None else max_kv_len
     return lib.qg_kv4_attention_workspace_bytes(cache._ref, q_heads, batch, max_q_len, max_kv_len)
 
 
-def attention_workspace(cache, q_heads, batch, max_q_len=1, max_kv_len=0):
-    """A workspace for attention() with at most these extents (None where it needs none); one per stream that calls run on."""
+def attention_workspace(cache, q_heads, batch, max_q_len=1, max_kv_len=None):
+    """A workspace for attention() with at most these extents (max_kv_len by default: any length); None where no call splits its keys.
+    One per stream that calls run on."""
     n = attention_workspace_bytes(cache, q_heads, batch, max_q_len, max_kv_len)
     if n == 0:
         return None

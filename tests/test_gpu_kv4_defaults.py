@@ -66,3 +66,17 @@ def test_block_takes_all_queries(env):
     assert torch.isfinite(out[0]).all()
     # (the same sums in another order where the bound chooses another kernel: one step of the 8-bit activations of the output product)
     assert (out[0] - out[1]).abs().max() <= 2 * (4.0 / 255) * np.abs(wo).max()
+
+
+def test_workspace_for_any_length(env):
+    """attention() without max_kv_len takes what the page table holds; attention_workspace() without it serves that, and keys are split."""
+    kv4, torch, dev = env
+    cache, pages, lens = filled(env, [3000])
+    ws = kv4.attention_workspace(cache, 4, 1)
+    assert ws is not None and ws.numel() == kv4.attention_workspace_bytes(cache, 4, 1) >= kv4.attention_workspace_bytes(cache, 4, 1, max_kv_len=3000)
+    q = torch.randn(1, 4, 64, device=dev)
+    ws[kv4.COUNTER_BYTES:] = 0xFF
+    got = kv4.attention(q, cache, pages, lens, workspace=ws)
+    assert (ws[kv4.COUNTER_BYTES:] != 0xFF).any()                       # (partial results went through it)
+    assert torch.equal(got, kv4.attention(q, cache, pages, lens, max_kv_len=pages.shape[1] * 16,
+                                          workspace=kv4.attention_workspace(cache, 4, 1, max_kv_len=pages.shape[1] * 16)))
