@@ -6,13 +6,15 @@
     o = kv4.attention(q, cache, pages, kv_lens)                            # one query token per sequence
 
 Tensors of heads are [tokens, heads, head_dim] in float32, bfloat16 or float16 with any strides but a unit stride of channels:
-views of a fused projection's rows are taken as they are.  Argument marshalling only, like qgemm.py: the calls that a program
-repeats first go through the extension module, and only a call that it declines is marshalled, and its error named, here.
+views of a fused projection's rows are taken as they are.  rope() is differentiable; what goes through the cache carries no gradient.
+Argument marshalling only, like qgemm.py: the calls that a program repeats first go through the extension module, and only a call that
+it declines is marshalled, and its error named, here.
 """
 import ctypes
 import math
 
 import torch
+from torch.autograd import forward_ad
 
 from .qgemm import QGemmError, _binding, _check, _stream, lib
 
@@ -95,7 +97,41 @@ def rope_table(max_pos, rot, base=10000.0, scaling="plain", factor=1.0, low=1.0,
 
 def rope(x, positions, table, interleaved=False, inverse=False, out=None):
     """x [tokens, heads, head_dim] with the first table.shape[1] channels of every head turned by the token's position (int32
-    [tokens]); inverse: turned back, the gradient.  `out` may be x."""
+    [tokens]); inverse: turned back, the gradient.  `out` may be x.  Differentiable in x where `out` is not given."""
+    if x.requires_grad or table.requires_grad or forward_ad._current_level >= 0 or (out is not None and out.requires_grad):
+        if _tracked(table) or (out is not None and (_tracked(x) or _tracked(out))):
+            raise RuntimeError("kv4.rope has a gradient for x alone, and none with out=")
+        if _tracked(x):
+            return _Rope.apply(x, positions, table, interleaved, inverse)
+    return _rope(x, positions, table, interleaved, inverse, out)
+
+
+def _tracked(x):
+    return (x.requires_grad and torch.is_grad_enabled()) or (forward_ad._current_level >= 0 and forward_ad.unpack_dual(x).tangent is not None)
+
+
+class _Rope(torch.autograd.Function):
+    """A linear map: its gradient is the map turned back, its differential the map itself."""
+
+    @staticmethod
+    def forward(ctx, x, positions, table, interleaved, inverse):
+        ctx.save_for_backward(positions, table)
+        ctx.save_for_forward(positions, table)
+        ctx.interleaved, ctx.inverse = interleaved, inverse
+        return _rope(x, positions, table, interleaved, inverse)
+
+    @staticmethod
+    def backward(ctx, g):
+        g = g if g.stride(2) == 1 else g.contiguous()          # (of a sum, say: one number with strides of 0)
+        return (rope(g, *ctx.saved_tensors, ctx.interleaved, not ctx.inverse),) + (None,) * 4
+
+    @staticmethod
+    def jvp(ctx, t, *_):
+        t = t if t.stride(2) == 1 else t.contiguous()
+        return rope(t, *ctx.saved_tensors, ctx.interleaved, ctx.inverse)
+
+
+def _rope(x, positions, table, interleaved=False, inverse=False, out=None):
     done = _binding.rope(x, positions, table, interleaved, inverse, out)
     if done is not None:
         return done
