@@ -110,7 +110,7 @@ __global__ __launch_bounds__(64 * WAVES, waves_per_simd(D, NR)) void qg_kv4_atte
   const int r = lane & 15, g = lane >> 4;
   job j;
   if (!j.init<ROWS, false>(p)) return;
-  const reader<D, SMALL> in(p, j.seq, j.head, r, g);
+  const reader<D, SMALL> in(p, j.seq, j.keys, j.head, r, g);
   int t0 = j.lo + wave * TILE;
   page_ids next = {0u, 0u};
   if (t0 < j.hi) next = in.pages(t0);

@@ -147,7 +147,7 @@ __global__ __launch_bounds__(64 * waves_of(D), waves_per_simd(D)) void qg_kv4_at
   const int r = lane & 15, g = lane >> 4;
   job j;
   if (!j.init<ROWS, true>(p)) return;
-  const reader<D, SMALL> in(p, j.seq, j.head, r, g);
+  const reader<D, SMALL> in(p, j.seq, j.keys, j.head, r, g);
   const int wave_row = j.row0 + wave * 16 * NR;
 
   raw_query<D, TYPE> raw[NR];
