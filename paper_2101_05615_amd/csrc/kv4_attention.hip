@@ -208,10 +208,13 @@ __global__ __launch_bounds__(64 * WAVES, waves_per_simd(D, NR)) void qg_kv4_atte
     }
   }
   if (j.slices == 1) return;
-  if (D == 256 && (j.last_row - j.row0 + 1) * (D / 4) > 2 * 64 * WAVES)
+  // More than two items a thread: four at once, so that their requests overlap (20 rows of 256 channels 25.6 us, one after the other
+  // 29.1; 32 rows of 128 channels over 32768 keys 68, 74; four sequences of 20 such rows 18.8, 17.9).  Fewer: 16 shares of one item at
+  // once (eight: 32768 keys of one KV head 24.8 -> 26.5, of 16 rows 41.5 -> 44.6; the four shares of 777 keys alone gain, 9.2 -> 8.6).
+  if (ROWS * (D / 4) > 2 * 64 * WAVES && (j.last_row - j.row0 + 1) * (D / 4) > 2 * 64 * WAVES)
     join<D, TYPE, 64 * WAVES, 4, 4>(p, j, w, nullptr, &ticket);
   else
-    join<D, TYPE, 64 * WAVES, 1, D == 128 && DIG == 1 ? 16 : 8>(p, j, w, part, &ticket);
+    join<D, TYPE, 64 * WAVES, 1, 16>(p, j, w, part, &ticket);
 }
 
 template <int D, int TYPE, int NR>
