@@ -196,11 +196,11 @@ static inline int qg_kv4_rows_per_workgroup(int head_dim, long long rows) {
   if (rows <= QG_KV4_FEW) return head_dim == 256 || rows <= 16 ? 16 : 32;
   return 128;  // (fp32 with 128 channels and less: 64; the split of the keys is the same for all types)
 }
-// Workgroups of a dealt launch at most: `units` (sequence, head, block of rows), of which each has one share more than it fills, beside
-// the `at_once` that are dealt to; shares have `least` stages of 64 tokens
+// Workgroups of a dealt launch at most: `units` (sequence, head, block of rows), of which each has one share more than it fills, in two
+// rounds of `at_once`; shares have `least` stages of 64 tokens
 static inline long long qg_kv4_dealt(long long units, int at_once, int max_kv_len, int least) {
-  const long long round = (long long)at_once + units, pieces = units * (((max_kv_len + 63) / 64 + least - 1) / least);
-  return round < pieces ? round : pieces;
+  const long long rounds = 2ll * at_once + units, pieces = units * (((max_kv_len + 63) / 64 + least - 1) / least);
+  return rounds < pieces ? rounds : pieces;
 }
 hipError_t qg_launch_kv4_attention_few(const qg_kv4_attention_args& a, int head_dim, int dtype, int rows, hipStream_t s);
 hipError_t qg_launch_kv4_attention_many(const qg_kv4_attention_args& a, int head_dim, int dtype, int rows, hipStream_t s);

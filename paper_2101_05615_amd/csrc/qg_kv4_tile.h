@@ -505,12 +505,10 @@ struct job {
       blocks = p.row_blocks;
       first = 0;
     } else {
-      // Every wave deals the keys for itself: shares of at most `chosen` stages of 64 tokens, of one length within a sequence, the
-      // fewest stages that make no more workgroups than there are CUs, or than run at once.  A share costs its stages and about four
-      // (queries in, results out; four fifths of it for a workgroup that has a CU to itself), the join one a share; the cheaper way is
-      // taken.  The prices are fitted: over 33 calls of all head sizes and types, 1 to 64 sequences, 20 to 512 queries, the choice is
-      // within 3 % of the better way but for one call, 7 % off (one sequence of 8192 keys of one KV head: 58 us the first way, 65 the
-      // second; four of up to 8192 of eight: 229 and 135).  Two rounds of shorter shares took up to 40 % more, and nowhere 3 % less.
+      // Every wave deals the keys for itself: shares of at most `stages` of 64 tokens, of one length within a sequence.  Three ways: the
+      // fewest stages that make no more workgroups than there are CUs, or than run at once, or half of what each of those
+      // would have on average.  A round costs its stages and about four (queries in, results out; four fifths of it for a workgroup
+      // that has a CU to itself), the join one a share; the cheapest way is taken.
       const int lane = (int)threadIdx.x & 63, longest = (p.max_kv_len + 63) / 64;
       int all, wide;  // of the lane's sequence: stages, workgroups of a share
       auto measure = [&](int b0) {
@@ -537,10 +535,11 @@ struct job {
         }
         return min(x, longest);
       };
-      const int alone = fit(min(p.shares, 256)), once = fit(p.shares);
+      const int alone = fit(min(p.shares, 256)), once = fit(p.shares), twice = max(p.least, (work + 2 * p.shares - 1) / (2 * p.shares));
       const float cost_alone = 0.8f * (float)(alone + 4) + (float)longest / (float)alone;
       const float cost_once = (float)(once + 4) + (float)longest / (float)once;
-      const int chosen = cost_alone < cost_once ? alone : once;
+      const float cost_twice = 2.0f * (float)(twice + 4) + (float)longest / (float)twice;
+      const int chosen = cost_twice < fminf(cost_alone, cost_once) ? twice : cost_alone < cost_once ? alone : once;
       first = 0;
       bool found = false;
       for (int b0 = 0; b0 < p.batch && !found; b0 += 64) {
