@@ -52,11 +52,11 @@ int check_rotation(const float* table, int max_pos, int rot, int interleaved, in
 //   Few rows: shares of equal length, so many that every CU has a workgroup if all sequences are as long as the longest may be.  More
 //   would cost more than it evens out: every share is written, and read by the last one to arrive (131072 keys of 8 KV heads, 8 rows:
 //   34 us in 256 shares, 40 in 512, 49 in 1024), and so would shares by the lengths there are, as below (64 sequences of up to 8192
-//   keys: 69.3 us for 69.0; 16 of up to 4096, 5 queries: 27.9 for 25.6).
+//   keys: 69.3 us for 69.0; 16 of up to 4096, 5 queries: 27.9 for 25.4).
 //   Many rows: workgroups run for long, so the kernel deals the keys by the lengths that it finds, in one or two rounds of the
 //   workgroups that run at once (three a CU with 64 channels, two with 128, one with 256).  512 queries of four sequences of 8192,
-//   1981, 1766 and 1310 keys, 32 heads over 8 of 128 channels: 150 us (equal shares 164, whole 240); four of 4096 keys: 171, as whole
-//   (two rounds 200); one of 8192, 8 heads over one: 56 (in as many shares as run at once 64).
+//   1981, 1766 and 1310 keys, 32 heads over 8 of 128 channels: 149 us (equal shares 164, whole 240); four of 4096 keys: 169, as whole
+//   (two rounds 197); one of 8192, 8 heads over one: 58 (in as many shares as run at once 65).
 constexpr int FEW_SHARES = 256;
 constexpr size_t COUNTERS = QG_KV4_COUNTER_BYTES / 4;  // a fixed part of every workspace, so that calls of other extents find it zero
 constexpr int LEAST_FEW = 256, LEAST_MANY = 512;       // tokens of a share; up to twice that keys are not split

@@ -27,7 +27,7 @@
 // against a reference of their own row, the largest such product that it has met, so that they lie below 2^12 and keep 11 bits
 // down to 2^-18 of that.  One such number is enough for a bf16 result (1.68e-3 off, 1.67e-3 with exact weights: the result's own rounding).
 // An fp16 result shows it (2.9e-4 off, 2.1e-4 with two), so fp16 and fp32 results take two: 131072 keys of 8 heads 34.4 -> 36.1 us, 512 rows
-// of four sequences 154 -> 181.
+// of four sequences 146 -> 178.
 // Scores, maxima, sums and outputs are fp32.
 //
 // References.  With alpha the value scale and S a power of two that all rows of a wave share, a row holds
