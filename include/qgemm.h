@@ -585,7 +585,7 @@ int qg_kv4_read(const qg_kv4_cache* c, const int64_t* slots, int tokens, int dty
  * QG_F16 and QG_F32, however many rows there are) relative to the
  * largest such product of the row, of which each key may lose 2^-28; keys that a row
  * does not see, or gives no weight, take nothing from it while scores are below 2^24
- * and their value scales less than 2^80 times those of the keys that carry it.
+ * and their value scales less than 2^64 times those of the keys that carry it.
  *   pages     dev int32 [batch][pages_stride]; entry i names the page of tokens
  *             i * page_tokens on.  Only entries below ceil(m / page_tokens) are read;
  *             one that is no page of the cache reads as page 0.

@@ -137,3 +137,17 @@ def test_tokens_of_zeros(env, n, size):
     got, hk, hv, span = run(env, keys, values, q)
     check(got, q, hk, hv, span, "float32", 0, rows=[0, n - 1])
     assert (run(env, keys, values * 0, q)[0] == 0).all()
+
+
+@pytest.mark.parametrize("n", [2, 40])
+@pytest.mark.parametrize("k", [40, 64])
+def test_many_keys_before_a_token_with_large_values(env, n, k):
+    """20000 keys of about equal weight, so that their sum is large where the last token's values change the common reference."""
+    kv4, torch, dev = env
+    rng = np.random.default_rng(n)
+    m, D = 20000, 64
+    keys, values = 0.1 * rng.standard_normal((m, HKV, D)), rng.standard_normal((m, HKV, D))
+    values[-1] *= 2.0 ** k
+    q = torch.from_numpy(rng.standard_normal((n, HQ, D)).astype(np.float32))
+    got, hk, hv, span = run(env, keys, values, q)
+    check(got, q, hk, hv, span, "float32", k, rows=[0, n - 1])
