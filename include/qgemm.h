@@ -619,6 +619,122 @@ size_t qg_kv4_attention_workspace_bytes(const qg_kv4_cache* c, int q_heads, int 
                                         int max_kv_len);
 int qg_kv4_attention(const qg_kv4_cache* c, const qg_kv4_attention_params* p, void* stream);
 
+/* ---- 8-bit floats with a scale for each block of 128 ------------------------ */
+
+/* Numbers are e4m3 (sign, 4 exponent bits, 3 mantissa bits: sizes up to 448, no
+ * infinity) times 2^e with one e for a block: 128 consecutive channels of a token,
+ * or 128 x 128 of a weight matrix.  From the largest size in the block, amax = m 2^k
+ * with 1 <= m < 2,
+ *   e = k - 8 where m <= 1.75, k - 7 otherwise, at least -127 (amax 0: -127)
+ *   code = x 2^-e rounded to e4m3, nearest even; x stands for code 2^e
+ * (a power of two loses nothing that a free scale would keep, the codes being
+ * floating, and is exact in every step).  An infinity or NaN makes its block NaN.
+ * Products of 8-bit numbers are exact.  The matrix cores for 8 bits align the products
+ * of eight neighbours in K to the largest of them, drop what lies 2^-13 below it, and
+ * sum the rest in fp32: about 2e-5 of a result's typical size.  With wide_sums = 1 a
+ * product runs on the bf16 cores instead, all sums fp32, at half the rate where there
+ * are many rows (up to 64 rows every product does).  A result is rounded once. */
+
+/* A matrix [tokens][channels] with unit channel stride; the stride counts elements,
+ * any sign, any alignment that the element type has by itself. */
+typedef struct {
+  void* data;             /* dev                     */
+  int64_t token_stride;
+} qg_rows;
+
+/* Activations in 8 bits: codes [tokens][channels rounded up to 128] bytes, 0 behind
+ * the last channel, 16-byte aligned; scales [tokens][blocks rounded up to 4] bytes
+ * e + 127 (255: NaN), 4-byte aligned.  tokens * channels may pass 2^31. */
+#define QG_FP8_MAX_CHANNELS (1 << 20)
+typedef struct {
+  void* codes;            /* dev, qg_fp8_codes_bytes()  */
+  void* scales;           /* dev, qg_fp8_scales_bytes() */
+  int32_t tokens, channels;
+} qg_fp8_blocks;
+size_t qg_fp8_codes_bytes(int tokens, int channels);   /* 0: not supported, or no tokens */
+size_t qg_fp8_scales_bytes(int tokens, int channels);
+
+/* x [tokens][channels] of `dtype` into 8 bits, and back (rounded to `dtype` once). */
+int qg_fp8_quantize(const qg_rows* x, int dtype, const qg_fp8_blocks* to, void* stream);
+int qg_fp8_dequantize(const qg_fp8_blocks* x, int dtype, const qg_rows* to, void* stream);
+
+/* Weights B [k][n] in 8 bits, laid out for the matrix cores: one buffer that the
+ * program keeps.  gated = 1: a pair of such matrices, gate and up, side by side. */
+typedef struct {
+  void* data;             /* dev, 16-byte aligned, qg_fp8_weight_bytes() */
+  int32_t k, n, gated;
+} qg_fp8_weight;
+size_t qg_fp8_weight_bytes(int k, int n, int gated);   /* 0: not supported */
+
+/* Any strides, in elements. */
+typedef struct {
+  const void* data;       /* dev */
+  int64_t row_stride, column_stride;
+} qg_matrix;
+
+/* B (and, for a pair, `up`; NULL otherwise) of `dtype` into `w` and, for products
+ * with the transpose, into `transposed`, with the same codes and scales; either may
+ * be NULL.  transposed: k = n of B, n = k of B, gated 0; of a pair k = 2 * (n rounded
+ * up to 128): the transpose of gate, then of up, which is the layout of the gradient
+ * that qg_fp8_gated_backward writes.  An ordinary run-time call. */
+int qg_fp8_pack(const qg_matrix* b, const qg_matrix* up, int k, int n, int dtype, const qg_fp8_weight* w,
+                const qg_fp8_weight* transposed, void* stream);
+
+/* Up to this many tokens the products below take activations as they are and put them
+ * into 8 bits on the way (the result is the same). */
+#define QG_FP8_FEW 16
+
+#define QG_SILU 0         /* g / (1 + exp(-g))                                  */
+#define QG_GELU 1         /* g (1 + erf(g / sqrt 2)) / 2                        */
+#define QG_GELU_TANH 2    /* g (1 + tanh(sqrt(2 / pi) (g + 0.044715 g^3))) / 2  */
+#define QG_RELU 3         /* max(g, 0)                                          */
+
+/* A workspace lets a call deal K, or the tokens of a gradient, over workgroups, which
+ * calls of few rows or small results need; one serves calls of any extents.  16-byte
+ * aligned, QG_FP8_WORKSPACE_BYTES, its first QG_FP8_COUNTER_BYTES zeroed once by
+ * qg_gemm_workspace_init before its first use; every call leaves it ready for the next
+ * one on the stream.  Calls that may overlap in time need one each.  NULL is allowed.
+ * The result of a call is the same every time it is made with the same workspace
+ * or without one. */
+#define QG_FP8_COUNTER_BYTES 16384
+#define QG_FP8_WORKSPACE_BYTES (QG_FP8_COUNTER_BYTES + (32 << 20))
+
+typedef struct {
+  qg_fp8_blocks x;        /* [tokens][k of the weights]; codes NULL: x_rows is taken */
+  qg_rows x_rows;         /* of type x_dtype, at most QG_FP8_FEW tokens              */
+  int32_t x_dtype, tokens;
+  qg_rows out;            /* [tokens][n]                                             */
+  int32_t dtype;          /* of out                                                  */
+  int32_t activation;     /* gated: QG_SILU ..                                       */
+  int32_t wide_sums;      /* 0 or 1                                                  */
+  const float* bias;      /* dev [n], or NULL; plain products only                   */
+  void* workspace;
+  size_t workspace_bytes;
+} qg_fp8_product;
+
+/* out = x B + bias */
+int qg_fp8_matmul(const qg_fp8_weight* w, const qg_fp8_product* p, void* stream);
+
+/* h = activation(x Gate) * (x Up), one kernel: into out, or, with out.data NULL (and x
+ * in 8 bits), into `held` [tokens][n], the 8-bit form of h's fp32 value. */
+int qg_fp8_gated(const qg_fp8_weight* w, const qg_fp8_product* p, const qg_fp8_blocks* held, void* stream);
+
+/* The gated block's backward pass.  From x in 8 bits and dh [tokens][n] of type
+ * dh_dtype it computes g = x Gate and u = x Up again, and with them, in fp32,
+ *   dg = dh u activation'(g),  du = dh activation(g),  h = activation(g) u
+ * dgu: bf16 [tokens][2][n rounded up to 128], contiguous, 16-byte aligned: dg and du, 0
+ * behind the last column, for the weights' gradients; dgu_held: the 8-bit form of
+ * their fp32 values, 2 * (n rounded up to 128) channels, for the gradient of x; held:
+ * that of h, as qg_fp8_gated writes it.  p: x, tokens, activation and workspace are used. */
+int qg_fp8_gated_backward(const qg_fp8_weight* w, const qg_fp8_product* p, const qg_rows* dh, int dh_dtype, void* dgu,
+                          const qg_fp8_blocks* dgu_held, const qg_fp8_blocks* held, void* stream);
+
+/* The gradient of the weights of x B: out [k][n] = x^T dy, from x in 8 bits and dy
+ * [tokens][n] of type dy_dtype: sums of exact products in fp32, every bit of dy used.
+ * No tokens: zeros. */
+int qg_fp8_weight_gradient(const qg_fp8_blocks* x, const qg_rows* dy, int dy_dtype, int n, const qg_rows* out, int dtype,
+                           void* workspace, size_t workspace_bytes, void* stream);
+
 const char* qg_status_string(int code);
 
 #ifdef __cplusplus

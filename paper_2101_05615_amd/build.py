@@ -9,7 +9,8 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libqgemm.so")
 BINDING = os.path.join(HERE, "_binding.so")
 SOURCES = ["api.hip", "pack.hip", "quantize_a.hip", "gemm_tile.hip", "gemm_skinny.hip", "conv_group.hip", "conv_patch.hip", "conv_runs.hip",
-           "api_kv4.hip", "rope.hip", "kv4_cache.hip", "kv4_attention.hip", "kv4_attention_rows.hip"]
+           "api_kv4.hip", "rope.hip", "kv4_cache.hip", "kv4_attention.hip", "kv4_attention_rows.hip",
+           "api_fp8.hip", "fp8_quantize.hip", "fp8_tile.hip", "fp8_stream.hip", "fp8_gradient.hip"]
 PROBES_SRC = os.path.join(ROOT, "bench_probes.hip")   # bench.py's measurement probes, a library of their own
 PROBES_LIB = os.path.join(ROOT, "libbench_probes.so")
 

@@ -1,0 +1,283 @@
+// Host side of the 8-bit floats with a scale per block of 128 (qgemm.h): argument checks, which kernel a call runs on, and how K is
+// dealt over workgroups.  As in the rest of the library nothing is allocated, created or waited for here.
+#include "qg_fp8.h"
+
+namespace {
+
+inline bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
+
+constexpr size_t ELEM[3] = {4, 2, 2};
+constexpr int MAX_TOKENS = 1 << 28;
+
+bool known(int dtype) { return dtype == QG_F32 || dtype == QG_BF16 || dtype == QG_F16; }
+
+bool extents_ok(int k, int n) { return k >= 1 && n >= 1 && k <= QG_FP8_MAX_CHANNELS && n <= QG_FP8_MAX_CHANNELS; }
+
+int pitch_of(int channels) { return qg_fp8_up(channels, 128); }
+int scale_pitch_of(int channels) { return qg_fp8_up(pitch_of(channels) / 128, 4); }
+
+int check_rows(const qg_rows& x, int dtype, qg_fp8_rows* out) {
+  if (!x.data) return QG_ENULL;
+  *out = {x.data, x.token_stride};
+  return aligned(x.data, ELEM[dtype]) ? QG_OK : QG_EALIGN;
+}
+bool tokens_ok(int tokens) { return tokens >= 0 && tokens <= MAX_TOKENS; }
+
+// (data pointers of no tokens are not referenced)
+int check_blocks(const qg_fp8_blocks* b, int tokens, int channels, qg_fp8_held* out) {
+  if (!b) return QG_ENULL;
+  if (!tokens_ok(b->tokens) || b->tokens != tokens || b->channels != channels || !extents_ok(channels, 1)) return QG_EINVAL;
+  *out = {static_cast<uint8_t*>(b->codes), static_cast<uint8_t*>(b->scales), pitch_of(channels), scale_pitch_of(channels)};
+  if (tokens == 0) return QG_OK;
+  if (!b->codes || !b->scales) return QG_ENULL;
+  return aligned(b->codes, 16) && aligned(b->scales, 4) ? QG_OK : QG_EALIGN;
+}
+
+size_t piece_bytes(int k, int groups) { return (size_t)groups * (pitch_of(k) / 128) * QG_FP8_PIECE; }
+int groups_of(int n, int gated) { return gated ? pitch_of(n) / 32 : qg_fp8_up(n, 256) / 64; }
+
+int check_weight(const qg_fp8_weight* w, qg_fp8_layout* out) {
+  if (!w) return QG_ENULL;
+  if (qg_fp8_weight_bytes(w->k, w->n, w->gated) == 0) return QG_EINVAL;
+  if (!w->data) return QG_ENULL;
+  if (!aligned(w->data, 16)) return QG_EALIGN;
+  const int groups = groups_of(w->n, w->gated), kb = pitch_of(w->k) / 128;
+  *out = {static_cast<const uint8_t*>(w->data),
+          reinterpret_cast<const uint32_t*>(static_cast<const uint8_t*>(w->data) + piece_bytes(w->k, groups)), w->k, w->n, kb,
+          qg_fp8_up(kb, 4), groups};
+  return QG_OK;
+}
+
+int done(hipError_t e) { return e == hipSuccess ? QG_OK : QG_ELAUNCH; }
+
+int check_workspace(void* workspace, size_t bytes) {
+  if (!workspace) return QG_OK;
+  if (bytes < QG_FP8_WORKSPACE_BYTES) return QG_EWORKSPACE;
+  return aligned(workspace, 16) ? QG_OK : QG_EALIGN;
+}
+
+constexpr int COUNTERS = QG_FP8_COUNTER_BYTES / 4;
+constexpr long long PARTIALS = (32 << 20) / 4;  // floats
+
+// Workgroups that share K: `parts` without, `floats` of sums each, `wanted` workgroups in all, at least `least` blocks of K each
+void deal(qg_fp8_product_args* a, void* workspace, long long parts, long long floats, int wanted, int least) {
+  a->slices = 1;
+  a->slice_kb = a->w.kb;
+  if (!workspace || parts > COUNTERS) return;
+  long long slices = wanted / parts;
+  if (slices > a->w.kb / least) slices = a->w.kb / least;
+  if (slices > PARTIALS / (parts * floats)) slices = PARTIALS / (parts * floats);
+  if (slices < 2) return;
+  a->slice_kb = qg_fp8_up((a->w.kb + (int)slices - 1) / (int)slices, 4);
+  a->slices = (a->w.kb + a->slice_kb - 1) / a->slice_kb;
+  a->counters = static_cast<int*>(workspace);
+  a->partial = reinterpret_cast<float*>(a->counters + COUNTERS);
+}
+
+int product(const qg_fp8_product_args& args, int end, int wide_sums, void* workspace, hipStream_t s) {
+  qg_fp8_product_args a = args;
+  const bool plain_out = a.out.data != nullptr && end != QG_FP8_GATED_BACK;
+  if (plain_out && a.tokens <= 64) {
+    const int rf = a.tokens <= 16 ? 1 : a.tokens <= 32 ? 2 : 4;
+    const int fragments = a.w.groups >= 256 ? 4 : 2, waves = rf == 4 ? 4 : 8;
+    const long long sets = (long long)a.w.groups * (4 / fragments);
+    deal(&a, workspace, sets, (long long)rf * fragments * 256, 256, 2 * waves);
+    if (sets * a.slices > 0x3fffffll) return QG_EUNSUPPORTED;
+    return done(qg_launch_fp8_stream(a, end == QG_FP8_GATED, fragments, waves, s));
+  }
+  const int fragments = a.tokens <= 32 ? 2 : a.tokens <= 64 ? 4 : 8;
+  const long long columns = a.w.groups / 4;
+  const long long rows = (a.tokens + 16ll * fragments - 1) / (16 * fragments);
+  deal(&a, workspace, rows * columns, fragments * 4096ll, 256, 4);
+  if (rows * columns * a.slices > 0x7fffffll) return QG_EUNSUPPORTED;
+  return done(qg_launch_fp8_tile(a, end, fragments, wide_sums, s));
+}
+
+int check_product(const qg_fp8_weight* w, const qg_fp8_product* p, qg_fp8_product_args* a) {
+  if (!p) return QG_ENULL;
+  *a = {};
+  int rc = check_weight(w, &a->w);
+  if (rc != QG_OK) return rc;
+  if (!tokens_ok(p->tokens) || (p->wide_sums != 0 && p->wide_sums != 1)) return QG_EINVAL;
+  a->tokens = p->tokens;
+  a->channels = w->n;
+  if (p->x.codes || p->tokens == 0) {
+    if (p->tokens && (rc = check_blocks(&p->x, p->tokens, w->k, &a->x8)) != QG_OK) return rc;
+  } else {
+    if (!p->x_rows.data) return QG_ENULL;
+    if (!known(p->x_dtype)) return QG_EINVAL;
+    if (p->tokens > QG_FP8_FEW) return QG_EUNSUPPORTED;
+    if ((rc = check_rows(p->x_rows, p->x_dtype, &a->x)) != QG_OK) return rc;
+    a->x_type = p->x_dtype;
+  }
+  return check_workspace(p->workspace, p->workspace_bytes);
+}
+
+bool activation_ok(int a) { return a >= QG_SILU && a <= QG_RELU; }
+
+}  // namespace
+
+extern "C" {
+
+size_t qg_fp8_codes_bytes(int tokens, int channels) {
+  return tokens_ok(tokens) && extents_ok(channels, 1) ? (size_t)tokens * pitch_of(channels) : 0;
+}
+size_t qg_fp8_scales_bytes(int tokens, int channels) {
+  return tokens_ok(tokens) && extents_ok(channels, 1) ? (size_t)tokens * scale_pitch_of(channels) : 0;
+}
+
+int qg_fp8_quantize(const qg_rows* x, int dtype, const qg_fp8_blocks* to, void* stream) {
+  if (!x || !to) return QG_ENULL;
+  if (!known(dtype)) return QG_EINVAL;
+  qg_fp8_held held;
+  int rc = check_blocks(to, to->tokens, to->channels, &held);
+  if (rc != QG_OK || to->tokens == 0) return rc;
+  qg_fp8_rows rows;
+  if ((rc = check_rows(*x, dtype, &rows)) != QG_OK) return rc;
+  if ((long long)to->tokens * (held.scale_pitch / 4) > 0x7fffffffll / 64) return QG_EUNSUPPORTED;
+  return done(qg_launch_fp8_quantize(rows, dtype, to->tokens, to->channels, held, static_cast<hipStream_t>(stream)));
+}
+
+int qg_fp8_dequantize(const qg_fp8_blocks* x, int dtype, const qg_rows* to, void* stream) {
+  if (!x || !to) return QG_ENULL;
+  if (!known(dtype)) return QG_EINVAL;
+  qg_fp8_held held;
+  int rc = check_blocks(x, x->tokens, x->channels, &held);
+  if (rc != QG_OK || x->tokens == 0) return rc;
+  qg_fp8_rows rows;
+  if ((rc = check_rows(*to, dtype, &rows)) != QG_OK) return rc;
+  if ((long long)x->tokens * (held.scale_pitch / 4) > 0x7fffffffll / 64) return QG_EUNSUPPORTED;
+  return done(qg_launch_fp8_dequantize(held, dtype, x->tokens, x->channels, rows, static_cast<hipStream_t>(stream)));
+}
+
+size_t qg_fp8_weight_bytes(int k, int n, int gated) {
+  if (!extents_ok(k, n) || (gated != 0 && gated != 1)) return 0;
+  const int groups = groups_of(n, gated);
+  return piece_bytes(k, groups) + (size_t)groups * scale_pitch_of(k) * 4;
+}
+
+int qg_fp8_pack(const qg_matrix* b, const qg_matrix* up, int k, int n, int dtype, const qg_fp8_weight* w,
+                const qg_fp8_weight* transposed, void* stream) {
+  if (!b || (!w && !transposed)) return QG_ENULL;
+  if (!known(dtype) || !extents_ok(k, n)) return QG_EINVAL;
+  qg_fp8_pack_args a = {};
+  a.gated = up != nullptr;
+  int rc;
+  if (w) {
+    qg_fp8_layout l;
+    if ((rc = check_weight(w, &l)) != QG_OK) return rc;
+    if (w->k != k || w->n != n || w->gated != a.gated) return QG_EINVAL;
+    a.pieces = const_cast<uint8_t*>(l.pieces);
+    a.scales = const_cast<uint32_t*>(l.scales);
+    a.groups = l.groups;
+    a.kb = l.kb;
+    a.kb4 = l.kb4;
+  }
+  if (transposed) {
+    qg_fp8_layout l;
+    if ((rc = check_weight(transposed, &l)) != QG_OK) return rc;
+    if (transposed->k != (a.gated ? 2 * pitch_of(n) : n) || transposed->n != k || transposed->gated) return QG_EINVAL;
+    a.t_pieces = const_cast<uint8_t*>(l.pieces);
+    a.t_scales = const_cast<uint32_t*>(l.scales);
+    a.t_groups = l.groups;
+    a.t_kb = l.kb;
+    a.t_kb4 = l.kb4;
+  }
+  for (const qg_matrix* m : {b, up}) {
+    if (!m) continue;
+    if (!m->data) return QG_ENULL;
+    if (!aligned(m->data, ELEM[dtype])) return QG_EALIGN;
+  }
+  a.b = {b->data, b->row_stride, b->column_stride};
+  if (up) a.up = {up->data, up->row_stride, up->column_stride};
+  a.k = k;
+  a.n = n;
+  return done(qg_launch_fp8_pack(a, dtype, static_cast<hipStream_t>(stream)));
+}
+
+int qg_fp8_matmul(const qg_fp8_weight* w, const qg_fp8_product* p, void* stream) {
+  qg_fp8_product_args a;
+  int rc = check_product(w, p, &a);
+  if (rc != QG_OK) return rc;
+  if (w->gated || !known(p->dtype)) return QG_EINVAL;
+  if (!aligned(p->bias, 4)) return QG_EALIGN;
+  if (p->tokens == 0) return QG_OK;
+  if ((rc = check_rows(p->out, p->dtype, &a.out)) != QG_OK) return rc;
+  a.out_type = p->dtype;
+  a.bias = p->bias;
+  return product(a, QG_FP8_PLAIN, p->wide_sums, p->workspace, static_cast<hipStream_t>(stream));
+}
+
+int qg_fp8_gated(const qg_fp8_weight* w, const qg_fp8_product* p, const qg_fp8_blocks* held, void* stream) {
+  qg_fp8_product_args a;
+  int rc = check_product(w, p, &a);
+  if (rc != QG_OK) return rc;
+  if (!w->gated || !activation_ok(p->activation) || p->bias) return QG_EINVAL;
+  if (p->tokens == 0) return QG_OK;
+  if (p->out.data) {
+    if (held || !known(p->dtype)) return QG_EINVAL;
+    if ((rc = check_rows(p->out, p->dtype, &a.out)) != QG_OK) return rc;
+    a.out_type = p->dtype;
+  } else {
+    if (a.x.data) return QG_EUNSUPPORTED;
+    if ((rc = check_blocks(held, p->tokens, w->n, &a.out8)) != QG_OK) return rc;
+  }
+  a.activation = p->activation;
+  return product(a, QG_FP8_GATED, p->wide_sums, p->workspace, static_cast<hipStream_t>(stream));
+}
+
+int qg_fp8_gated_backward(const qg_fp8_weight* w, const qg_fp8_product* p, const qg_rows* dh, int dh_dtype, void* dgu,
+                          const qg_fp8_blocks* dgu_held, const qg_fp8_blocks* held, void* stream) {
+  qg_fp8_product_args a;
+  int rc = check_product(w, p, &a);
+  if (rc != QG_OK) return rc;
+  if (!dh || !dgu_held || !held) return QG_ENULL;
+  if (!w->gated || !activation_ok(p->activation) || !known(dh_dtype) || 2ll * pitch_of(w->n) > QG_FP8_MAX_CHANNELS) return QG_EINVAL;
+  if (p->tokens == 0) return QG_OK;
+  if (a.x.data) return QG_EUNSUPPORTED;
+  if ((rc = check_rows(*dh, dh_dtype, &a.dh)) != QG_OK) return rc;
+  if ((rc = check_blocks(dgu_held, p->tokens, 2 * pitch_of(w->n), &a.dgu8)) != QG_OK) return rc;
+  if ((rc = check_blocks(held, p->tokens, w->n, &a.out8)) != QG_OK) return rc;
+  if (!dgu) return QG_ENULL;
+  if (!aligned(dgu, 16)) return QG_EALIGN;
+  a.dh_type = dh_dtype;
+  a.dgu = static_cast<__bf16*>(dgu);
+  a.activation = p->activation;
+  return product(a, QG_FP8_GATED_BACK, 0, p->workspace, static_cast<hipStream_t>(stream));
+}
+
+int qg_fp8_weight_gradient(const qg_fp8_blocks* x, const qg_rows* dy, int dy_dtype, int n, const qg_rows* out, int dtype,
+                           void* workspace, size_t workspace_bytes, void* stream) {
+  if (!x || !dy || !out) return QG_ENULL;
+  if (!known(dy_dtype) || !known(dtype) || !extents_ok(1, n)) return QG_EINVAL;
+  qg_fp8_gradient_args a = {};
+  int rc = check_blocks(x, x->tokens, x->channels, &a.x8);
+  if (rc != QG_OK) return rc;
+  if ((rc = check_workspace(workspace, workspace_bytes)) != QG_OK) return rc;
+  if (x->tokens && (rc = check_rows(*dy, dy_dtype, &a.dy)) != QG_OK) return rc;
+  if ((rc = check_rows(*out, dtype, &a.out)) != QG_OK) return rc;
+  a.dy_type = dy_dtype;
+  a.out_type = dtype;
+  a.tokens = x->tokens;
+  a.k = x->channels;
+  a.n = n;
+  const int tile = 128;
+  const long long tiles = (long long)((a.k + tile - 1) / tile) * ((a.n + tile - 1) / tile);
+  a.slices = 1;
+  a.slice_tokens = qg_fp8_up(a.tokens, 64);
+  if (workspace && tiles <= COUNTERS) {
+    long long slices = 512 / tiles;
+    if (slices > a.tokens / 256) slices = a.tokens / 256;
+    if (slices > PARTIALS / (tiles * tile * tile)) slices = PARTIALS / (tiles * tile * tile);
+    if (slices > 1) {
+      a.slice_tokens = qg_fp8_up((a.tokens + (int)slices - 1) / (int)slices, 64);
+      a.slices = (a.tokens + a.slice_tokens - 1) / a.slice_tokens;
+      a.counters = static_cast<int*>(workspace);
+      a.partial = reinterpret_cast<float*>(a.counters + COUNTERS);
+    }
+  }
+  if (tiles * a.slices > 0x7fffffll) return QG_EUNSUPPORTED;
+  return done(qg_launch_fp8_gradient(a, static_cast<hipStream_t>(stream)));
+}
+
+}  // extern "C"

@@ -1,0 +1,245 @@
+// 8-bit floats with a scale per block of 128: layouts, and what the kernels that write, multiply and read them share.
+// Not part of the public interface.
+#pragma once
+
+#include "qg_kv4.h"
+
+// ---------------------------------------------------------------------------
+// A number is e4m3 (sign, 4 exponent bits with bias 7, 3 of mantissa; sizes 0, 2^-9 .. 448; 0x7f NaN) times 2^e, one e for a block, held
+// as the byte e + 127 (255: the block is NaN).  A block is 128 channels of a token, or 128 x 128 of a weight matrix.
+//
+// Activations: codes [tokens][pitch], pitch = channels rounded up to 128 (codes 0 behind the last channel); scale bytes
+// [tokens][scale pitch], scale pitch = blocks rounded up to 4: a dword is the scales of four blocks of a token, which the matrix
+// instructions take by byte.
+//
+// Weights B [K][N]: cut into pieces of 64 slots x 128 of K, 8 KiB each: [slots / 64][K / 128][4 fragments][2 halves][64 lanes][16 bytes].
+// A fragment is 16 slots x 128 of K as v_mfma_scale_f32_16x16x128_f8f6f4 takes it for its first operand: lane (i + 16 g) has the bytes
+//     B[128 kb + 64 half + 16 g + 0..15][column of slot i]
+// (the instruction's own order of K differs; both operands have this one, so the sum is the same).  Slot i = 4 q + r of fragment j is
+//     plain:  column 64 group + 16 q + 4 j + r
+//     gated:  column 32 group + 8 q + 4 (j >> 1) + r of the gate matrix for even j, of the up matrix for odd
+// so that a lane of the result, which has the slots 4 q + 0..3 of every fragment, has 16 consecutive columns (8 of each matrix).  Behind the
+// pieces lie the scales: [slots / 64][K / 128 rounded up to 4] dwords, byte j for fragment j.  Columns are padded to 256 slots, codes 0.
+// ---------------------------------------------------------------------------
+#define QG_FP8_BLOCK 128
+#define QG_FP8_PIECE 8192
+
+static inline __host__ __device__ int qg_fp8_up(int x, int m) { return (x + m - 1) / m * m; }
+
+struct qg_fp8_layout {  // of a packed matrix
+  const uint8_t* pieces;
+  const uint32_t* scales;
+  int k, n;      // extents of B (gated: of each of both)
+  int kb, kb4;   // blocks along K, and rounded up to 4
+  int groups;    // of 64 slots, a multiple of 4
+};
+
+struct qg_fp8_rows {  // a float matrix [tokens][channels] with unit channel stride
+  void* data;
+  long long stride;
+};
+struct qg_fp8_held {  // a matrix of activations in 8 bits
+  uint8_t* codes;
+  uint8_t* scales;
+  int pitch, scale_pitch;
+};
+
+struct qg_fp8_product_args {
+  qg_fp8_layout w;
+  qg_fp8_held x8;
+  qg_fp8_rows x;         // streaming kernel: activations that are not in 8 bits yet
+  int tokens;
+  int x_type, out_type;  // QG_F32 ..
+  int activation;
+  int channels;          // columns of the result (gated: of h)
+  qg_fp8_rows out;       // plain and gated results; data null: held8
+  const float* bias;
+  qg_fp8_held out8;      // gated: h in 8 bits
+  // the gated block's backward pass
+  qg_fp8_rows dh;        // of type dh_type
+  int dh_type;
+  __bf16* dgu;           // [tokens][2 * channels rounded up to 128]: gate, then up
+  qg_fp8_held dgu8;
+  // K dealt over workgroups
+  int slices, slice_kb;  // blocks of a slice, a multiple of 4
+  int* counters;
+  float* partial;
+};
+
+struct qg_fp8_gradient_args {
+  qg_fp8_held x8;
+  qg_fp8_rows dy, out;
+  int dy_type, out_type;
+  int tokens, k, n;
+  int slices, slice_tokens;  // a multiple of 64
+  int* counters;
+  float* partial;
+};
+
+struct qg_fp8_matrix_args {
+  const void* data;
+  long long row_stride, column_stride;
+};
+struct qg_fp8_pack_args {
+  qg_fp8_matrix_args b, up;
+  int k, n, gated;
+  uint8_t *pieces, *t_pieces;   // of B, and of its transpose; either may be null
+  uint32_t *scales, *t_scales;
+  int groups, kb, kb4;          // of B's pieces
+  int t_groups, t_kb, t_kb4;    // of the transpose's
+};
+
+hipError_t qg_launch_fp8_quantize(const qg_fp8_rows& x, int type, int tokens, int channels, const qg_fp8_held& to, hipStream_t s);
+hipError_t qg_launch_fp8_dequantize(const qg_fp8_held& x, int type, int tokens, int channels, const qg_fp8_rows& to, hipStream_t s);
+hipError_t qg_launch_fp8_pack(const qg_fp8_pack_args& a, int type, hipStream_t s);
+enum qg_fp8_end { QG_FP8_PLAIN, QG_FP8_GATED, QG_FP8_GATED_BACK };
+hipError_t qg_launch_fp8_tile(const qg_fp8_product_args& a, int end, int row_fragments, int wide_sums, hipStream_t s);
+hipError_t qg_launch_fp8_stream(const qg_fp8_product_args& a, int gated, int fragments, int waves, hipStream_t s);
+hipError_t qg_launch_fp8_gradient(const qg_fp8_gradient_args& a, hipStream_t s);
+
+#ifdef __HIPCC__
+namespace {
+
+typedef float f4 __attribute__((ext_vector_type(4)));
+typedef unsigned u4 __attribute__((ext_vector_type(4)));
+typedef unsigned u2 __attribute__((ext_vector_type(2)));
+typedef int i8v __attribute__((ext_vector_type(8)));
+
+// The scale byte for a block whose largest size has these bits (of |x| in fp32, the largest as an integer: an infinity or NaN is above
+// every number): amax = m 2^k, e = k - 8 up to m = 1.75 and k - 7 above, at least -127.  A subnormal amax (k below -126) ends at -127.
+__device__ inline unsigned scale_byte(unsigned amax) {
+  if (amax >= 0x7f800000u) return 255u;
+  const int e = (int)(amax >> 23) - 8 + ((amax & 0x7fffffu) > 0x600000u ? 1 : 0);  // + 127
+  return (unsigned)(e < 0 ? 0 : e);
+}
+// The scale as the conversions and the widening take it: the power of two with this exponent byte (they read nothing else; 0 is 2^-127)
+__device__ inline float scale_of(unsigned byte) { return __builtin_bit_cast(float, byte << 23); }
+
+typedef short s2 __attribute__((ext_vector_type(2)));
+typedef __bf16 b2 __attribute__((ext_vector_type(2)));
+typedef __bf16 b8 __attribute__((ext_vector_type(8)));
+typedef _Float16 h2 __attribute__((ext_vector_type(2)));
+
+// Four numbers over 2^e as e4m3, rounded once (at most 448 in size: nothing saturates)
+__device__ inline unsigned codes_of(float a, float b, float c, float d, float scale) {
+  s2 w = {0, 0};
+  w = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(w, a, b, scale, false);
+  return __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(w, c, d, scale, true));
+}
+// ... of two dwords of bf16 or fp16
+template <int TYPE>
+__device__ inline unsigned codes_of_pairs(unsigned a, unsigned b, float scale) {
+  s2 w = {0, 0};
+  if (TYPE == QG_BF16) {
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(w, __builtin_bit_cast(b2, a), scale, false);
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(w, __builtin_bit_cast(b2, b), scale, true);
+  } else {
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp8_f16(w, __builtin_bit_cast(h2, a), scale, false);
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp8_f16(w, __builtin_bit_cast(h2, b), scale, true);
+  }
+  return __builtin_bit_cast(unsigned, w);
+}
+// Two of the four codes of a dword (`high`: the upper two) times 2^e as bf16: exact
+__device__ inline unsigned widened(unsigned codes, float scale, bool high) {
+  return __builtin_bit_cast(unsigned, high ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)codes, scale, true)
+                                           : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)codes, scale, false));
+}
+__device__ inline unsigned size_bits(float x) { return __builtin_bit_cast(unsigned, x) & 0x7fffffffu; }
+__device__ inline unsigned umax(unsigned a, unsigned b) { return a > b ? a : b; }
+
+// The largest over the lanes that differ in bits 4 and 5 of their number
+__device__ inline unsigned max_over_quads(unsigned x) {
+  x = umax(x, (unsigned)__shfl_xor((int)x, 16));
+  return umax(x, (unsigned)__shfl_xor((int)x, 32));
+}
+
+__device__ inline f4 matrix_product(i8v a, i8v b, f4 c, int which_a, unsigned scale_a, unsigned scale_b) {
+  switch (which_a) {  // (the byte of scale_a is part of the instruction)
+    case 0: return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, c, 0, 0, 0, (int)scale_a, 0, (int)scale_b);
+    case 1: return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, c, 0, 0, 1, (int)scale_a, 0, (int)scale_b);
+    case 2: return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, c, 0, 0, 2, (int)scale_a, 0, (int)scale_b);
+    default: return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, c, 0, 0, 3, (int)scale_a, 0, (int)scale_b);
+  }
+}
+
+// Codes of a lane's 32 numbers of K as the bf16 matrix instructions take them, eight at a time.  The 8-bit instructions align the products
+// of eight neighbours to the largest of them and drop what lies 2^-13 below its leading bit (measured; the sums of eight, and the
+// accumulator, are fp32): 2e-5 of a typical result, nothing for 16-bit results, too much for fp32 ones.  bf16 holds e4m3 times a power of
+// two exactly, and its instructions sum in fp32: 5e-7, at half the rate.
+struct wide {
+  b8 x[4];
+  __device__ inline wide() {}
+  __device__ inline wide(u4 low, u4 high, float scale) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const unsigned a = h ? high[2 * i] : low[2 * i], b = h ? high[2 * i + 1] : low[2 * i + 1];
+        const u4 w = {widened(a, scale, false), widened(a, scale, true), widened(b, scale, false), widened(b, scale, true)};
+        x[2 * h + i] = __builtin_bit_cast(b8, w);
+      }
+  }
+};
+__device__ inline f4 wide_product(const wide& a, const wide& b, f4 c) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.x[i], b.x[i], c, 0, 0, 0);
+  return c;
+}
+
+__device__ inline i8v both(u4 low, u4 high) {
+  i8v x;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) x[i] = (int)low[i], x[i + 4] = (int)high[i];
+  return x;
+}
+
+// ---- activations: value and slope, in fp32
+constexpr float SQRT_HALF = 0.70710678118654752f, INV_SQRT_2PI = 0.39894228040143268f, TANH_R = 0.79788456080286536f, TANH_C = 0.044715f;
+
+// 1 / (1 + exp(-z)): of z far below zero exp(-z) is infinite and the result 0
+__device__ inline float logistic(float z) { return 1.0f / (1.0f + __expf(-z)); }
+
+template <bool SLOPE>
+__device__ inline float activate(int kind, float g, float* slope) {
+  if (kind == QG_SILU) {
+    const float p = logistic(g);
+    if (SLOPE) *slope = p * (1.0f + g * (1.0f - p));
+    return g * p;
+  }
+  if (kind == QG_GELU) {
+    const float p = 0.5f * erfcf(-g * SQRT_HALF);
+    if (SLOPE) *slope = p + g * __expf(-0.5f * g * g) * INV_SQRT_2PI;
+    return g * p;
+  }
+  if (kind == QG_GELU_TANH) {  // (1 + tanh z) / 2 = 1 / (1 + exp(-2 z))
+    const float p = logistic(2.0f * TANH_R * (g + TANH_C * g * g * g));
+    // (far out p (1 - p) is 0, and the square must not be infinite beside it)
+    if (SLOPE) *slope = p + 2.0f * g * p * (1.0f - p) * TANH_R * (1.0f + 3.0f * TANH_C * fminf(g * g, 1e8f));
+    return g * p;
+  }
+  if (SLOPE) *slope = g > 0.0f ? 1.0f : g <= 0.0f ? 0.0f : g;  // (of a NaN: NaN)
+  return g > 0.0f ? g : g <= 0.0f ? 0.0f : g;
+}
+
+// ---- N consecutive results of a row, as far as the row has columns
+template <int TYPE, int N>
+__device__ inline void put(const qg_fp8_rows& to, int row, int column, int columns, const float* v) {
+  typedef typename qg_elem<TYPE>::t T;
+  T* out = static_cast<T*>(to.data) + row * to.stride + column;
+  if (column + N <= columns) {
+    qg_store<TYPE, N>(out, v);
+  } else {
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+      if (column + i < columns) out[i] = qg_elem<TYPE>::down(v[i]);
+  }
+}
+template <int N>
+__device__ inline void put(int type, const qg_fp8_rows& to, int row, int column, int columns, const float* v) {
+  if (type == QG_F32) put<QG_F32, N>(to, row, column, columns, v);
+  if (type == QG_BF16) put<QG_BF16, N>(to, row, column, columns, v);
+  if (type == QG_F16) put<QG_F16, N>(to, row, column, columns, v);
+}
+
+}  // namespace
+#endif

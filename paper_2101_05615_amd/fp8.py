@@ -1,0 +1,382 @@
+"""Products of 8-bit floats with a scale for each block of 128, the gated feed-forward block over them, and activations kept in 8 bits for
+the backward pass (include/qgemm.h, the qg_fp8_* calls).
+
+    w_in, w_out = fp8.pack_gated(gate, up), fp8.pack(down)                 # once per model; matrices are [in, out]
+    ws = fp8.workspace()                                                   # once per stream
+    y = fp8.feed_forward(x, w_in, w_out, workspace=ws)                     # serving: down(silu(x gate) * (x up))
+    y = fp8.matmul(x, fp8.pack(b), workspace=ws)                           # one projection
+
+    y = fp8.linear(x, b, workspace=ws)                                     # training: differentiable, b is what the optimizer holds
+    y = fp8.gated_mlp(x, gate, up, down, workspace=ws)                     # ... what it keeps for the backward pass is x in 8 bits
+
+Activations are [tokens, channels] in float32, bfloat16 or float16 with a unit stride of channels; a view of wider rows is taken as it
+is.  Weights may have any strides.  A product computes with the 8-bit values of both; results are of x's type unless said otherwise.
+In the training calls gradients of 8-bit values pass to what they stand for, the gradient that comes in is put into 8 bits for the
+product with the weights, and taken as it is for the weights' own gradient.
+Argument marshalling only, like qgemm.py.
+"""
+import ctypes
+
+import torch
+from torch.autograd import forward_ad
+
+from .qgemm import QGemmError, _binding, _check, _stream, lib
+
+F32, BF16, F16 = 0, 1, 2
+_TYPES = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}
+BLOCK = 128
+FEW = 16                                       # QG_FP8_FEW
+COUNTER_BYTES = 16384                          # QG_FP8_COUNTER_BYTES
+WORKSPACE_BYTES = COUNTER_BYTES + (32 << 20)   # QG_FP8_WORKSPACE_BYTES
+ACTIVATIONS = {"silu": 0, "gelu": 1, "gelu_tanh": 2, "relu": 3}
+
+
+class _Rows(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("token_stride", ctypes.c_int64)]
+
+
+class _BlocksDesc(ctypes.Structure):
+    _fields_ = [("codes", ctypes.c_void_p), ("scales", ctypes.c_void_p), ("tokens", ctypes.c_int32), ("channels", ctypes.c_int32)]
+
+
+class _WeightDesc(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("k", ctypes.c_int32), ("n", ctypes.c_int32), ("gated", ctypes.c_int32)]
+
+
+class _Matrix(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("row_stride", ctypes.c_int64), ("column_stride", ctypes.c_int64)]
+
+
+class _Product(ctypes.Structure):
+    _fields_ = [("x", _BlocksDesc), ("x_rows", _Rows), ("x_dtype", ctypes.c_int32), ("tokens", ctypes.c_int32), ("out", _Rows),
+                ("dtype", ctypes.c_int32), ("activation", ctypes.c_int32), ("wide_sums", ctypes.c_int32), ("bias", ctypes.c_void_p), ("workspace", ctypes.c_void_p),
+                ("workspace_bytes", ctypes.c_size_t)]
+
+
+def _declare():
+    vp, i, P, sz = ctypes.c_void_p, ctypes.c_int, ctypes.POINTER, ctypes.c_size_t
+    for f in (lib.qg_fp8_codes_bytes, lib.qg_fp8_scales_bytes):
+        f.argtypes, f.restype = [i, i], sz
+    lib.qg_fp8_weight_bytes.argtypes, lib.qg_fp8_weight_bytes.restype = [i, i, i], sz
+    lib.qg_fp8_quantize.argtypes = [P(_Rows), i, P(_BlocksDesc), vp]
+    lib.qg_fp8_dequantize.argtypes = [P(_BlocksDesc), i, P(_Rows), vp]
+    lib.qg_fp8_pack.argtypes = [P(_Matrix), P(_Matrix), i, i, i, P(_WeightDesc), P(_WeightDesc), vp]
+    lib.qg_fp8_matmul.argtypes = [P(_WeightDesc), P(_Product), vp]
+    lib.qg_fp8_gated.argtypes = [P(_WeightDesc), P(_Product), P(_BlocksDesc), vp]
+    lib.qg_fp8_gated_backward.argtypes = [P(_WeightDesc), P(_Product), P(_Rows), i, vp, P(_BlocksDesc), P(_BlocksDesc), vp]
+    lib.qg_fp8_weight_gradient.argtypes = [P(_BlocksDesc), P(_Rows), i, i, P(_Rows), i, vp, sz, vp]
+
+
+_declare()
+
+
+class Blocks:
+    """Activations in 8 bits: codes uint8 [tokens, channels rounded up to 128] (e4m3), scales uint8 [tokens, blocks rounded up to 4]
+    (exponents + 127; 255: NaN)."""
+
+    def __init__(self, codes, scales, channels):
+        tokens = codes.shape[0]
+        assert codes.is_cuda and scales.is_cuda and codes.device == scales.device and codes.dtype == scales.dtype == torch.uint8
+        assert channels >= 1 and codes.is_contiguous() and tuple(codes.shape) == (tokens, _up(channels, BLOCK))
+        assert scales.is_contiguous() and tuple(scales.shape) == (tokens, _up(_up(channels, BLOCK) // BLOCK, 4))
+        self.codes, self.scales, self.shape, self.device = codes, scales, (tokens, channels), codes.device
+        self._desc = _BlocksDesc(codes.data_ptr(), scales.data_ptr(), tokens, channels)
+        self._ref = ctypes.byref(self._desc)
+
+
+class Weight:
+    """Weights in 8 bits in the library's own layout: B [k, n], or a pair of such matrices (gated).  transposed: the same for products
+    with the transpose, where it was asked for."""
+
+    def __init__(self, k, n, gated, device, transposed=None):
+        size = lib.qg_fp8_weight_bytes(k, n, int(gated))
+        if size == 0:
+            raise QGemmError(-2, "qg_fp8_weight_bytes")
+        self.data = torch.empty(size, dtype=torch.uint8, device=device)
+        self.k, self.n, self.gated, self.transposed, self.device = k, n, bool(gated), transposed, self.data.device
+        self._desc = _WeightDesc(self.data.data_ptr(), k, n, int(gated))
+        self._ref = ctypes.byref(self._desc)
+
+
+def _up(x, m):
+    return (x + m - 1) // m * m
+
+
+def _on(device):
+    """The calls run on the current stream of the current device: their tensors must be there."""
+    if device.type != "cuda":
+        raise RuntimeError(f"fp8: tensors are on {device}, the calls run on a GPU")
+    if device.index != torch.cuda.current_device():
+        raise RuntimeError(f"fp8: tensors are on {device}, the current device is cuda:{torch.cuda.current_device()}")
+
+
+def _check_rows(x, tokens=None, channels=None):
+    assert x.dim() == 2 and x.dtype in _TYPES and (x.stride(1) == 1 or x.shape[1] <= 1 or x.shape[0] == 0), "[tokens, channels] with a unit stride of channels"
+    assert (tokens is None or x.shape[0] == tokens) and (channels is None or x.shape[1] == channels)
+    _on(x.device)
+
+
+def _rows(x):
+    return _Rows(x.data_ptr(), x.stride(0))
+
+
+def _matrix(b):
+    return _Matrix(b.data_ptr(), b.stride(0), b.stride(1))
+
+
+def _no_gradient(name, *tensors):
+    for t in tensors:
+        if isinstance(t, torch.Tensor) and ((t.requires_grad and torch.is_grad_enabled()) or
+                                            (forward_ad._current_level >= 0 and forward_ad.unpack_dual(t).tangent is not None)):
+            raise RuntimeError(f"fp8.{name} has no gradient: fp8.linear and fp8.gated_mlp have")
+
+
+def new_blocks(tokens, channels, device="cuda"):
+    """Room for [tokens, channels] in 8 bits."""
+    if channels < 1 or channels > 1 << 20 or tokens < 0 or tokens > 1 << 28:
+        raise QGemmError(-2, "qg_fp8_codes_bytes")
+    pitch = _up(channels, BLOCK)
+    codes = torch.empty((tokens, pitch), dtype=torch.uint8, device=device)
+    return Blocks(codes, torch.empty((tokens, _up(pitch // BLOCK, 4)), dtype=torch.uint8, device=codes.device), channels)
+
+
+def quantize(x, out=None):
+    """x [tokens, channels] in 8 bits."""
+    x = x.detach()
+    _check_rows(x)
+    if out is None:
+        out = new_blocks(x.shape[0], x.shape[1], x.device)
+    else:
+        assert out.shape == tuple(x.shape) and out.device == x.device
+    _check(lib.qg_fp8_quantize(ctypes.byref(_rows(x)), _TYPES[x.dtype], out._ref, _stream()), "qg_fp8_quantize")
+    return out
+
+
+def dequantize(x, dtype=torch.float32, out=None):
+    """The values that x stands for, [tokens, channels] of `dtype`."""
+    _on(x.device)
+    if out is None:
+        out = torch.empty(x.shape, dtype=dtype, device=x.device)
+    else:
+        _check_rows(out, *x.shape)
+        assert out.dtype == dtype and out.device == x.device
+    _check(lib.qg_fp8_dequantize(x._ref, _TYPES[dtype], ctypes.byref(_rows(out)), _stream()), "qg_fp8_dequantize")
+    return out
+
+
+def _pack(b, up, transposed, only_transposed=False):
+    assert b.dim() == 2 and b.dtype in _TYPES
+    k, n = b.shape
+    if up is not None:
+        assert up.shape == b.shape and up.dtype == b.dtype and up.device == b.device
+    _on(b.device)
+    t = None
+    if transposed:
+        t = Weight(2 * _up(n, BLOCK) if up is not None else n, k, False, b.device)
+    w = Weight(k, n, up is not None, b.device, t)
+    u = None if up is None else ctypes.byref(_matrix(up))
+    _check(lib.qg_fp8_pack(ctypes.byref(_matrix(b)), u, k, n, _TYPES[b.dtype], w._ref, None if t is None else t._ref, _stream()), "qg_fp8_pack")
+    return w
+
+
+def pack(b, transposed=False):
+    """Weights B [in, out] in 8 bits; transposed: for products with the transpose too."""
+    return _pack(b.detach(), None, transposed)
+
+
+def pack_gated(gate, up, transposed=False):
+    """The two input matrices [in, inner] of a gated block."""
+    return _pack(gate.detach(), up.detach(), transposed)
+
+
+def workspace(device="cuda"):
+    """A workspace for the calls below, of any extents.  One per stream that calls run on."""
+    ws = torch.empty(WORKSPACE_BYTES, dtype=torch.uint8, device=device)
+    with torch.cuda.device(ws.device):
+        _check(lib.qg_gemm_workspace_init(ws.data_ptr(), COUNTER_BYTES, _stream()), "qg_gemm_workspace_init")
+    return ws
+
+
+def _product(x, w, dtype, activation=0, bias=None, ws=None, out=None, wide_sums=False):
+    """Parameters of a product of x (a tensor, or Blocks) and w, and what has to live until it is issued."""
+    p = _Product()
+    tokens, k = x.shape
+    assert k == w.k, f"x has {k} channels, the weights take {w.k}"
+    assert x.device == w.device
+    if isinstance(x, Blocks):
+        _on(x.device)
+        held = x
+    else:
+        _check_rows(x)
+        held = None if tokens <= FEW else quantize(x)
+    if held is not None:
+        p.x = held._desc
+    else:
+        p.x_rows, p.x_dtype = _rows(x), _TYPES[x.dtype]
+    p.tokens, p.activation, p.wide_sums = tokens, activation, int(wide_sums)
+    if out is not None:
+        p.out, p.dtype = _rows(out), _TYPES[dtype]
+    if bias is not None:
+        assert bias.dtype == torch.float32 and bias.is_contiguous() and tuple(bias.shape) == (w.n,) and bias.device == x.device
+        p.bias = bias.data_ptr()
+    if ws is not None:
+        assert ws.is_cuda and ws.is_contiguous() and ws.device == x.device
+        p.workspace, p.workspace_bytes = ws.data_ptr(), ws.numel() * ws.element_size()
+    return p, held
+
+
+def _out(x, w, dtype, out):
+    dtype = dtype if dtype is not None else out.dtype if out is not None else torch.bfloat16 if isinstance(x, Blocks) else x.dtype
+    assert dtype in _TYPES
+    if out is None:
+        return torch.empty((x.shape[0], w.n), dtype=dtype, device=x.device)
+    _check_rows(out, x.shape[0], w.n)
+    assert out.dtype == dtype and out.device == x.device
+    return out
+
+
+def matmul(x, w, bias=None, dtype=None, out=None, workspace=None, wide_sums=None):
+    """x B + bias: x [tokens, in] or Blocks; bias float32 [out].  dtype: of the result, by default x's (of Blocks: bfloat16).  wide_sums:
+    sums all in fp32, at half the rate of the 8-bit matrix cores, whose own are about 2e-5 off (default: where the result is float32)."""
+    _no_gradient("matmul", x, bias, out)
+    assert not w.gated
+    out = _out(x, w, dtype, out)
+    p, _held = _product(x, w, out.dtype, bias=bias, ws=workspace, out=out, wide_sums=out.dtype == torch.float32 if wide_sums is None else wide_sums)
+    _check(lib.qg_fp8_matmul(w._ref, ctypes.byref(p), _stream()), "qg_fp8_matmul")
+    return out
+
+
+def gated(x, w, activation="silu", dtype=None, out=None, workspace=None, wide_sums=None):
+    """activation(x Gate) * (x Up) in one kernel, [tokens, inner]; w from pack_gated().  `out` may be Blocks: the result in 8 bits.
+    wide_sums: as in matmul()."""
+    _no_gradient("gated", x, out)
+    assert w.gated
+    if isinstance(out, Blocks):
+        assert dtype is None and out.shape == (x.shape[0], w.n) and out.device == x.device
+        x = x if isinstance(x, Blocks) else quantize(x)
+        p, _held = _product(x, w, None, ACTIVATIONS[activation], ws=workspace, wide_sums=bool(wide_sums))
+        _check(lib.qg_fp8_gated(w._ref, ctypes.byref(p), out._ref, _stream()), "qg_fp8_gated")
+        return out
+    out = _out(x, w, dtype, out)
+    p, _held = _product(x, w, out.dtype, ACTIVATIONS[activation], ws=workspace, out=out,
+                        wide_sums=out.dtype == torch.float32 if wide_sums is None else wide_sums)
+    _check(lib.qg_fp8_gated(w._ref, ctypes.byref(p), None, _stream()), "qg_fp8_gated")
+    return out
+
+
+def gated_backward(x, w, dh, activation="silu", workspace=None):
+    """The backward pass of gated() from x in 8 bits (Blocks) and the gradient dh [tokens, inner] of its result: (dgu, dgu8, h8).  dgu
+    bfloat16 [tokens, 2, inner rounded up to 128] holds the gradients of x Gate and of x Up, dgu8 their 8-bit form (Blocks
+    [tokens, 2 * inner rounded up to 128], for matmul() with w.transposed: the gradient of x), h8 the block's result in 8 bits."""
+    _no_gradient("gated_backward", dh)
+    assert w.gated and isinstance(x, Blocks)
+    T, inner = x.shape[0], _up(w.n, BLOCK)
+    _check_rows(dh, T, w.n)
+    assert dh.device == x.device
+    dgu = torch.empty((T, 2, inner), dtype=torch.bfloat16, device=x.device)
+    dgu8, h8 = new_blocks(T, 2 * inner, x.device), new_blocks(T, w.n, x.device)
+    p, _held = _product(x, w, None, ACTIVATIONS[activation], ws=workspace)
+    _check(lib.qg_fp8_gated_backward(w._ref, ctypes.byref(p), ctypes.byref(_rows(dh)), _TYPES[dh.dtype], dgu.data_ptr(), dgu8._ref, h8._ref,
+                                     _stream()), "qg_fp8_gated_backward")
+    return dgu, dgu8, h8
+
+
+def weight_gradient(x, dy, dtype=None, out=None, workspace=None):
+    """x^T dy [in, out]: the gradient of the weights of x B from x in 8 bits (Blocks) and the gradient dy [tokens, out] of the product.
+    dtype: of the result, by default dy's."""
+    _no_gradient("weight_gradient", dy, out)
+    assert isinstance(x, Blocks) and x.device == dy.device
+    _check_rows(dy, x.shape[0])
+    dtype = dtype if dtype is not None else out.dtype if out is not None else dy.dtype
+    if out is None:
+        out = torch.empty((x.shape[1], dy.shape[1]), dtype=dtype, device=dy.device)
+    else:
+        _check_rows(out, x.shape[1], dy.shape[1])
+        assert out.dtype == dtype and out.device == dy.device
+    ws, size = None, 0
+    if workspace is not None:
+        assert workspace.is_cuda and workspace.is_contiguous() and workspace.device == dy.device
+        ws, size = workspace.data_ptr(), workspace.numel() * workspace.element_size()
+    _check(lib.qg_fp8_weight_gradient(x._ref, ctypes.byref(_rows(dy)), _TYPES[dy.dtype], dy.shape[1], ctypes.byref(_rows(out)), _TYPES[dtype],
+                                      ws, size, _stream()), "qg_fp8_weight_gradient")
+    return out
+
+
+def feed_forward(x, w_in, w_out, activation="silu", dtype=None, out=None, workspace=None):
+    """(activation(x Gate) * (x Up)) Down: w_in from pack_gated(), w_out from pack().  What is between goes into the second product in 8
+    bits, made from its fp32 value."""
+    _no_gradient("feed_forward", x, out)
+    assert w_in.gated and not w_out.gated and w_out.k == w_in.n
+    out = _out(x, w_out, dtype, out)
+    if x.shape[0] <= 4 * FEW:
+        h = gated(x, w_in, activation, dtype=torch.float32, workspace=workspace)
+    else:
+        h = gated(x, w_in, activation, out=new_blocks(x.shape[0], w_in.n, x.device), workspace=workspace)
+    return matmul(h, w_out, out=out, workspace=workspace)
+
+
+def _unit(g):
+    return g if g.stride(1) == 1 or g.shape[1] <= 1 else g.contiguous()          # (of a sum, say: one number with strides of 0)
+
+
+class _Linear(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, b, ws):
+        w = pack(b, transposed=ctx.needs_input_grad[0])
+        x8 = quantize(x)
+        ctx.x8 = x8 if ctx.needs_input_grad[1] else None
+        ctx.w, ctx.ws, ctx.types = w.transposed, ws, (x.dtype, b.dtype)
+        return matmul(x8, w, dtype=x.dtype, workspace=ws)
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dy):
+        dy = _unit(dy)
+        dx = matmul(quantize(dy), ctx.w, dtype=ctx.types[0], workspace=ctx.ws) if ctx.needs_input_grad[0] else None
+        db = weight_gradient(ctx.x8, dy, dtype=ctx.types[1], workspace=ctx.ws) if ctx.needs_input_grad[1] else None
+        return dx, db, None
+
+
+def linear(x, b, workspace=None):
+    """x B, differentiable in x and in the weights b [in, out], which are put into 8 bits here.  Kept for the backward pass: x and the
+    weights' transpose in 8 bits."""
+    _check_rows(x)
+    assert b.dim() == 2 and b.shape[0] == x.shape[1]
+    return _Linear.apply(x, b, workspace)
+
+
+class _GatedMlp(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, gate, up, down, activation, ws):
+        back = any(ctx.needs_input_grad)
+        w_in, w_out = pack_gated(gate, up, transposed=ctx.needs_input_grad[0]), pack(down, transposed=back)
+        x8 = quantize(x)
+        h8 = gated(x8, w_in, activation, out=new_blocks(x.shape[0], gate.shape[1], x.device), workspace=ws)
+        if back:
+            ctx.x8, ctx.w_in, ctx.w_out = x8, w_in, w_out.transposed
+        ctx.activation, ctx.ws, ctx.types = activation, ws, (x.dtype, gate.dtype, down.dtype)
+        return matmul(h8, w_out, dtype=x.dtype, workspace=ws)
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dy):
+        dy = _unit(dy)
+        need, ws, n = ctx.needs_input_grad, ctx.ws, ctx.w_in.n
+        # (fp32: what follows goes into 8 bits from its fp32 value)
+        dh = matmul(quantize(dy), ctx.w_out, dtype=torch.float32, workspace=ws, wide_sums=False)
+        dgu, dgu8, h8 = gated_backward(ctx.x8, ctx.w_in, dh, ctx.activation, workspace=ws)
+        del dh
+        dx = matmul(dgu8, ctx.w_in.transposed, dtype=ctx.types[0], workspace=ws) if need[0] else None
+        dgate = weight_gradient(ctx.x8, dgu[:, 0, :n], dtype=ctx.types[1], workspace=ws) if need[1] else None
+        dup = weight_gradient(ctx.x8, dgu[:, 1, :n], dtype=ctx.types[1], workspace=ws) if need[2] else None
+        ddown = weight_gradient(h8, dy, dtype=ctx.types[2], workspace=ws) if need[3] else None
+        return dx, dgate, dup, ddown, None, None
+
+
+def gated_mlp(x, gate, up, down, activation="silu", workspace=None):
+    """(activation(x Gate) * (x Up)) Down, differentiable in x and in the weights gate, up [in, inner] and down [inner, out], which are put
+    into 8 bits here.  Kept for the backward pass: x and the weights in 8 bits; the rest is computed again."""
+    _check_rows(x)
+    assert gate.dim() == 2 and gate.shape[0] == x.shape[1] and up.shape == gate.shape and down.dim() == 2 and down.shape[0] == gate.shape[1]
+    assert activation in ACTIVATIONS
+    return _GatedMlp.apply(x, gate, up, down, activation, workspace)
