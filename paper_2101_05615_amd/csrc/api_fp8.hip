@@ -85,10 +85,12 @@ int product(const qg_fp8_product_args& args, int end, int wide_sums, void* works
     if (sets * a.slices > 0x3fffffll) return QG_EUNSUPPORTED;
     return done(qg_launch_fp8_stream(a, end == QG_FP8_GATED, fragments, waves, s));
   }
-  const int fragments = a.tokens <= 32 ? 2 : a.tokens <= 64 ? 4 : 8;
   const long long columns = a.w.groups / 4;
+  const int fragments = !wide_sums && (a.tokens + 255ll) / 256 * columns >= 200 ? 16 : a.tokens <= 64 ? 4 : 8;
   const long long rows = (a.tokens + 16ll * fragments - 1) / (16 * fragments);
-  deal(&a, workspace, rows * columns, fragments * 4096ll, 256, 4);
+  a.slices = 1;
+  a.slice_kb = a.w.kb;
+  if (fragments < 16) deal(&a, workspace, rows * columns, fragments * 4096ll, 256, 4);
   if (rows * columns * a.slices > 0x7fffffll) return QG_EUNSUPPORTED;
   return done(qg_launch_fp8_tile(a, end, fragments, wide_sums, s));
 }
@@ -261,11 +263,11 @@ int qg_fp8_weight_gradient(const qg_fp8_blocks* x, const qg_rows* dy, int dy_dty
   a.tokens = x->tokens;
   a.k = x->channels;
   a.n = n;
-  const int tile = 128;
+  const int tile = (long long)((a.k + 255) / 256) * ((n + 255) / 256) >= 200 ? 256 : 128;
   const long long tiles = (long long)((a.k + tile - 1) / tile) * ((a.n + tile - 1) / tile);
   a.slices = 1;
   a.slice_tokens = qg_fp8_up(a.tokens, 64);
-  if (workspace && tiles <= COUNTERS) {
+  if (workspace && tile == 128 && tiles <= COUNTERS) {
     long long slices = 512 / tiles;
     if (slices > a.tokens / 256) slices = a.tokens / 256;
     if (slices > PARTIALS / (tiles * tile * tile)) slices = PARTIALS / (tiles * tile * tile);
@@ -277,7 +279,7 @@ int qg_fp8_weight_gradient(const qg_fp8_blocks* x, const qg_rows* dy, int dy_dty
     }
   }
   if (tiles * a.slices > 0x7fffffll) return QG_EUNSUPPORTED;
-  return done(qg_launch_fp8_gradient(a, static_cast<hipStream_t>(stream)));
+  return done(qg_launch_fp8_gradient(a, tile, static_cast<hipStream_t>(stream)));
 }
 
 }  // extern "C"

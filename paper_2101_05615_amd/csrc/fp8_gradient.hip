@@ -13,6 +13,13 @@ typedef float f16v __attribute__((ext_vector_type(16)));
 
 constexpr int TILE_K = 16;  // tokens of a matrix instruction
 
+__device__ const uint8_t no_numbers[64] __attribute__((aligned(16))) = {};
+// (said to be in memory, or the compiler takes a selected address for one that could lie in LDS)
+template <typename V>
+__device__ inline V from_memory(const void* p) { return *(const __attribute__((address_space(1))) V*)p; }
+typedef u4 u4_any __attribute__((aligned(2)));
+typedef u2 u2_any __attribute__((aligned(2)));
+
 __device__ inline unsigned pair_low(unsigned a, unsigned b) { return __builtin_amdgcn_perm(b, a, 0x05040100u); }   // low halves
 __device__ inline unsigned pair_high(unsigned a, unsigned b) { return __builtin_amdgcn_perm(b, a, 0x07060302u); }  // high halves
 
@@ -27,54 +34,76 @@ template <int TYPE, int PARTS, int CW>
 struct dy_line {
   static constexpr int BYTES = CW * (int)sizeof(typename qg_elem<TYPE>::t);
   unsigned raw[BYTES / 4];
-  __device__ inline void load(const void* base, long long at, int left) {
-    typedef typename qg_elem<TYPE>::t T;
-    const T* from = static_cast<const T*>(base) + at;
-    if (left >= CW) {
-      typedef unsigned vec __attribute__((ext_vector_type(BYTES / 4 < 4 ? BYTES / 4 : 4)));
-      typedef vec vec_any __attribute__((aligned(sizeof(T))));
-      constexpr int W = BYTES / 4 < 4 ? BYTES / 4 : 4;
+  typedef typename qg_elem<TYPE>::t T;
+  __device__ inline void load(const T* from) {
+    if constexpr (BYTES == 16) {
+      const u4 v = from_memory<u4_any>(from);
 #pragma unroll
-      for (int i = 0; i < BYTES / 4; i += W) {
-        const vec v = *reinterpret_cast<const vec_any*>(reinterpret_cast<const uint8_t*>(from) + 4 * i);
-#pragma unroll
-        for (int j = 0; j < W; ++j) raw[i + j] = v[j];
-      }
+      for (int i = 0; i < 4; ++i) raw[i] = v[i];
     } else {
-      T v[CW];
-#pragma unroll
-      for (int i = 0; i < CW; ++i) v[i] = i < left ? from[i] : (T)0.0f;
-      __builtin_memcpy(raw, v, BYTES);
+      static_assert(BYTES == 8, "a line");
+      const u2 v = from_memory<u2_any>(from);
+      raw[0] = v[0];
+      raw[1] = v[1];
     }
   }
-  __device__ inline void split(unsigned (*out)[CW / 2]) const {  // [PARTS][CW / 2]
-    if constexpr (TYPE == QG_BF16) {
+  __device__ inline void load_some(const T* from, int last) {  // fewer columns than CW; behind the last one: that one again
+    if constexpr (TYPE == QG_F32) {
 #pragma unroll
-      for (int i = 0; i < CW / 2; ++i) out[0][i] = raw[i];
+      for (int i = 0; i < CW; ++i) raw[i] = from_memory<unsigned>(from + min(i, last));
     } else {
-      typename qg_elem<TYPE>::t v[CW];
-      __builtin_memcpy(v, raw, BYTES);
 #pragma unroll
       for (int i = 0; i < CW / 2; ++i) {
-        float a = qg_elem<TYPE>::up(v[2 * i]), b = qg_elem<TYPE>::up(v[2 * i + 1]);
+        raw[i] = from_memory<unsigned short>(from + min(2 * i, last)) | (unsigned)from_memory<unsigned short>(from + min(2 * i + 1, last)) << 16;
+        asm volatile("" : "+v"(raw[i]));  // (put together here, not wherever they are used)
+      }
+    }
+  }
+  __device__ inline void split(int pair, unsigned (&out)[PARTS]) const {  // columns 2 pair and 2 pair + 1
+    if constexpr (TYPE == QG_BF16) {
+      out[0] = raw[pair];
+    } else {
+      float a, b;
+      if constexpr (TYPE == QG_F32) {
+        a = __builtin_bit_cast(float, raw[2 * pair]);
+        b = __builtin_bit_cast(float, raw[2 * pair + 1]);
+      } else {
+        const h2 v = __builtin_bit_cast(h2, raw[pair]);
+        a = (float)v[0];
+        b = (float)v[1];
+      }
 #pragma unroll
-        for (int p = 0; p < PARTS; ++p) {
-          out[p][i] = bf16_pair(a, b);
-          const float ra = bf16_up(out[p][i] & 0xffffu), rb = bf16_up(out[p][i] >> 16);
-          // (what does not fit: exact; of an infinity nothing, it would become NaN)
-          a = __builtin_isfinite(ra) ? a - ra : 0.0f;
-          b = __builtin_isfinite(rb) ? b - rb : 0.0f;
-        }
+      for (int p = 0; p < PARTS; ++p) {
+        out[p] = bf16_pair(a, b);
+        const float ra = bf16_up(out[p] & 0xffffu), rb = bf16_up(out[p] >> 16);
+        // (what does not fit: exact; of an infinity nothing, it would become NaN)
+        a = __builtin_isfinite(ra) ? a - ra : 0.0f;
+        b = __builtin_isfinite(rb) ? b - rb : 0.0f;
       }
     }
   }
 };
 
-// TS tokens of a stage; CW columns a thread: 256 threads cover TILE columns x TS tokens in blocks of CW x 8
+template <int TILE>
+__device__ inline void add_product(f16v& c, b8 a, b8 b) {
+  if constexpr (TILE == 256) {
+    // in place: with all 256 accumulator registers in use the compiler moves them about.  It does not know how long the result takes, which
+    // whoever reads it waits for, nor that operands are to be two cycles old if they were computed (free in the shadow of the product before).
+    asm volatile("s_nop 1\n\tv_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+a"(c) : "v"(a), "v"(b));
+  } else {
+    c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
+  }
+}
+
+// TS tokens of a stage; CW columns a thread: 256 threads cover TILE columns x TS tokens in blocks of CW x 8.  A wave has TILE / 2 squared of
+// the result.  While a stage is multiplied the next one, which is in registers, goes to the other half of LDS, and the one after that is
+// requested: both in pieces between the matrix instructions, in whose shadow they cost little.
+//   256 x 256, one wave per SIMD: LDS is read 64 KiB a stage and half-filled once, 96 of its 128 bytes a cycle; a wave of 64 x 64 would read
+//   as much for a quarter of the products.  128 x 128 where there are few tiles.
 template <int TILE, int TYPE, int PARTS>
-__global__ __launch_bounds__(256, PARTS == 1 ? 2 : 1) void qg_fp8_gradient_kernel(qg_fp8_gradient_args p, int row_tiles, int column_tiles) {
-  constexpr int CW = TILE == 256 && PARTS == 1 ? 8 : 4, TS = 256 * 8 * CW / TILE, WT = TILE / 2, F = WT / 32;
-  constexpr int PLANE = TILE * TS * 2, STAGE = PLANE * (1 + PARTS);
+__global__ __launch_bounds__(256, TILE == 256 || PARTS > 1 ? 1 : 2) void qg_fp8_gradient_kernel(qg_fp8_gradient_args p, int row_tiles, int column_tiles) {
+  constexpr int CW = TILE == 256 && PARTS == 1 ? 8 : 4, TS = 256 * 8 * CW / TILE, WT = TILE / 2, F = WT / 32, STEPS = TS / TILE_K;
+  constexpr int PLANE = TILE * TS * 2, STAGE = PLANE * (1 + PARTS), PAIRS = CW / 2, GROUPS = STEPS * F;
   static_assert(2 * STAGE <= 160 * 1024 - 64, "two stages");
   __shared__ __align__(1024) uint8_t lds[2 * STAGE];
   __shared__ int ticket;
@@ -83,84 +112,84 @@ __global__ __launch_bounds__(256, PARTS == 1 ? 2 : 1) void qg_fp8_gradient_kerne
   const int id = (int)blockIdx.x % (per * 8), slice = (int)blockIdx.x / (per * 8);
   const int at = id % 8 * per + id / 8;
   if (at >= tiles) return;
-  const int panel = at / (4 * column_tiles), in_panel = at - panel * 4 * column_tiles;
-  const int panel_rows = min(4, row_tiles - panel * 4);
-  const int row_tile = panel * 4 + in_panel % panel_rows, column_tile = in_panel / panel_rows;
+  const int panel = at / (8 * column_tiles), in_panel = at - panel * 8 * column_tiles;
+  const int panel_rows = min(8, row_tiles - panel * 8);
+  const int row_tile = panel * 8 + in_panel % panel_rows, column_tile = in_panel / panel_rows;
   const int t0 = slice * p.slice_tokens, t1 = min(t0 + p.slice_tokens, p.tokens);
 
   // what this thread fetches: columns c0 .. of both operands, tokens 8 * tb .. of a stage
-  const int chunks = TILE / CW, c0 = t % chunks * CW, tb = t / chunks;
-  const int xc = row_tile * TILE + c0, yc = column_tile * TILE + c0;
-  const bool x_there = xc < p.x8.pitch;
-  const int y_left = p.n - yc;
+  constexpr int CHUNKS = TILE / CW;
+  const int c0 = t % CHUNKS * CW, tb = t / CHUNKS;
+  // (chunks that would end behind the last column end there: two threads bring the same columns, and what lies behind is never written)
+  const int cx = min(c0, p.x8.pitch - CW - row_tile * TILE), cy = max(min(c0, p.n - CW - column_tile * TILE), 0);
+  const bool narrow = p.n < CW;
+  const int xc = row_tile * TILE + cx, yc = column_tile * TILE + cy;
+  typedef typename qg_elem<TYPE>::t T;
+  const uint8_t* const x_base = p.x8.codes + (long long)(t0 + 8 * tb) * p.x8.pitch + xc;
+  const uint8_t* const s_base = p.x8.scales + (long long)(t0 + 8 * tb) * p.x8.scale_pitch + xc / QG_FP8_BLOCK;
+  const T* const y_base = static_cast<const T*>(p.dy.data) + (long long)(t0 + 8 * tb) * p.dy.stride + yc;
   unsigned xraw[8][CW / 4], xs[8];
   dy_line<TYPE, PARTS, CW> y[8];
-  auto fetch = [&](int from) {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const int token = from + 8 * tb + i;
-      if (token < t1) {
-        if (x_there) {
-          const uint8_t* src = p.x8.codes + (size_t)token * p.x8.pitch + xc;
-          if constexpr (CW == 8) {
-            const u2 v = *reinterpret_cast<const u2*>(src);
-            xraw[i][0] = v[0];
-            xraw[i][1] = v[1];
-          } else {
-            xraw[i][0] = *reinterpret_cast<const unsigned*>(src);
-          }
-          xs[i] = p.x8.scales[(size_t)token * p.x8.scale_pitch + xc / QG_FP8_BLOCK];
-        } else {
-#pragma unroll
-          for (int d = 0; d < CW / 4; ++d) xraw[i][d] = 0u;
-          xs[i] = 0u;
-        }
-        y[i].load(p.dy.data, token * p.dy.stride + yc, y_left);
+  auto fetch_x = [&](const uint8_t* src, const uint8_t* scale, int i) {
+    if constexpr (CW == 8) {
+      const u2 v = from_memory<u2>(src);
+      xraw[i][0] = v[0];
+      xraw[i][1] = v[1];
+    } else {
+      xraw[i][0] = from_memory<unsigned>(src);
+    }
+    xs[i] = from_memory<uint8_t>(scale);
+  };
+  auto fetch = [&](int from, int i, bool inside) {  // token i of this thread's eight
+    const long long at = from - t0 + i;
+    const uint8_t *src = x_base + at * p.x8.pitch, *scale = s_base + at * p.x8.scale_pitch;
+    const T* dy = y_base + at * p.dy.stride;
+    if (inside && !narrow) {
+      fetch_x(src, scale, i);
+      y[i].load(dy);
+    } else {
+      const bool there = from + 8 * tb + i < t1;   // (a token behind the last: zeros)
+      fetch_x(there ? src : no_numbers, there ? scale : no_numbers, i);
+      dy = there ? dy : reinterpret_cast<const T*>(no_numbers);
+      if (narrow) {
+        y[i].load_some(dy, p.n - 1);
       } else {
-#pragma unroll
-        for (int d = 0; d < CW / 4; ++d) xraw[i][d] = 0u;
-        xs[i] = 0u;
-#pragma unroll
-        for (int d = 0; d < (int)(sizeof(y[i].raw) / 4); ++d) y[i].raw[d] = 0u;
+        y[i].load(dy);
       }
     }
   };
-  // a stage's planes: [32 columns][TS / 16 steps][2 halves of 8 tokens][32 columns, turned by the number of the 32][8 tokens]
-  auto place = [&](int column) {
+  // A stage's planes: [32 columns][TS / 16 steps][2 halves of 8 tokens][32 columns, turned by the number of the 32][8 tokens].  Two columns
+  // of this thread's eight tokens go there in SLICES pieces.
+  unsigned line[8], part[8][PARTS];
+  auto place = [&](uint8_t* plane, int column, unsigned a0, unsigned a1, unsigned a2, unsigned a3) {
     const int f = column / 32;
-    return (unsigned)((f * (TS / TILE_K) + tb / 2) * 1024 + (tb & 1) * 512 + ((column % 32) ^ (f & 7)) * 16);
+    *reinterpret_cast<u4*>(plane + (f * STEPS + tb / 2) * 1024 + (tb & 1) * 512 + ((column % 32) ^ (f & 7)) * 16) = (u4){a0, a1, a2, a3};
   };
-  auto put_plane = [&](uint8_t* plane, const unsigned (*line)[CW / 2]) {  // line[token][column pair]
+  constexpr int SLICES = 6 + 2 * PARTS;
+  auto store = [&](uint8_t* stage, int pair, int slice) {
+    if (slice < 2 || slice == 4 || slice == 5) {
 #pragma unroll
-    for (int j = 0; j < CW; ++j) {
-      u4 v;
-#pragma unroll
-      for (int d = 0; d < 4; ++d) v[d] = j & 1 ? pair_high(line[2 * d][j / 2], line[2 * d + 1][j / 2]) : pair_low(line[2 * d][j / 2], line[2 * d + 1][j / 2]);
-      *reinterpret_cast<u4*>(plane + place(c0 + j)) = v;
-    }
-  };
-  auto store = [&](uint8_t* stage) {
-    unsigned line[8][CW / 2];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const float s = scale_of(xs[i]);
-#pragma unroll
-      for (int d = 0; d < CW / 4; ++d) {
-        line[i][2 * d] = widened(xraw[i][d], s, false);
-        line[i][2 * d + 1] = widened(xraw[i][d], s, true);
+      for (int i = 0; i < 4; ++i) {
+        const int k = slice % 2 * 4 + i;
+        if (slice < 2) {
+          line[k] = widened(xraw[k][pair / 2], scale_of(xs[k]), pair & 1);
+        } else {
+          y[k].split(pair, part[k]);
+        }
       }
-    }
-    put_plane(stage, line);
-    unsigned parts[8][PARTS][CW / 2];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) y[i].split(parts[i]);
-#pragma unroll
-    for (int q = 0; q < PARTS; ++q) {
-#pragma unroll
-      for (int i = 0; i < 8; ++i)
-#pragma unroll
-        for (int d = 0; d < CW / 2; ++d) line[i][d] = parts[i][q][d];
-      put_plane(stage + (1 + q) * PLANE, line);
+    } else if (slice == 2) {
+      place(stage, cx + 2 * pair, pair_low(line[0], line[1]), pair_low(line[2], line[3]), pair_low(line[4], line[5]), pair_low(line[6], line[7]));
+    } else if (slice == 3) {
+      place(stage, cx + 2 * pair + 1, pair_high(line[0], line[1]), pair_high(line[2], line[3]), pair_high(line[4], line[5]), pair_high(line[6], line[7]));
+    } else {
+      const int q = (slice - 6) / 2;
+      if (slice % 2 == 0) {
+        place(stage + (1 + q) * PLANE, cy + 2 * pair, pair_low(part[0][q], part[1][q]), pair_low(part[2][q], part[3][q]),
+            pair_low(part[4][q], part[5][q]), pair_low(part[6][q], part[7][q]));
+      } else {
+        place(stage + (1 + q) * PLANE, cy + 2 * pair + 1, pair_high(part[0][q], part[1][q]), pair_high(part[2][q], part[3][q]),
+            pair_high(part[4][q], part[5][q]), pair_high(part[6][q], part[7][q]));
+      }
     }
   };
 
@@ -173,36 +202,74 @@ __global__ __launch_bounds__(256, PARTS == 1 ? 2 : 1) void qg_fp8_gradient_kerne
       for (int e = 0; e < 16; ++e) c[i][j][e] = 0.0f;
   const int wr = wave >> 1, wc = wave & 1;
   auto operand = [&](const uint8_t* plane, int f, int step) {
-    return *reinterpret_cast<const b8*>(plane + (f * (TS / TILE_K) + step) * 1024 + (lane >> 5) * 512 + ((lane & 31) ^ (f & 7)) * 16);
+    return *reinterpret_cast<const b8*>(plane + (f * STEPS + step) * 1024 + (lane >> 5) * 512 + ((lane & 31) ^ (f & 7)) * 16);
   };
   if (t0 < t1) {
-    fetch(t0);
-    store(lds);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) fetch(t0, i, t0 + TS <= t1);
+#pragma unroll
+    for (int u = 0; u < PAIRS; ++u)
+#pragma unroll
+      for (int e = 0; e < SLICES; ++e) store(lds, u, e);
+    if (t0 + TS < t1) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) fetch(t0 + TS, i, t0 + 2 * TS <= t1);
+    }
     int now = 0;
+#pragma unroll 1
     for (int from = t0; from < t1; from += TS, now ^= 1) {
-      const bool more = from + TS < t1;
-      if (more) fetch(from + TS);
+      // (past the end: the last stage's numbers again, into the half that nobody reads any more)
+      const int ahead = min(from + 2 * TS, t0 + (t1 - 1 - t0) / TS * TS);
+      const bool inside = !narrow && ahead + TS <= t1;
       __syncthreads();
-      const uint8_t* stage = lds + now * STAGE;
+      const uint8_t* const stage = lds + now * STAGE;
+      uint8_t* const other = lds + (now ^ 1) * STAGE;
+      b8 x[2][F], g[2][PARTS];
 #pragma unroll
-      for (int s = 0; s < TS / TILE_K; ++s) {
-        b8 x[F];
+      for (int i = 0; i < F; ++i) x[0][i] = operand(stage, wr * F + i, 0);
 #pragma unroll
-        for (int i = 0; i < F; ++i) x[i] = operand(stage, wr * F + i, s);
+      for (int q = 0; q < PARTS; ++q) g[0][q] = operand(stage + (1 + q) * PLANE, wc * F, 0);
+      // the matrix instructions of a stage, one by one: the first half with pieces of the next stage's way to LDS, the second with requests
+      constexpr int PRODUCTS = GROUPS * PARTS * F, HALF = PRODUCTS / 2, ALL = PAIRS * SLICES;
+      each<0, PRODUCTS>([&](auto number) {
+        constexpr int n = decltype(number)::value, group = n / (PARTS * F), q = n / F % PARTS, i = n % F, s = group / F, j = group % F;
+        if constexpr (n % (PARTS * F) == 0) {
+          if constexpr (group + 1 < GROUPS) {
 #pragma unroll
-        for (int j = 0; j < F; ++j)
-#pragma unroll
-          for (int q = 0; q < PARTS; ++q) {
-            const b8 g = operand(stage + (1 + q) * PLANE, wc * F + j, s);
-#pragma unroll
-            for (int i = 0; i < F; ++i) c[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(g, x[i], c[i][j], 0, 0, 0);
+            for (int k = 0; k < PARTS; ++k) g[(group + 1) & 1][k] = operand(stage + (1 + k) * PLANE, wc * F + (group + 1) % F, (group + 1) / F);
           }
-      }
-      if (more) store(lds + (now ^ 1) * STAGE);
+          if constexpr (s + 1 < STEPS) x[(s + 1) & 1][j] = operand(stage, wr * F + j, s + 1);  // a part of the next step's rows with every group
+        }
+        if constexpr (n < HALF) {
+          constexpr int first = n * ALL / HALF, last = (n + 1) * ALL / HALF;
+          each<first, last>([&](auto piece) {
+            constexpr int e = decltype(piece)::value;
+            store(other, e / SLICES, e % SLICES);
+          });
+        } else {
+          constexpr int first = (n - HALF) * 8 / HALF, last = (n - HALF + 1) * 8 / HALF;
+          if constexpr (first < last) {
+            if (inside) {
+              each<first, last>([&](auto token) { fetch(ahead, decltype(token)::value, true); });
+            } else {
+              each<first, last>([&](auto token) { fetch(ahead, decltype(token)::value, false); });
+            }
+          }
+        }
+        add_product<TILE>(c[i][j], g[group & 1][q], x[s & 1][i]);
+        __builtin_amdgcn_sched_barrier(0);
+      });
     }
   }
+  if constexpr (TILE == 256) {
+    asm volatile("s_nop 15\n\ts_nop 15" ::: "memory");
+#pragma unroll
+    for (int i = 0; i < F; ++i)
+#pragma unroll
+      for (int j = 0; j < F; ++j) asm volatile("" : "+a"(c[i][j]));
+  }
   // a lane has, of fragment (i, j), row 32 i + lane % 32 and the columns 32 j + 8 (e / 4) + 4 (lane / 32) + e % 4
-  if (p.slices > 1) {  // sums of the slices through memory; the last one to arrive adds them in order
+  if (TILE == 128 && p.slices > 1) {  // sums of the slices through memory; the last one to arrive adds them in order
     const int tile = row_tile * column_tiles + column_tile;
     const size_t step = (size_t)TILE * TILE;
     float* const mine = p.partial + (size_t)tile * p.slices * step + (size_t)wave * (F * F * 1024) + lane * 4;
@@ -274,6 +341,6 @@ hipError_t launch(const qg_fp8_gradient_args& a, hipStream_t s) {
 
 }  // namespace
 
-hipError_t qg_launch_fp8_gradient(const qg_fp8_gradient_args& a, hipStream_t s) {
-  return launch<128>(a, s);
+hipError_t qg_launch_fp8_gradient(const qg_fp8_gradient_args& a, int tile, hipStream_t s) {
+  return tile == 256 ? launch<256>(a, s) : launch<128>(a, s);
 }

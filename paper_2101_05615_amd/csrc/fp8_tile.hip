@@ -1,176 +1,430 @@
 // Products of 8-bit floats, many rows: plain, the gated block's forward pass, and its backward pass.
 //
-// Bound by the matrix cores.  A workgroup of four waves has 16 * MF rows and 256 slots of the weights; a wave has all the rows and 64 of
-// the slots, as 4 * MF tiles of 16 x 16 in fp32.  The rows' codes go into LDS without passing registers, two blocks of K ahead, and
-// every wave reads them all; the weights, which no two waves share, go from memory to registers in the order they are packed in, one
-// block of K ahead.  The scales, one for a row's block and one for a fragment's, are operands of the matrix instruction.
+// Bound by the matrix cores.  A workgroup of four waves has all of its rows' products with 256 slots of the weights; a wave has all the
+// rows and 64 of the slots.  The rows' codes go into LDS without passing registers, two blocks of K ahead, and every wave reads them
+// all; the weights, which no two waves share, go from memory to registers in the order they are packed in, one block of K ahead.  The
+// scales, one for a row's block and one for a fragment's, are operands of the matrix instruction.  Two shapes:
+//   256 rows  32 x 32 tiles, one wave per SIMD with all the accumulators there are: where there are tiles for nearly every CU
+//   64 or 128 rows  16 x 16 tiles, two workgroups a CU; K dealt over workgroups where there are few
 #include "qg_fp8.h"
 
 namespace {
 
+typedef float f16v __attribute__((ext_vector_type(16)));
+
 constexpr int SLOTS = 256, STAGES = 3;
 
-__device__ inline void request_rows(unsigned lds, unsigned offset, const uint8_t* base) {
+// 16 (4) bytes a lane from memory to LDS: lane i's to lds + 16 i (4 i).  The compiler knows nothing of these requests: whoever reads the
+// result has waited for all of the wave's.
+__device__ inline void request_16(unsigned lds, unsigned offset, const uint8_t* base) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(offset), "s"(base) : "memory");
 }
+__device__ inline void request_4(unsigned lds, unsigned offset, const uint8_t* base) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" ::"s"(lds), "v"(offset), "s"(base) : "memory");
+}
+__device__ inline unsigned lds_address(const void* p) { return (unsigned)(size_t)(const __attribute__((address_space(3))) uint8_t*)p; }
 
-struct piece {  // a wave's weights of one block of K
-  u4 x[4][2];
-  __device__ inline void load(const uint8_t* from, int lane) {
+// ---- shapes: how a wave's accumulators lie.  An item is a lane's 16 consecutive columns of a row (gated: 8 of each matrix): value
+// (j, r) belongs to fragment j, slot 4 q + r of the quarter q.
+
+template <int MF>
+struct small {  // 16 x 16: lane m + 16 g has row m of a fragment, quarter g
+  static constexpr int ROWS = 16 * MF, FRAGMENT = 16, ITEMS = MF;
+  f4 c[MF][4];
+  // sums start from the bias of their columns, or 0
+  __device__ inline void start(const float* bias, int first, int columns, int lane) {
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
+    for (int j = 0; j < 4; ++j) {
+      f4 v = (f4){0.0f, 0.0f, 0.0f, 0.0f};
+      if (bias) {
+        const int column = first + 16 * (lane >> 4) + 4 * j;
 #pragma unroll
-      for (int h = 0; h < 2; ++h) x[j][h] = *reinterpret_cast<const u4*>(from + j * 2048 + h * 1024 + lane * 16);
+        for (int r = 0; r < 4; ++r)
+          if (column + r < columns) v[r] = bias[column + r];
+      }
+#pragma unroll
+      for (int i = 0; i < MF; ++i) c[i][j] = v;
+    }
   }
-  __device__ inline void arrived() {  // (in registers from here on: the compiler waits in front of this)
+  template <int T>
+  __device__ inline f4 quad(int j) const { return c[T][j]; }
+  template <int T>
+  __device__ inline void here() {}
+  static __device__ inline int row(int item, int lane) { return 16 * item + (lane & 15); }
+  static __device__ inline int quarter(int, int lane) { return lane >> 4; }
+};
+
+struct large {  // 32 x 32: lane m + 32 g has row m, quarters g and g + 2; 16 registers are slots 8 (e / 4) + 4 g + e % 4 of two fragments
+  static constexpr int ROWS = 256, FRAGMENT = 32, ITEMS = 16;
+  f16v c[8][2];
+  __device__ inline void start(const float* bias, int first, int columns, int lane) {
 #pragma unroll
-    for (int j = 0; j < 4; ++j) asm volatile("" : "+v"(x[j][0]), "+v"(x[j][1]));
+    for (int j = 0; j < 2; ++j)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        float v = 0.0f;
+        const int column = first + 16 * ((lane >> 5) + 2 * (e / 4 % 2)) + 4 * (2 * j + e / 8) + e % 4;
+        if (bias && column < columns) v = bias[column];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) c[i][j][e] = v;
+      }
+  }
+  template <int T>
+  __device__ inline f4 quad(int j) const {
+    const f16v& v = c[T / 2][j / 2];
+    const int e = j % 2 * 8 + T % 2 * 4;
+    return (f4){v[e], v[e + 1], v[e + 2], v[e + 3]};
+  }
+  template <int T>
+  __device__ inline void here() {  // (taken out of the accumulators here and not earlier, where there are no registers for it)
+    if (T % 2 == 0) asm volatile("" : "+a"(c[T / 2][0]), "+a"(c[T / 2][1]));
+  }
+  static __device__ inline int row(int item, int lane) { return 32 * (item / 2) + (lane & 31); }
+  static __device__ inline int quarter(int item, int lane) { return (lane >> 5) + 2 * (item % 2); }
+};
+
+// Where a workgroup's tile lies.  Workgroups go round-robin over the 8 XCDs: each gets a run of tiles, some rows of tiles at a time, so
+// that those that run at once on an XCD share rows and columns in its L2.
+struct place {
+  int row_tile, column_tile, row_tiles, column_tiles, slice;
+  __device__ inline bool find(int rows, int columns) {
+    row_tiles = rows;
+    column_tiles = columns;
+    const int tiles = rows * columns, per = (tiles + 7) / 8;
+    const int id = (int)blockIdx.x % (per * 8);
+    slice = (int)blockIdx.x / (per * 8);
+    const int at = id % 8 * per + id / 8;
+    if (at >= tiles) return false;
+    const int panel = at / (8 * columns), in_panel = at - panel * 8 * columns;
+    const int panel_rows = min(8, rows - panel * 8);
+    row_tile = panel * 8 + in_panel % panel_rows;
+    column_tile = in_panel / panel_rows;
+    return true;
   }
 };
 
-template <int TYPE, int N>
+// ---- what becomes of the sums
+
+template <typename A>
+__device__ inline void finish_plain(const qg_fp8_product_args& p, A& acc, const place& at, int wave, int lane, float* lds) {
+  const int row0 = at.row_tile * A::ROWS, group = at.column_tile * 4 + wave;
+  if (group * 64 >= p.channels) return;
+  const int rest = min(64, p.channels - group * 64) % 16, first = p.channels - rest;   // columns of the item that has fewer than 16, if any
+  each<0, A::ITEMS>([&](auto item) {
+    constexpr int t = decltype(item)::value;
+    acc.template here<t>();
+    f4 v[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) v[j] = acc.template quad<t>(j);
+    const float* const x = reinterpret_cast<const float*>(v);
+    const int in_tile = A::row(t, lane), row = row0 + in_tile, column = group * 64 + 16 * A::quarter(t, lane);
+    if (rest != 0 && column == first) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) *reinterpret_cast<f4*>(lds + in_tile * 16 + 4 * j) = v[j];
+    }
+    const bool there = row < p.tokens && column + 16 <= p.channels;
+    const long long to = row * p.out.stride + column;
+    if (p.out_type == QG_F32) {
+      if (there) qg_store<QG_F32, 16>(static_cast<float*>(p.out.data) + to, x);
+    } else if (p.out_type == QG_BF16) {
+      if (there) qg_store<QG_BF16, 16>(static_cast<__bf16*>(p.out.data) + to, x);
+    } else {
+      if (there) qg_store<QG_F16, 16>(static_cast<_Float16*>(p.out.data) + to, x);
+    }
+  });
+  if (rest == 0) return;
+  // through LDS, one result a lane at a time; the other waves of this workgroup have whole items, or none
+  const int rows = min(A::ROWS, p.tokens - row0);
+  for (int e = lane; e < rows * rest; e += 64) {
+    const int row = e / rest, column = e % rest;
+    put<1>(p.out_type, p.out, row0 + row, first + column, p.channels, lds + row * 16 + column);
+  }
+}
+
+template <int TYPE>
 __device__ inline void get(const qg_fp8_rows& from, int row, int column, int columns, float* v) {
   typedef typename qg_elem<TYPE>::t T;
   const T* in = static_cast<const T*>(from.data) + row * from.stride + column;
-  if (column + N <= columns) {
-    qg_load<TYPE, N>(in, v);
+  if (column + 8 <= columns) {
+    qg_load<TYPE, 8>(in, v);
   } else {
 #pragma unroll
-    for (int i = 0; i < N; ++i) v[i] = column + i < columns ? qg_elem<TYPE>::up(in[i]) : 0.0f;
+    for (int i = 0; i < 8; ++i) v[i] = column + i < columns ? qg_elem<TYPE>::up(in[i]) : 0.0f;
   }
 }
 
-__device__ inline void put_codes(const qg_fp8_held& to, int row, int column, const float* v, float power) {
-  const u2 w = {codes_of(v[0], v[1], v[2], v[3], power), codes_of(v[4], v[5], v[6], v[7], power)};
+__device__ inline void put_codes(const qg_fp8_held& to, int row, int column, const f4* v, float power) {
+  const u2 w = {codes_of(v[0][0], v[0][1], v[0][2], v[0][3], power), codes_of(v[1][0], v[1][1], v[1][2], v[1][3], power)};
   *reinterpret_cast<u2*>(to.codes + (size_t)row * to.pitch + column) = w;
 }
-__device__ inline unsigned top_of(const float* v) {
-  unsigned top = 0u;
+
+// h, and in the backward pass dg and du, from g and u.  The accumulators go through LDS, so that one piece of code serves all items in turn
+// (the activations are long); so do the results that become 8-bit floats, until the largest size of their block is known: a block of
+// 128 columns is what the four waves have of a row together.
+constexpr int ITEM_F4 = 6 * 64;  // of an item's place: 24 numbers a lane
+template <typename A>
+constexpr int batch_of() { return A::ITEMS == 16 ? 4 : 2; }  // (two workgroups of the smaller tiles share a CU's LDS)
+template <typename A>
+constexpr int gated_lds() { return batch_of<A>() * 4 * ITEM_F4 * 16 + 3 * (batch_of<A>() / (A::ITEMS * A::FRAGMENT / A::ROWS)) * A::FRAGMENT * 4; }
+
+template <typename A, bool BACK>
+__device__ inline void finish_gated(const qg_fp8_product_args& p, const A& acc, const place& at, int wave, int lane, f4* lds) {
+  constexpr int BATCH = batch_of<A>(), PER_ROW = A::ITEMS * A::FRAGMENT / A::ROWS, ROWS = BATCH / PER_ROW * A::FRAGMENT;
+  const int group = at.column_tile * 4 + wave, padded = at.column_tiles * 128, last_row = p.tokens - 1;
+  f4* const mine = lds + wave * BATCH * ITEM_F4 + lane;
+  unsigned* const tops = reinterpret_cast<unsigned*>(lds + 4 * BATCH * ITEM_F4);  // [3][ROWS]
+  const bool held = BACK || p.out.data == nullptr;
+  each<0, A::ITEMS / BATCH>([&](auto batch) {
+    constexpr int b0 = decltype(batch)::value * BATCH;
+    const int row0 = at.row_tile * A::ROWS + b0 / PER_ROW * A::FRAGMENT;
+    __syncthreads();
+    for (int e = (int)threadIdx.x; e < 3 * ROWS; e += 256) tops[e] = 0u;
+    each<0, BATCH>([&](auto item) {
+      constexpr int t = decltype(item)::value;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) top = umax(top, size_bits(v[i]));
-  return max_over_quads(top);
+      for (int j = 0; j < 4; ++j) mine[t * ITEM_F4 + j * 64] = acc.template quad<b0 + t>(j);
+    });
+    __syncthreads();
+    float dh[8];
+    auto fetch = [&](int t) {
+      const int row = min(row0 + A::row(t, lane), last_row), column = group * 32 + 8 * A::quarter(t, lane);
+      if (p.dh_type == QG_F32) get<QG_F32>(p.dh, row, column, p.channels, dh);
+      if (p.dh_type == QG_BF16) get<QG_BF16>(p.dh, row, column, p.channels, dh);
+      if (p.dh_type == QG_F16) get<QG_F16>(p.dh, row, column, p.channels, dh);
+    };
+    if (BACK) fetch(0);
+#pragma unroll 1
+    for (int t = 0; t < BATCH; ++t) {
+      f4* const place = mine + t * ITEM_F4;
+      const int in_batch = A::row(t, lane), row = row0 + in_batch, column = group * 32 + 8 * A::quarter(t, lane);
+      f4 h[2], dg[2], du[2];
+      (void)dg;
+      (void)du;
+      unsigned top_h = 0u, top_g = 0u, top_u = 0u;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const float gate = place[j / 4 * 2 * 64][j % 4], up = place[(j / 4 * 2 + 1) * 64][j % 4];
+        float slope = 0.0f;
+        const float a = activate<BACK>(p.activation, gate, &slope);
+        h[j / 4][j % 4] = a * up;
+        top_h = umax(top_h, size_bits(a * up));
+        if (BACK) {
+          dg[j / 4][j % 4] = dh[j] * up * slope;
+          du[j / 4][j % 4] = dh[j] * a;
+          top_g = umax(top_g, size_bits(dh[j] * up * slope));
+          top_u = umax(top_u, size_bits(dh[j] * a));
+        }
+      }
+      if (BACK && t + 1 < BATCH) fetch(t + 1);
+      if (!held) {
+        if (row <= last_row && column < p.channels) put<8>(p.out_type, p.out, row, column, p.channels, reinterpret_cast<const float*>(h));
+        continue;
+      }
+      place[0] = h[0];
+      place[64] = h[1];
+      atomicMax(tops + in_batch, top_h);
+      if (BACK) {
+        place[2 * 64] = dg[0];
+        place[3 * 64] = dg[1];
+        place[4 * 64] = du[0];
+        place[5 * 64] = du[1];
+        atomicMax(tops + ROWS + in_batch, top_g);
+        atomicMax(tops + 2 * ROWS + in_batch, top_u);
+      }
+    }
+    if (!held) return;
+    __syncthreads();
+#pragma unroll 1
+    for (int t = 0; t < BATCH; ++t) {
+      const f4* const place = mine + t * ITEM_F4;
+      const int in_batch = A::row(t, lane), row = row0 + in_batch, quarter = A::quarter(t, lane), column = group * 32 + 8 * quarter;
+      if (row > last_row) continue;
+      const f4 h[2] = {place[0], place[64]};
+      const unsigned byte = scale_byte(tops[in_batch]);
+      put_codes(p.out8, row, column, h, scale_of(byte));
+      const bool first = wave == 0 && quarter == 0;
+      if (first) p.out8.scales[(size_t)row * p.out8.scale_pitch + at.column_tile] = (uint8_t)byte;
+      if (BACK) {
+        const f4 dg[2] = {place[2 * 64], place[3 * 64]}, du[2] = {place[4 * 64], place[5 * 64]};
+        const unsigned byte_g = scale_byte(tops[ROWS + in_batch]), byte_u = scale_byte(tops[2 * ROWS + in_batch]);
+        put_codes(p.dgu8, row, column, dg, scale_of(byte_g));
+        put_codes(p.dgu8, row, padded + column, du, scale_of(byte_u));
+        if (first) {
+          uint8_t* scales = p.dgu8.scales + (size_t)row * p.dgu8.scale_pitch;
+          scales[at.column_tile] = (uint8_t)byte_g;
+          scales[at.column_tiles + at.column_tile] = (uint8_t)byte_u;
+        }
+        __bf16* to = p.dgu + (size_t)row * 2 * padded + column;
+        qg_store<QG_BF16, 8>(to, reinterpret_cast<const float*>(dg));
+        qg_store<QG_BF16, 8>(to + padded, reinterpret_cast<const float*>(du));
+      }
+    }
+  });
 }
+
+template <typename A, int END>
+__device__ inline void finish(const qg_fp8_product_args& p, A& acc, const place& at, int wave, int lane, uint8_t* lds) {
+  __syncthreads();
+  if constexpr (END == QG_FP8_PLAIN) {
+    finish_plain<A>(p, acc, at, wave, lane, reinterpret_cast<float*>(lds));
+  } else {
+    finish_gated<A, END == QG_FP8_GATED_BACK>(p, acc, at, wave, lane, reinterpret_cast<f4*>(lds));
+  }
+}
+template <typename A, int END>
+constexpr int lds_bytes() {
+  constexpr int loop = STAGES * A::ROWS * 128 + 2 * A::ROWS * 4, end = END == QG_FP8_PLAIN ? A::ROWS * 64 : gated_lds<A>();
+  return loop > end ? loop : end;
+}
+
+// ---- the rows' side of the main loop: both shapes fetch them alike
+template <int ROWS>
+struct row_requests {
+  static constexpr int N = ROWS / 32, STAGE = ROWS * 128;
+  unsigned offset[N], scale_offset, lds, scales_lds;
+  const uint8_t *codes, *scales;
+  bool scales_mine;
+  // Requests of 1 KiB: eight rows; within a row's 128 bytes chunk c lies at place c ^ (row >> 1 & 7), so that the reads of 16 rows of one
+  // chunk go through all banks
+  __device__ inline void init(const qg_fp8_product_args& p, int row0, int wave, int lane, const uint8_t* base) {
+    const int last_row = p.tokens - 1;
+#pragma unroll
+    for (int r = 0; r < N; ++r) {
+      const int row = 8 * (wave + 4 * r) + lane / 8;
+      offset[r] = (unsigned)(min(row0 + row, last_row) - row0) * (unsigned)p.x8.pitch + (unsigned)((lane % 8 ^ (row >> 1 & 7)) * 16);
+    }
+    scale_offset = (unsigned)(min(row0 + wave * 64 + lane, last_row) - row0) * (unsigned)p.x8.scale_pitch;
+    codes = p.x8.codes + (size_t)row0 * p.x8.pitch;
+    scales = p.x8.scales + (size_t)row0 * p.x8.scale_pitch;
+    lds = lds_address(base) + (unsigned)wave * 1024u;
+    scales_lds = lds_address(base) + STAGES * STAGE + (unsigned)wave * 256u;
+    scales_mine = wave * 64 < ROWS;
+  }
+  __device__ inline void rows(int stage, int kb, int r) const { request_16(lds + (unsigned)stage * STAGE + r * 4096u, offset[r], codes + (size_t)kb * 128); }
+  __device__ inline void four_scales(int kb) const {  // of the blocks kb .. kb + 3
+    if (scales_mine) request_4(scales_lds + (unsigned)(kb >> 2 & 1) * (ROWS * 4), scale_offset, scales + kb);
+  }
+};
+
+// One block of K a turn, in both kernels.  At its end all its requests have arrived: the weights of the next block, which take the place
+// of its own behind their last use, and the rows of the block after that, which the other waves may read behind the next barrier.  The barrier
+// comes late in a turn, when nobody waits at it, and two fragments before its end, so that the first reads of the next block are there in time.
+// Requests go out between the matrix instructions, in whose shadow they cost nothing.
+
+struct piece {  // a wave's weights of one block of K
+  u4 x[4][2];
+  unsigned scales;
+  __device__ inline void load(const uint8_t* from, int i) { x[i / 2][i % 2] = *reinterpret_cast<const u4*>(from + i * 1024); }
+  __device__ inline void arrived() {  // (in registers from here on: the compiler waits in front of this)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) asm volatile("" : "+v"(x[j][0]), "+v"(x[j][1]));
+    asm volatile("" : "+v"(scales));
+  }
+};
 
 // WIDE: sums by the bf16 instructions
 template <int MF, int END, bool WIDE>
-__global__ __launch_bounds__(256, MF >= 8 ? 1 : 2) void qg_fp8_tile_kernel(qg_fp8_product_args p, int row_tiles, int column_tiles) {
-  constexpr int ROWS = 16 * MF, STAGE = ROWS * 128, REQUESTS = MF >= 2 ? MF / 2 : 1;
-  __shared__ __align__(1024) uint8_t rows_lds[STAGES * STAGE];
+__global__ __launch_bounds__(256, WIDE && MF == 8 ? 1 : 2) void qg_fp8_tile_kernel(qg_fp8_product_args p, int row_tiles, int column_tiles) {
+  typedef small<MF> A;
+  constexpr int ROWS = A::ROWS, STAGE = ROWS * 128, RING = 4;
+  static_assert(MF % RING == 0, "a fragment's registers");
+  __shared__ __align__(1024) uint8_t lds[lds_bytes<A, END>()];
   __shared__ int ticket;
   const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   const int m = lane & 15, g = lane >> 4;
-
-  // Workgroups go round-robin over the 8 XCDs: each gets a run of tiles, eight rows of tiles at a time, so that those that run at once
-  // on an XCD share rows and columns in its L2
-  const int tiles = row_tiles * column_tiles, per = (tiles + 7) / 8;
-  const int id = (int)blockIdx.x % (per * 8), slice = (int)blockIdx.x / (per * 8);
-  const int at = id % 8 * per + id / 8;
-  if (at >= tiles || id / 8 >= per) return;
-  const int panel = at / (8 * column_tiles), in_panel = at - panel * 8 * column_tiles;
-  const int panel_rows = min(8, row_tiles - panel * 8);
-  const int row_tile = panel * 8 + in_panel % panel_rows, column_tile = in_panel / panel_rows;
-  const int row0 = row_tile * ROWS, last_row = p.tokens - 1;
-  const int group = column_tile * 4 + wave;
-  const int k0 = slice * p.slice_kb, k1 = min(k0 + p.slice_kb, p.w.kb);
-
-  // requests of 1 KiB: eight rows; within a row's 128 bytes chunk c lies at place c ^ (row >> 1 & 7), so that the reads of 16 rows of one
-  // chunk go through all banks
-  unsigned offset[REQUESTS];
-#pragma unroll
-  for (int r = 0; r < REQUESTS; ++r) {
-    const int row = 8 * (wave + 4 * r) + lane / 8;
-    offset[r] = (unsigned)(min(row0 + row, last_row) - row0) * (unsigned)p.x8.pitch + (unsigned)((lane % 8 ^ (row >> 1 & 7)) * 16);
-  }
-  const uint8_t* const codes = p.x8.codes + (size_t)row0 * p.x8.pitch;
-  const unsigned lds0 = (unsigned)(size_t)(__attribute__((address_space(3))) uint8_t*)rows_lds;
-  auto request = [&](int kb) {
-    if (wave * 8 >= ROWS) return;
-    const unsigned to = lds0 + (unsigned)((kb - k0) % STAGES) * STAGE + (unsigned)wave * 1024u;
-#pragma unroll
-    for (int r = 0; r < REQUESTS; ++r) request_rows(to + r * 4096u, offset[r], codes + (size_t)kb * 128);
-  };
-  const uint8_t* const pieces = p.w.pieces + (size_t)group * p.w.kb * QG_FP8_PIECE;
+  place at;
+  if (!at.find(row_tiles, column_tiles)) return;
+  const int row0 = at.row_tile * ROWS, group = at.column_tile * 4 + wave;
+  const int k0 = at.slice * p.slice_kb, k1 = min(k0 + p.slice_kb, p.w.kb);
+  row_requests<ROWS> request;
+  request.init(p, row0, wave, lane, lds);
+  const uint8_t* const pieces = p.w.pieces + (size_t)group * p.w.kb * QG_FP8_PIECE + lane * 16;
   const uint32_t* const weight_scales = p.w.scales + (size_t)group * p.w.kb4;
-  const uint8_t* row_scales[MF];
-#pragma unroll
-  for (int i = 0; i < MF; ++i) row_scales[i] = p.x8.scales + (size_t)min(row0 + 16 * i + m, last_row) * p.x8.scale_pitch;
 
-  f4 c[MF][4];
+  A acc;
+  acc.start(END == QG_FP8_PLAIN && at.slice == 0 ? p.bias : nullptr, group * 64, p.channels, lane);
+  // a ring of row fragments on their way from LDS, three ahead of the one that is multiplied
+  const unsigned read0 = (unsigned)(m * 128 + ((g ^ (m >> 1)) * 16)), read1 = read0 ^ 64u;
+  u4 x[RING][2];
+  unsigned xs[RING];
+  auto read = [&](int stage, int kb, int i) {
+    x[i % RING][0] = *reinterpret_cast<const u4*>(lds + stage * STAGE + i * 2048 + read0);
+    x[i % RING][1] = *reinterpret_cast<const u4*>(lds + stage * STAGE + i * 2048 + read1);
+    xs[i % RING] = lds[STAGES * STAGE + (kb >> 2 & 1) * (ROWS * 4) + i * 64 + m * 4 + (kb & 3)];
+  };
+  piece now;
+  int stage = 0;  // of the block that is multiplied
+  request.four_scales(k0);
 #pragma unroll
-  for (int i = 0; i < MF; ++i)
+  for (int r = 0; r < request.N; ++r) request.rows(0, k0, r);
 #pragma unroll
-    for (int j = 0; j < 4; ++j) c[i][j] = (f4){0.0f, 0.0f, 0.0f, 0.0f};
-
-  const unsigned read0 = (unsigned)(m * 128 + ((g ^ (m >> 1)) * 16));
-  unsigned scale[MF], next_scale[MF];
-  piece now, next;
-  request(k0);
-  if (k0 + 1 < k1) request(k0 + 1);
-  next.load(pieces + (size_t)k0 * QG_FP8_PIECE, lane);
+  for (int r = 0; r < request.N; ++r) request.rows(1, min(k0 + 1, k1 - 1), r);
 #pragma unroll
-  for (int i = 0; i < MF; ++i) next_scale[i] = *reinterpret_cast<const uint32_t*>(row_scales[i] + k0);
+  for (int i = 0; i < 8; ++i) now.load(pieces + (size_t)k0 * QG_FP8_PIECE, i);
+  now.scales = weight_scales[k0];
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+  read(0, k0, 0);
+  read(0, k0, 1);
   for (int kb = k0; kb < k1; ++kb) {
-    next.arrived();
-#pragma unroll
-    for (int i = 0; i < MF; ++i) asm volatile("" : "+v"(next_scale[i]));
-    now = next;
-    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
-    __builtin_amdgcn_s_barrier();  // the rows of this block are there, and nobody reads the last one's any more
-    asm volatile("" ::: "memory");
-    if (kb % 4 == 0) {
-#pragma unroll
-      for (int i = 0; i < MF; ++i) scale[i] = next_scale[i];
-    } else {
-#pragma unroll
-      for (int i = 0; i < MF; ++i) scale[i] >>= 8;
-    }
-    if (kb + 2 < k1) request(kb + 2);
-    if (kb + 1 < k1) next.load(pieces + (size_t)(kb + 1) * QG_FP8_PIECE, lane);
-    if (kb % 4 == 3 && kb + 1 < k1) {
-#pragma unroll
-      for (int i = 0; i < MF; ++i) next_scale[i] = *reinterpret_cast<const uint32_t*>(row_scales[i] + kb + 1);
-    }
-    const unsigned ws = weight_scales[kb];
-    const uint8_t* stage = rows_lds + (kb - k0) % STAGES * STAGE;
-    if constexpr (WIDE) {
-      wide w[4] = {wide(now.x[0][0], now.x[0][1], scale_of(ws & 255u)), wide(now.x[1][0], now.x[1][1], scale_of(ws >> 8 & 255u)),
-                   wide(now.x[2][0], now.x[2][1], scale_of(ws >> 16 & 255u)), wide(now.x[3][0], now.x[3][1], scale_of(ws >> 24))};
-#pragma unroll
-      for (int i = 0; i < MF; ++i) {
-        const wide x(*reinterpret_cast<const u4*>(stage + i * 2048 + read0), *reinterpret_cast<const u4*>(stage + i * 2048 + (read0 ^ 64u)),
-                     scale_of(scale[i] & 255u));
-#pragma unroll
-        for (int j = 0; j < 4; ++j) c[i][j] = wide_product(w[j], x, c[i][j]);
-      }
-      continue;
-    }
+    const int ahead = stage + 2 >= STAGES ? stage + 2 - STAGES : stage + 2, after = stage + 1 == STAGES ? 0 : stage + 1;
+    const int next_kb = min(kb + 1, k1 - 1), rows_kb = min(kb + 2, k1 - 1);   // (past the end: the last block again, not used)
+    const uint8_t* const next_piece = pieces + (size_t)next_kb * QG_FP8_PIECE;
+    piece next;
+    if ((kb & 3) == 1 && kb + 3 < k1) request.four_scales(kb + 3);
+    next.scales = weight_scales[next_kb];
+    read(stage, kb, 2);
+    constexpr int LOADS = MF >= 8 ? 1 : 4;   // of weights, in the shadow of a fragment
 #pragma unroll
     for (int i = 0; i < MF; ++i) {
-      const i8v x = both(*reinterpret_cast<const u4*>(stage + i * 2048 + read0), *reinterpret_cast<const u4*>(stage + i * 2048 + (read0 ^ 64u)));
+      if (i + 3 < MF) read(stage, kb, i + 3);
+      if (i == MF - 2) {
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+      }
+      if (i >= MF - 2) read(after, kb + 1, i - (MF - 2));
+      if (i < request.N) request.rows(ahead, rows_kb, i);
+      if (i * LOADS < 8) {
 #pragma unroll
-      for (int j = 0; j < 4; ++j) c[i][j] = matrix_product(both(now.x[j][0], now.x[j][1]), x, c[i][j], j, ws, scale[i]);
+        for (int l = 0; l < LOADS; ++l) next.load(next_piece, i * LOADS + l);
+      }
+      if (i == MF - 1) next.arrived();
+      if constexpr (WIDE) {
+        const wide r(x[i % RING][0], x[i % RING][1], scale_of(xs[i % RING]));
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          acc.c[i][j] = wide_product(wide(now.x[j][0], now.x[j][1], scale_of(now.scales >> (8 * j) & 255u)), r, acc.c[i][j]);
+      } else {
+        const i8v r = both(x[i % RING][0], x[i % RING][1]);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) acc.c[i][j] = matrix_product(both(now.x[j][0], now.x[j][1]), r, acc.c[i][j], j, now.scales, xs[i % RING]);
+      }
+      if (i < MF - 1) __builtin_amdgcn_sched_barrier(0);
     }
+    now = next;
+    stage = after;
   }
+  asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");   // (what was requested past the end)
 
   if (p.slices > 1) {  // sums of the slices through memory, past the L2s that the XCDs do not share; the last one to arrive adds them in order
-    const int tile = row_tile * column_tiles + column_tile;
+    const int tile = at.row_tile * column_tiles + at.column_tile;
     float* const mine = p.partial + ((size_t)tile * p.slices * (SLOTS / 64) + wave) * (size_t)(ROWS * 64) + lane * 4;
     const size_t step = (size_t)(SLOTS / 64) * (ROWS * 64);
 #pragma unroll
     for (int i = 0; i < MF; ++i)
 #pragma unroll
       for (int j = 0; j < 4; ++j)
-        asm volatile("global_store_dwordx4 %0, %1, off sc1\n\ts_nop 1" ::"v"(mine + slice * step + (i * 4 + j) * 256), "v"(c[i][j]) : "memory");
+        asm volatile("global_store_dwordx4 %0, %1, off sc1\n\ts_nop 1" ::"v"(mine + at.slice * step + (i * 4 + j) * 256), "v"(acc.c[i][j]) : "memory");
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();
     if (threadIdx.x == 0) ticket = __hip_atomic_fetch_add(p.counters + tile, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     __syncthreads();
     if (ticket != p.slices - 1) return;
     if (threadIdx.x == 0) __hip_atomic_store(p.counters + tile, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);  // ready for the next call
-#pragma unroll
-    for (int i = 0; i < MF; ++i)
-#pragma unroll
-      for (int j = 0; j < 4; ++j) c[i][j] = (f4){0.0f, 0.0f, 0.0f, 0.0f};
+    acc.start(nullptr, 0, 0, lane);
+#pragma unroll 1
     for (int s = 0; s < p.slices; ++s) {
       const float* theirs = mine + s * step;
 #pragma unroll
@@ -180,107 +434,131 @@ __global__ __launch_bounds__(256, MF >= 8 ? 1 : 2) void qg_fp8_tile_kernel(qg_fp
           const unsigned long long* from = reinterpret_cast<const unsigned long long*>(theirs + (i * 4 + j) * 256);
           const unsigned long long a = __hip_atomic_load(from, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
           const unsigned long long b = __hip_atomic_load(from + 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-          c[i][j][0] += __builtin_bit_cast(float, (unsigned)a);
-          c[i][j][1] += __builtin_bit_cast(float, (unsigned)(a >> 32));
-          c[i][j][2] += __builtin_bit_cast(float, (unsigned)b);
-          c[i][j][3] += __builtin_bit_cast(float, (unsigned)(b >> 32));
+          acc.c[i][j][0] += __builtin_bit_cast(float, (unsigned)a);
+          acc.c[i][j][1] += __builtin_bit_cast(float, (unsigned)(a >> 32));
+          acc.c[i][j][2] += __builtin_bit_cast(float, (unsigned)b);
+          acc.c[i][j][3] += __builtin_bit_cast(float, (unsigned)(b >> 32));
         }
     }
   }
+  finish<A, END>(p, acc, at, wave, lane, lds);
+}
 
-  if constexpr (END == QG_FP8_PLAIN) {
-    const int column = group * 64 + 16 * g;
-    if (column >= p.channels) return;
-    float bias[16];
-#pragma unroll
-    for (int i = 0; i < 16; ++i) bias[i] = p.bias && column + i < p.channels ? p.bias[column + i] : 0.0f;
-#pragma unroll
-    for (int i = 0; i < MF; ++i) {
-      const int row = row0 + 16 * i + m;
-      if (row > last_row) continue;
-      float v[16];
-#pragma unroll
-      for (int j = 0; j < 16; ++j) v[j] = c[i][j / 4][j % 4] + bias[j];
-      put<16>(p.out_type, p.out, row, column, p.channels, v);
-    }
+// The matrix instruction in place: with all 256 accumulator registers in use the compiler moves them about between turns.  It does not
+// know how long the result takes: whoever reads it waits (19 cycles of 4 after the last one).  Nor does it know that the operands are to be
+// two cycles old if they were computed; in the shadow of the product before, waiting is free.
+template <int HIGH>
+__device__ inline void add_product(f16v& c, i8v a, i8v b, unsigned scale_a, unsigned scale_b) {
+  if (HIGH) {  // byte 2 of scale_a
+    asm volatile("s_nop 1\n\tv_mfma_scale_f32_32x32x64_f8f6f4 %0, %1, %2, %0, %3, %4 op_sel_hi:[1,0,0]" : "+a"(c) : "v"(a), "v"(b), "v"(scale_a), "v"(scale_b));
   } else {
-    // 32 columns of the inner size a wave, 8 a lane
-    const int column = group * 32 + 8 * g, block = column_tile, padded = column_tiles * 128;
-    constexpr int BATCH = MF < 4 ? MF : 4;   // row fragments whose largest values meet at once
-    float* const tops_f = reinterpret_cast<float*>(rows_lds);
-    unsigned* const tops = reinterpret_cast<unsigned*>(tops_f);  // [3][4 waves][16 * BATCH]
-    const bool held = END == QG_FP8_GATED_BACK || p.out.data == nullptr;
-    for (int b0 = 0; b0 < MF; b0 += BATCH) {
-      float h[BATCH][8], dg[BATCH][8], du[BATCH][8];
-      (void)dg;
-      (void)du;
-      __syncthreads();
-#pragma unroll
-      for (int b = 0; b < BATCH; ++b) {
-        const int i = b0 + b, row = row0 + 16 * i + m;
-        float dh[8];
-        if (END == QG_FP8_GATED_BACK) {
-          const int from = min(row, last_row);
-          if (p.dh_type == QG_F32) get<QG_F32, 8>(p.dh, from, column, p.channels, dh);
-          if (p.dh_type == QG_BF16) get<QG_BF16, 8>(p.dh, from, column, p.channels, dh);
-          if (p.dh_type == QG_F16) get<QG_F16, 8>(p.dh, from, column, p.channels, dh);
-        }
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          f4 gs = c[0][0], us = c[0][0];
-#pragma unroll
-          for (int f = 0; f < MF; ++f)
-            if (f == i) gs = c[f][j / 4 * 2], us = c[f][j / 4 * 2 + 1];
-          const float gate = gs[j % 4], up = us[j % 4];
-          float slope = 0.0f;
-          const float a = activate<END == QG_FP8_GATED_BACK>(p.activation, gate, &slope);
-          h[b][j] = a * up;
-          if (END == QG_FP8_GATED_BACK) {
-            dg[b][j] = dh[j] * up * slope;
-            du[b][j] = dh[j] * a;
-          }
-        }
-        if (!held) {
-          if (row <= last_row && column < p.channels) put<8>(p.out_type, p.out, row, column, p.channels, h[b]);
-          continue;
-        }
-        const unsigned top_h = top_of(h[b]);
-        if (g == 0) tops[wave * 16 * BATCH + 16 * b + m] = top_h;
-        if (END == QG_FP8_GATED_BACK) {
-          const unsigned top_g = top_of(dg[b]), top_u = top_of(du[b]);
-          if (g == 0) tops[(4 + wave) * 16 * BATCH + 16 * b + m] = top_g;
-          if (g == 0) tops[(8 + wave) * 16 * BATCH + 16 * b + m] = top_u;
-        }
-      }
-      if (!held) continue;
-      __syncthreads();
-#pragma unroll
-      for (int b = 0; b < BATCH; ++b) {
-        const int row = row0 + 16 * (b0 + b) + m;
-        unsigned byte[3];
-#pragma unroll
-        for (int s = 0; s < (END == QG_FP8_GATED_BACK ? 3 : 1); ++s) {
-          const unsigned* of = tops + s * 64 * BATCH + 16 * b + m;
-          byte[s] = scale_byte(umax(umax(of[0], of[16 * BATCH]), umax(of[32 * BATCH], of[48 * BATCH])));
-        }
-        if (row > last_row) continue;
-        put_codes(p.out8, row, column, h[b], scale_of(byte[0]));
-        if (wave == 0 && g == 0) p.out8.scales[(size_t)row * p.out8.scale_pitch + block] = (uint8_t)byte[0];
-        if (END == QG_FP8_GATED_BACK) {
-          put_codes(p.dgu8, row, column, dg[b], scale_of(byte[1]));
-          put_codes(p.dgu8, row, padded + column, du[b], scale_of(byte[2]));
-          if (wave == 0 && g == 0) {
-            uint8_t* scales = p.dgu8.scales + (size_t)row * p.dgu8.scale_pitch;
-            scales[block] = (uint8_t)byte[1];
-            scales[column_tiles + block] = (uint8_t)byte[2];
-          }
-          __bf16* to = p.dgu + (size_t)row * 2 * padded + column;
-          qg_store<QG_BF16, 8>(to, dg[b]);
-          qg_store<QG_BF16, 8>(to + padded, du[b]);
-        }
-      }
-    }
+    asm volatile("s_nop 1\n\tv_mfma_scale_f32_32x32x64_f8f6f4 %0, %1, %2, %0, %3, %4 op_sel_hi:[0,0,0]" : "+a"(c) : "v"(a), "v"(b), "v"(scale_a), "v"(scale_b));
   }
+}
+
+template <int END>
+__global__ __launch_bounds__(256, 1) void qg_fp8_tile256_kernel(qg_fp8_product_args p, int row_tiles, int column_tiles) {
+  typedef large A;
+  constexpr int ROWS = A::ROWS, STAGE = ROWS * 128, RING = 3;
+  __shared__ __align__(1024) uint8_t lds[lds_bytes<A, END>()];
+  const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+  const int m = lane & 31, g = lane >> 5;
+  place at;
+  if (!at.find(row_tiles, column_tiles)) return;
+  const int row0 = at.row_tile * ROWS, group = at.column_tile * 4 + wave, kbs = p.w.kb;
+  row_requests<ROWS> request;
+  request.init(p, row0, wave, lane, lds);
+  // an operand is two fragments of 16 slots; a lane's two chunks of 16 bytes are those of the quarters 2 g and 2 g + 1
+  const uint8_t* const pieces = p.w.pieces + (size_t)group * kbs * QG_FP8_PIECE + (m >> 4) * 2048 + (m & 15) * 16 + g * 512;
+  const uint32_t* const weight_scales = p.w.scales + (size_t)group * p.w.kb4;
+  const int scale_shift = (m >> 4) * 8;
+
+  A acc;
+  acc.start(END == QG_FP8_PLAIN ? p.bias : nullptr, group * 64, p.channels, lane);
+  // chunk c = 4 half + 2 g + e of a row
+  const unsigned row_at = (unsigned)m * 128u;
+  unsigned place_of[2][2];
+#pragma unroll
+  for (int h = 0; h < 2; ++h)
+#pragma unroll
+    for (int e = 0; e < 2; ++e) place_of[h][e] = row_at + (unsigned)(((4 * h + 2 * g + e) ^ (m >> 1 & 7)) * 16);
+  u4 x[RING][2][2];
+  unsigned xs[RING];
+  auto read = [&](int stage, int kb, int i, int to) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) x[to][h][e] = *reinterpret_cast<const u4*>(lds + stage * STAGE + i * 4096 + place_of[h][e]);
+    xs[to] = lds[STAGES * STAGE + (kb >> 2 & 1) * (ROWS * 4) + i * 128 + m * 4 + (kb & 3)];
+  };
+  u4 now[2][2][2], next[2][2][2];  // [operand][half][chunk]
+  unsigned now_scales, next_scales;
+  auto load = [&](u4 (&w)[2][2][2], const uint8_t* from, int i) {
+    w[i >> 2][i >> 1 & 1][i & 1] = *reinterpret_cast<const u4*>(from + (i >> 2) * 4096 + (i >> 1 & 1) * 1024 + (i & 1) * 256);
+  };
+  int stage = 0;
+  request.four_scales(0);
+#pragma unroll
+  for (int r = 0; r < request.N; ++r) request.rows(0, 0, r);
+#pragma unroll
+  for (int r = 0; r < request.N; ++r) request.rows(1, min(1, kbs - 1), r);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) load(now, pieces, i);
+  now_scales = weight_scales[0] >> scale_shift;
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+  read(0, 0, 0, 0);
+  read(0, 0, 1, 1);
+  for (int kb = 0; kb < kbs; ++kb) {
+    const int ahead = stage + 2 >= STAGES ? stage + 2 - STAGES : stage + 2, after = stage + 1 == STAGES ? 0 : stage + 1;
+    const int next_kb = min(kb + 1, kbs - 1), rows_kb = min(kb + 2, kbs - 1);   // (past the end: the last block again, not used)
+    const uint8_t* const next_piece = pieces + (size_t)next_kb * QG_FP8_PIECE;
+    if ((kb & 3) == 1 && kb + 3 < kbs) request.four_scales(kb + 3);
+    next_scales = weight_scales[next_kb];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      if (i + 2 < 8) read(stage, kb, i + 2, (i + 2) % RING);
+      if (i == 6) {
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+        read(after, kb + 1, 0, 2);   // (fragment 8, as it were: the ring goes on)
+      }
+      if (i == 7) read(after, kb + 1, 1, 0);
+      request.rows(ahead, rows_kb, i);
+      load(next, next_piece, i);
+      const unsigned s = xs[i % RING];
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const i8v r = both(x[i % RING][h][0], x[i % RING][h][1]);
+        add_product<0>(acc.c[i][0], both(now[0][h][0], now[0][h][1]), r, now_scales, s);
+        add_product<1>(acc.c[i][1], both(now[1][h][0], now[1][h][1]), r, now_scales, s);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    // the ring starts with fragment 0 again
+    u4 t[2][2];
+    unsigned ts = xs[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        t[h][e] = x[2][h][e];
+        x[1][h][e] = x[0][h][e];
+        x[0][h][e] = t[h][e];
+      }
+    xs[1] = xs[0];
+    xs[0] = ts;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) now[i >> 2][i >> 1 & 1][i & 1] = next[i >> 2][i >> 1 & 1][i & 1];
+    now_scales = next_scales >> scale_shift;
+    stage = after;
+  }
+  asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_nop 15\n\ts_nop 15" ::: "memory");   // (what was requested past the end; the last products)
+#pragma unroll
+  for (int i = 0; i < 8; ++i) asm volatile("" : "+a"(acc.c[i][0]), "+a"(acc.c[i][1]));
+  finish<A, END>(p, acc, at, wave, lane, lds);
 }
 
 template <int MF, int END, bool WIDE>
@@ -290,11 +568,19 @@ hipError_t launch(const qg_fp8_product_args& a, hipStream_t s) {
   hipLaunchKernelGGL((qg_fp8_tile_kernel<MF, END, WIDE>), dim3(per * 8 * (unsigned)a.slices), dim3(256), 0, s, a, rows, columns);
   return hipGetLastError();
 }
+template <int END>
+hipError_t launch256(const qg_fp8_product_args& a, hipStream_t s) {
+  const int rows = (a.tokens + 255) / 256, columns = a.w.groups / 4;
+  const unsigned per = (unsigned)(((long long)rows * columns + 7) / 8);
+  hipLaunchKernelGGL((qg_fp8_tile256_kernel<END>), dim3(per * 8), dim3(256), 0, s, a, rows, columns);
+  return hipGetLastError();
+}
 template <int END, bool WIDE>
 hipError_t launch(const qg_fp8_product_args& a, int row_fragments, hipStream_t s) {
-  if (row_fragments == 2) return launch<2, END, WIDE>(a, s);
-  if (row_fragments == 4) return launch<4, END, WIDE>(a, s);
-  return launch<8, END, WIDE>(a, s);
+  if constexpr (!WIDE) {
+    if (row_fragments == 16) return launch256<END>(a, s);
+  }
+  return row_fragments == 4 ? launch<4, END, WIDE>(a, s) : launch<8, END, WIDE>(a, s);
 }
 
 }  // namespace

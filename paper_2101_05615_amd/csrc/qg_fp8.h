@@ -2,6 +2,8 @@
 // Not part of the public interface.
 #pragma once
 
+#include <type_traits>
+
 #include "qg_kv4.h"
 
 // ---------------------------------------------------------------------------
@@ -95,7 +97,7 @@ hipError_t qg_launch_fp8_pack(const qg_fp8_pack_args& a, int type, hipStream_t s
 enum qg_fp8_end { QG_FP8_PLAIN, QG_FP8_GATED, QG_FP8_GATED_BACK };
 hipError_t qg_launch_fp8_tile(const qg_fp8_product_args& a, int end, int row_fragments, int wide_sums, hipStream_t s);
 hipError_t qg_launch_fp8_stream(const qg_fp8_product_args& a, int gated, int fragments, int waves, hipStream_t s);
-hipError_t qg_launch_fp8_gradient(const qg_fp8_gradient_args& a, hipStream_t s);
+hipError_t qg_launch_fp8_gradient(const qg_fp8_gradient_args& a, int tile, hipStream_t s);
 
 #ifdef __HIPCC__
 namespace {
@@ -219,6 +221,14 @@ __device__ inline float activate(int kind, float g, float* slope) {
   }
   if (SLOPE) *slope = g > 0.0f ? 1.0f : g <= 0.0f ? 0.0f : g;  // (of a NaN: NaN)
   return g > 0.0f ? g : g <= 0.0f ? 0.0f : g;
+}
+
+template <int FIRST, int LAST, typename F>
+__device__ inline void each(F&& f) {  // f(0), f(1) ... with constants
+  if constexpr (FIRST < LAST) {
+    f(std::integral_constant<int, FIRST>());
+    each<FIRST + 1, LAST>(f);
+  }
 }
 
 // ---- N consecutive results of a row, as far as the row has columns

@@ -576,3 +576,87 @@ def test_beyond_32_bits(env):
     g = fp8.weight_gradient(big, dy, workspace=fp8.workspace(dev))
     want = x8.sum(0)
     compare(f64(g), np.repeat(want[:, None], 8, 1), np.repeat((np.abs(x8).sum(0) * 2.0 ** -20)[:, None], 8, 1), "gradient")
+
+
+# ---- enough rows and columns for the kernel of 256 x 256 tiles ------------------------------------------------------------------
+
+
+def big64(torch, dev, a, b):
+    return (torch.from_numpy(a).to(dev) @ torch.from_numpy(b).to(dev)).cpu().numpy()
+
+
+@pytest.mark.parametrize("T,K,N", [(2500, 300, 5200), (2561, 128, 5121), (300, 1100, 25600)])
+def test_matmul_large_tiles(env, T, K, N):
+    fp8, torch, dev = env
+    rng = np.random.default_rng(T)
+    say(f"large tiles {T} x {K} x {N}")
+    x, b = tensor(torch, dev, inputs(rng, T, K), "bfloat16"), tensor(torch, dev, weights(rng, K, N), "bfloat16")
+    bias = torch.randn(N, device=dev)
+    w, x8, b8 = fp8.pack(b), ref.held(f64(x)), ref.held_weight(f64(b))
+    want = big64(torch, dev, x8, b8) + f64(bias)
+    bound = ref.sum_bound(big64(torch, dev, np.abs(x8), np.abs(b8)) + np.abs(f64(bias)), K, False)
+    for dtype in DTYPES:
+        store = torch.full((T, N + 5), 3.0, dtype=getattr(torch, dtype), device=dev)
+        fp8.matmul(x, w, bias=bias, out=store[:, 2:2 + N], wide_sums=False)
+        compare(f64(store[:, 2:2 + N]), want, bound + ref.rounding(np.abs(want) + bound, dtype), dtype)
+        assert (store[:, :2] == 3).all() and (store[:, 2 + N:] == 3).all()
+    # a product whose sums stay exact on the 8-bit cores too: every row against the kernel of smaller tiles
+    x = torch.randint(-2, 3, (T, K), device=dev).to(torch.bfloat16)
+    b = torch.randint(-2, 3, (K, N), device=dev).to(torch.bfloat16)
+    w = fp8.pack(b)
+    y = fp8.matmul(x, w, dtype=torch.float32, wide_sums=False)
+    assert torch.equal(y, torch.cat([fp8.matmul(part.contiguous(), w, dtype=torch.float32) for part in x.split(100)]))
+    assert torch.equal(y.double(), x.double() @ b.double())
+
+
+@pytest.mark.parametrize("T,K,F", [(2500, 300, 2700), (2561, 140, 2561)])
+@pytest.mark.parametrize("act", ["silu", "relu"])
+def test_gated_large_tiles(env, T, K, F, act):
+    fp8, torch, dev = env
+    rng = np.random.default_rng(T)
+    say(f"gated, large tiles {T} x {K} x {F} {act}")
+    x, dh = tensor(torch, dev, inputs(rng, T, K), "bfloat16"), tensor(torch, dev, inputs(rng, T, F, 0.01), "float32")
+    gate, up = (tensor(torch, dev, weights(rng, K, F) * s, "bfloat16") for s in (2.0, 1.0))
+    w, xq = fp8.pack_gated(gate, up), fp8.quantize(x)
+    x8, g8, u8, d = ref.held(f64(x)), ref.held_weight(f64(gate)), ref.held_weight(f64(up)), f64(dh)
+    g, u = big64(torch, dev, x8, g8), big64(torch, dev, x8, u8)
+    g_err, u_err = (ref.sum_bound(big64(torch, dev, np.abs(x8), np.abs(b)), K, False) for b in (g8, u8))
+    a, slope = ref.activate(act, g)
+    h, h_err = gated_reference(act, g, u, g_err, u_err)
+    for dtype in DTYPES:
+        y = fp8.gated(xq, w, act, dtype=getattr(torch, dtype), wide_sums=False)
+        compare(f64(y), h, h_err + ref.rounding(np.abs(h) + h_err, dtype), dtype)
+    q = fp8.gated(xq, w, act, out=fp8.new_blocks(T, F, dev))
+    got, held_f32 = f64(fp8.dequantize(q)), fp8.gated(xq, w, act, dtype=torch.float32, wide_sums=False)
+    check_blocks(q, f64(held_f32), "the 8-bit form of the same kernel's fp32 result")
+    assert not (q.codes[:, F:] & 127).any()
+    dgu, dgu8, h8 = fp8.gated_backward(xq, w, dh, act)
+    Fp = ref.up(F, 128)
+    assert torch.equal(h8.codes, q.codes) and torch.equal(h8.scales[:, :Fp // 128], q.scales[:, :Fp // 128])
+    s_err = np.where(np.abs(g) <= g_err, 1.0, 0.0) if act == "relu" else 1.2 * g_err + 2.0 ** -19 * (1 + np.abs(g))
+    a_err = 1.2 * g_err + 2.0 ** -20 * np.abs(a) * (1 + np.abs(g)) + 2.0 ** -22 * np.abs(g)
+    for i, (want, err) in enumerate(((d * u * slope, np.abs(d) * (u_err * (np.abs(slope) + s_err) + np.abs(u) * s_err) + 2.0 ** -22 * np.abs(d * u * slope)),
+                                     (d * a, np.abs(d) * a_err + 2.0 ** -23 * np.abs(d * a)))):
+        compare(f64(dgu[:, i, :F]), want, err + ref.rounding(np.abs(want) + err, "bfloat16"), f"dgu {i}")
+        assert not dgu[:, i, F:].any()
+        # the 8-bit form is of the fp32 value, which dgu has to half a step: no further than that from the 8-bit form of dgu
+        part, near = f64(fp8.dequantize(dgu8))[:, i * Fp:i * Fp + F], f64(dgu[:, i, :F])
+        compare(part, ref.held(near), ref.held_bound(near, ref.rounding(np.abs(near), "bfloat16") * 1.01) + 1e-300, f"dgu8 {i}")
+
+
+@pytest.mark.parametrize("T,K,N", [(130, 3601, 3700), (1, 3800, 3841), (257, 130, 51400)])
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_weight_gradient_large_tiles(env, T, K, N, dtype):
+    fp8, torch, dev = env
+    rng = np.random.default_rng(T + K)
+    say(f"weight gradient, large tiles {T} x {K} x {N} {dtype}")
+    x, dy = tensor(torch, dev, inputs(rng, T, K), dtype), tensor(torch, dev, inputs(rng, T, N, 0.01), dtype)
+    x8, d = ref.held(f64(x)), f64(dy)
+    want, mass = big64(torch, dev, x8.T.copy(), d), big64(torch, dev, np.abs(x8).T.copy(), np.abs(d))
+    bound = mass * ((64 + 32 + T / 16 * 3) * 2.0 ** -23) + np.abs(x8).sum(0)[:, None] * 2.0 ** -130
+    store = torch.full((K, N + 5), 3.0, dtype=torch.float32, device=dev)
+    y = fp8.weight_gradient(fp8.quantize(x), wide_rows(torch, dy), dtype=torch.float32, out=store[:, 2:2 + N])
+    compare(f64(y), want, bound + ref.rounding(np.abs(want) + bound, "float32"), "fp32")
+    assert (store[:, :2] == 3).all() and (store[:, 2 + N:] == 3).all()
+    y = fp8.weight_gradient(fp8.quantize(x), dy, dtype=torch.bfloat16)
+    compare(f64(y), want, bound + ref.rounding(np.abs(want) + bound, "bfloat16"), "bf16")
