@@ -125,8 +125,9 @@ __global__ __launch_bounds__(256, TILE == 256 || PARTS > 1 ? 1 : 2) void qg_fp8_
   const bool narrow = p.n < CW;
   const int xc = row_tile * TILE + cx, yc = column_tile * TILE + cy;
   typedef typename qg_elem<TYPE>::t T;
-  const uint8_t* const x_base = p.x8.codes + (long long)(t0 + 8 * tb) * p.x8.pitch + xc;
-  const uint8_t* const s_base = p.x8.scales + (long long)(t0 + 8 * tb) * p.x8.scale_pitch + xc / QG_FP8_BLOCK;
+  // addresses: what all threads share, which moves on token by token, and this thread's part
+  const unsigned x_mine = (unsigned)(8 * tb) * (unsigned)p.x8.pitch + (unsigned)xc;
+  const unsigned s_mine = (unsigned)(8 * tb) * (unsigned)p.x8.scale_pitch + (unsigned)(xc / QG_FP8_BLOCK);
   const T* const y_base = static_cast<const T*>(p.dy.data) + (long long)(t0 + 8 * tb) * p.dy.stride + yc;
   unsigned xraw[8][CW / 4], xs[8];
   dy_line<TYPE, PARTS, CW> y[8];
@@ -141,9 +142,9 @@ __global__ __launch_bounds__(256, TILE == 256 || PARTS > 1 ? 1 : 2) void qg_fp8_
     xs[i] = from_memory<uint8_t>(scale);
   };
   auto fetch = [&](int from, int i, bool inside) {  // token i of this thread's eight
-    const long long at = from - t0 + i;
-    const uint8_t *src = x_base + at * p.x8.pitch, *scale = s_base + at * p.x8.scale_pitch;
-    const T* dy = y_base + at * p.dy.stride;
+    const uint8_t* const src = p.x8.codes + (long long)(from + i) * p.x8.pitch + x_mine;
+    const uint8_t* const scale = p.x8.scales + (long long)(from + i) * p.x8.scale_pitch + s_mine;
+    const T* dy = y_base + (long long)(from - t0 + i) * p.dy.stride;
     if (inside && !narrow) {
       fetch_x(src, scale, i);
       y[i].load(dy);
@@ -158,12 +159,19 @@ __global__ __launch_bounds__(256, TILE == 256 || PARTS > 1 ? 1 : 2) void qg_fp8_
       }
     }
   };
-  // A stage's planes: [32 columns][TS / 16 steps][2 halves of 8 tokens][32 columns, turned by the number of the 32][8 tokens].  Two columns
-  // of this thread's eight tokens go there in SLICES pieces.
-  unsigned line[8], part[8][PARTS];
-  auto place = [&](uint8_t* plane, int column, unsigned a0, unsigned a1, unsigned a2, unsigned a3) {
+  // A stage's planes: [32 columns][TS / 16 steps][2 halves of 8 tokens][32 columns, turned by the number of their 16][8 tokens]: the 16 lanes
+  // whose 16 bytes are written, or read, at a time go through all banks.  Two columns of this thread's eight tokens go there in SLICES
+  // pieces.
+  auto place_of = [&](int column) {
     const int f = column / 32;
-    *reinterpret_cast<u4*>(plane + (f * STEPS + tb / 2) * 1024 + (tb & 1) * 512 + ((column % 32) ^ (f & 7)) * 16) = (u4){a0, a1, a2, a3};
+    return (unsigned)((f * STEPS + tb / 2) * 1024 + (tb & 1) * 512 + ((column % 32) ^ (column >> 4 & 7)) * 16);
+  };
+  unsigned x_place[CW], y_place[CW];
+#pragma unroll
+  for (int k = 0; k < CW; ++k) x_place[k] = place_of(cx + k), y_place[k] = place_of(cy + k);
+  unsigned line[8], part[8][PARTS];
+  auto place = [&](uint8_t* plane, unsigned to, unsigned a0, unsigned a1, unsigned a2, unsigned a3) {
+    *reinterpret_cast<u4*>(plane + to) = (u4){a0, a1, a2, a3};
   };
   constexpr int SLICES = 6 + 2 * PARTS;
   auto store = [&](uint8_t* stage, int pair, int slice) {
@@ -178,16 +186,16 @@ __global__ __launch_bounds__(256, TILE == 256 || PARTS > 1 ? 1 : 2) void qg_fp8_
         }
       }
     } else if (slice == 2) {
-      place(stage, cx + 2 * pair, pair_low(line[0], line[1]), pair_low(line[2], line[3]), pair_low(line[4], line[5]), pair_low(line[6], line[7]));
+      place(stage, x_place[2 * pair], pair_low(line[0], line[1]), pair_low(line[2], line[3]), pair_low(line[4], line[5]), pair_low(line[6], line[7]));
     } else if (slice == 3) {
-      place(stage, cx + 2 * pair + 1, pair_high(line[0], line[1]), pair_high(line[2], line[3]), pair_high(line[4], line[5]), pair_high(line[6], line[7]));
+      place(stage, x_place[2 * pair + 1], pair_high(line[0], line[1]), pair_high(line[2], line[3]), pair_high(line[4], line[5]), pair_high(line[6], line[7]));
     } else {
       const int q = (slice - 6) / 2;
       if (slice % 2 == 0) {
-        place(stage + (1 + q) * PLANE, cy + 2 * pair, pair_low(part[0][q], part[1][q]), pair_low(part[2][q], part[3][q]),
+        place(stage + (1 + q) * PLANE, y_place[2 * pair], pair_low(part[0][q], part[1][q]), pair_low(part[2][q], part[3][q]),
             pair_low(part[4][q], part[5][q]), pair_low(part[6][q], part[7][q]));
       } else {
-        place(stage + (1 + q) * PLANE, cy + 2 * pair + 1, pair_high(part[0][q], part[1][q]), pair_high(part[2][q], part[3][q]),
+        place(stage + (1 + q) * PLANE, y_place[2 * pair + 1], pair_high(part[0][q], part[1][q]), pair_high(part[2][q], part[3][q]),
             pair_high(part[4][q], part[5][q]), pair_high(part[6][q], part[7][q]));
       }
     }
@@ -201,8 +209,9 @@ __global__ __launch_bounds__(256, TILE == 256 || PARTS > 1 ? 1 : 2) void qg_fp8_
 #pragma unroll
       for (int e = 0; e < 16; ++e) c[i][j][e] = 0.0f;
   const int wr = wave >> 1, wc = wave & 1;
+  const unsigned operand_at = (unsigned)((lane >> 5) * 512 + ((lane & 31) ^ (lane >> 4 & 1)) * 16);
   auto operand = [&](const uint8_t* plane, int f, int step) {
-    return *reinterpret_cast<const b8*>(plane + (f * STEPS + step) * 1024 + (lane >> 5) * 512 + ((lane & 31) ^ (f & 7)) * 16);
+    return *reinterpret_cast<const b8*>(plane + (f * STEPS + step) * 1024 + (operand_at ^ (unsigned)((2 * f & 7) * 16)));
   };
   if (t0 < t1) {
 #pragma unroll
@@ -229,8 +238,10 @@ __global__ __launch_bounds__(256, TILE == 256 || PARTS > 1 ? 1 : 2) void qg_fp8_
       for (int i = 0; i < F; ++i) x[0][i] = operand(stage, wr * F + i, 0);
 #pragma unroll
       for (int q = 0; q < PARTS; ++q) g[0][q] = operand(stage + (1 + q) * PLANE, wc * F, 0);
-      // the matrix instructions of a stage, one by one: the first half with pieces of the next stage's way to LDS, the second with requests
-      constexpr int PRODUCTS = GROUPS * PARTS * F, HALF = PRODUCTS / 2, ALL = PAIRS * SLICES;
+      // The matrix instructions of a stage, one by one: first with pieces of the next stage's way to LDS, then with the requests of the stage
+      // behind it, which have the rest of this stage to arrive
+      constexpr int PRODUCTS = GROUPS * PARTS * F, PIECES = PAIRS * SLICES;
+      constexpr int MOVE = PARTS == 1 ? PRODUCTS * 3 / 8 : PRODUCTS / 2, REQUEST = PRODUCTS / 8 < 8 ? PRODUCTS / 4 : 8;
       each<0, PRODUCTS>([&](auto number) {
         constexpr int n = decltype(number)::value, group = n / (PARTS * F), q = n / F % PARTS, i = n % F, s = group / F, j = group % F;
         if constexpr (n % (PARTS * F) == 0) {
@@ -240,20 +251,18 @@ __global__ __launch_bounds__(256, TILE == 256 || PARTS > 1 ? 1 : 2) void qg_fp8_
           }
           if constexpr (s + 1 < STEPS) x[(s + 1) & 1][j] = operand(stage, wr * F + j, s + 1);  // a part of the next step's rows with every group
         }
-        if constexpr (n < HALF) {
-          constexpr int first = n * ALL / HALF, last = (n + 1) * ALL / HALF;
+        if constexpr (n < MOVE) {
+          constexpr int first = n * PIECES / MOVE, last = (n + 1) * PIECES / MOVE;
           each<first, last>([&](auto piece) {
             constexpr int e = decltype(piece)::value;
             store(other, e / SLICES, e % SLICES);
           });
-        } else {
-          constexpr int first = (n - HALF) * 8 / HALF, last = (n - HALF + 1) * 8 / HALF;
-          if constexpr (first < last) {
-            if (inside) {
-              each<first, last>([&](auto token) { fetch(ahead, decltype(token)::value, true); });
-            } else {
-              each<first, last>([&](auto token) { fetch(ahead, decltype(token)::value, false); });
-            }
+        } else if constexpr (n < MOVE + REQUEST) {
+          constexpr int first = (n - MOVE) * 8 / REQUEST, last = (n - MOVE + 1) * 8 / REQUEST;
+          if (inside) {
+            each<first, last>([&](auto token) { fetch(ahead, decltype(token)::value, true); });
+          } else {
+            each<first, last>([&](auto token) { fetch(ahead, decltype(token)::value, false); });
           }
         }
         add_product<TILE>(c[i][j], g[group & 1][q], x[s & 1][i]);

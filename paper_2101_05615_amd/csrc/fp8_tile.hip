@@ -168,7 +168,7 @@ template <typename A>
 constexpr int gated_lds() { return batch_of<A>() * 4 * ITEM_F4 * 16 + 3 * (batch_of<A>() / (A::ITEMS * A::FRAGMENT / A::ROWS)) * A::FRAGMENT * 4; }
 
 template <typename A, bool BACK>
-__device__ inline void finish_gated(const qg_fp8_product_args& p, const A& acc, const place& at, int wave, int lane, f4* lds) {
+__device__ inline void finish_gated(const qg_fp8_product_args& p, A& acc, const place& at, int wave, int lane, f4* lds) {
   constexpr int BATCH = batch_of<A>(), PER_ROW = A::ITEMS * A::FRAGMENT / A::ROWS, ROWS = BATCH / PER_ROW * A::FRAGMENT;
   const int group = at.column_tile * 4 + wave, padded = at.column_tiles * 128, last_row = p.tokens - 1;
   f4* const mine = lds + wave * BATCH * ITEM_F4 + lane;
@@ -181,6 +181,7 @@ __device__ inline void finish_gated(const qg_fp8_product_args& p, const A& acc, 
     for (int e = (int)threadIdx.x; e < 3 * ROWS; e += 256) tops[e] = 0u;
     each<0, BATCH>([&](auto item) {
       constexpr int t = decltype(item)::value;
+      acc.template here<b0 + t>();
 #pragma unroll
       for (int j = 0; j < 4; ++j) mine[t * ITEM_F4 + j * 64] = acc.template quad<b0 + t>(j);
     });
@@ -306,25 +307,26 @@ struct row_requests {
   }
 };
 
-// One block of K a turn, in both kernels.  At its end all its requests have arrived: the weights of the next block, which take the place
-// of its own behind their last use, and the rows of the block after that, which the other waves may read behind the next barrier.  The barrier
-// comes late in a turn, when nobody waits at it, and two fragments before its end, so that the first reads of the next block are there in time.
-// Requests go out between the matrix instructions, in whose shadow they cost nothing.
+// One block of K a turn, in both kernels.  The weights are requested two turns before their own, and the compiler's wait for them at its
+// start -- no more than the loads of the turn between may still be on their way -- takes the rows in that were requested in front of those.  The
+// barrier behind which the other waves' rows of the next block may be read comes late in a turn, when nobody waits at it, and two fragments
+// before its end, so that the first reads of the next block are there in time.  Requests go out between the matrix instructions, in
+// whose shadow they cost nothing.  (8192^3 on the larger tiles: weights one turn ahead, and the rows and weights of a turn waited for at its
+// end, 509 us.)
 
 struct piece {  // a wave's weights of one block of K
   u4 x[4][2];
   unsigned scales;
-  __device__ inline void load(const uint8_t* from, int i) { x[i / 2][i % 2] = *reinterpret_cast<const u4*>(from + i * 1024); }
-  __device__ inline void arrived() {  // (in registers from here on: the compiler waits in front of this)
+  __device__ inline void load(const uint8_t* from, const uint32_t* s) {
 #pragma unroll
-    for (int j = 0; j < 4; ++j) asm volatile("" : "+v"(x[j][0]), "+v"(x[j][1]));
-    asm volatile("" : "+v"(scales));
+    for (int i = 0; i < 8; ++i) x[i / 2][i % 2] = *reinterpret_cast<const u4*>(from + i * 1024);
+    scales = *s;
   }
 };
 
 // WIDE: sums by the bf16 instructions
 template <int MF, int END, bool WIDE>
-__global__ __launch_bounds__(256, WIDE && MF == 8 ? 1 : 2) void qg_fp8_tile_kernel(qg_fp8_product_args p, int row_tiles, int column_tiles) {
+__global__ __launch_bounds__(256, 1) void qg_fp8_tile_kernel(qg_fp8_product_args p, int row_tiles, int column_tiles) {
   typedef small<MF> A;
   constexpr int ROWS = A::ROWS, STAGE = ROWS * 128, RING = 4;
   static_assert(MF % RING == 0, "a fragment's registers");
@@ -352,59 +354,69 @@ __global__ __launch_bounds__(256, WIDE && MF == 8 ? 1 : 2) void qg_fp8_tile_kern
     x[i % RING][1] = *reinterpret_cast<const u4*>(lds + stage * STAGE + i * 2048 + read1);
     xs[i % RING] = lds[STAGES * STAGE + (kb >> 2 & 1) * (ROWS * 4) + i * 64 + m * 4 + (kb & 3)];
   };
-  piece now;
-  int stage = 0;  // of the block that is multiplied
+  piece w0, w1, w2;
+  int stage = 0, kb = k0;
   request.four_scales(k0);
 #pragma unroll
   for (int r = 0; r < request.N; ++r) request.rows(0, k0, r);
 #pragma unroll
   for (int r = 0; r < request.N; ++r) request.rows(1, min(k0 + 1, k1 - 1), r);
-#pragma unroll
-  for (int i = 0; i < 8; ++i) now.load(pieces + (size_t)k0 * QG_FP8_PIECE, i);
-  now.scales = weight_scales[k0];
+  w0.load(pieces + (size_t)k0 * QG_FP8_PIECE, weight_scales + k0);
+  w1.load(pieces + (size_t)min(k0 + 1, k1 - 1) * QG_FP8_PIECE, weight_scales + min(k0 + 1, k1 - 1));
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
   __builtin_amdgcn_s_barrier();
   asm volatile("" ::: "memory");
   read(0, k0, 0);
   read(0, k0, 1);
-  for (int kb = k0; kb < k1; ++kb) {
+  auto turn = [&](piece& now, piece& last) {
     const int ahead = stage + 2 >= STAGES ? stage + 2 - STAGES : stage + 2, after = stage + 1 == STAGES ? 0 : stage + 1;
-    const int next_kb = min(kb + 1, k1 - 1), rows_kb = min(kb + 2, k1 - 1);   // (past the end: the last block again, not used)
-    const uint8_t* const next_piece = pieces + (size_t)next_kb * QG_FP8_PIECE;
-    piece next;
+    const int last_kb = min(kb + 2, k1 - 1);   // (past the end: the last block again, not used)
     if ((kb & 3) == 1 && kb + 3 < k1) request.four_scales(kb + 3);
-    next.scales = weight_scales[next_kb];
     read(stage, kb, 2);
-    constexpr int LOADS = MF >= 8 ? 1 : 4;   // of weights, in the shadow of a fragment
+    typename std::conditional<WIDE, wide, int>::type w[4];
+    if constexpr (WIDE) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) w[j] = wide(now.x[j][0], now.x[j][1], scale_of(now.scales >> (8 * j) & 255u));
+    }
 #pragma unroll
     for (int i = 0; i < MF; ++i) {
       if (i + 3 < MF) read(stage, kb, i + 3);
-      if (i == MF - 2) {
-        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+      if (i == 0) {
+#pragma unroll
+        for (int r = 0; r < request.N; ++r) request.rows(ahead, last_kb, r);
+      }
+      if (i == 1) last.load(pieces + (size_t)last_kb * QG_FP8_PIECE, weight_scales + last_kb);
+      if (i == MF - 2) {  // the rows that were requested in the turn before: behind them came its 9 loads, and the requests and loads of this turn
+        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(18 + request.N) : "memory");
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
       }
       if (i >= MF - 2) read(after, kb + 1, i - (MF - 2));
-      if (i < request.N) request.rows(ahead, rows_kb, i);
-      if (i * LOADS < 8) {
-#pragma unroll
-        for (int l = 0; l < LOADS; ++l) next.load(next_piece, i * LOADS + l);
-      }
-      if (i == MF - 1) next.arrived();
       if constexpr (WIDE) {
         const wide r(x[i % RING][0], x[i % RING][1], scale_of(xs[i % RING]));
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
-          acc.c[i][j] = wide_product(wide(now.x[j][0], now.x[j][1], scale_of(now.scales >> (8 * j) & 255u)), r, acc.c[i][j]);
+        for (int j = 0; j < 4; ++j) acc.c[i][j] = wide_product(w[j], r, acc.c[i][j]);
       } else {
         const i8v r = both(x[i % RING][0], x[i % RING][1]);
 #pragma unroll
         for (int j = 0; j < 4; ++j) acc.c[i][j] = matrix_product(both(now.x[j][0], now.x[j][1]), r, acc.c[i][j], j, now.scales, xs[i % RING]);
       }
-      if (i < MF - 1) __builtin_amdgcn_sched_barrier(0);
+      __builtin_amdgcn_sched_barrier(0);
     }
-    now = next;
     stage = after;
+    ++kb;
+  };
+#pragma unroll 1
+  for (int rest = (k1 - k0) % 3; rest > 0; --rest) {  // turns that do not make three: what is on its way is waited for, and moves on
+    turn(w0, w2);
+    w0 = w1;
+    w1 = w2;
+  }
+#pragma unroll 1
+  while (kb < k1) {  // (three turns are one piece of code: nothing that is on its way can change its registers)
+    turn(w0, w2);
+    turn(w1, w0);
+    turn(w2, w1);
   }
   asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");   // (what was requested past the end)
 
@@ -491,69 +503,92 @@ __global__ __launch_bounds__(256, 1) void qg_fp8_tile256_kernel(qg_fp8_product_a
       for (int e = 0; e < 2; ++e) x[to][h][e] = *reinterpret_cast<const u4*>(lds + stage * STAGE + i * 4096 + place_of[h][e]);
     xs[to] = lds[STAGES * STAGE + (kb >> 2 & 1) * (ROWS * 4) + i * 128 + m * 4 + (kb & 3)];
   };
-  u4 now[2][2][2], next[2][2][2];  // [operand][half][chunk]
-  unsigned now_scales, next_scales;
-  auto load = [&](u4 (&w)[2][2][2], const uint8_t* from, int i) {
-    w[i >> 2][i >> 1 & 1][i & 1] = *reinterpret_cast<const u4*>(from + (i >> 2) * 4096 + (i >> 1 & 1) * 1024 + (i & 1) * 256);
+  // The weights of this block, of the next and of the one after that: each is requested in the second half of a turn and arrives at the end
+  // of the next.  What the compiler waits for there is that no more than the requests behind it are on their way; it counts its own, so
+  // it waits for the rows of this turn too, which therefore go first.
+  struct weights {
+    u4 x[2][2][2];  // [operand][half][chunk]
+    unsigned scales;
+    __device__ inline void load(const uint8_t* from, int i) {
+      x[i >> 2][i >> 1 & 1][i & 1] = *reinterpret_cast<const u4*>(from + (i >> 2) * 4096 + (i >> 1 & 1) * 1024 + (i & 1) * 256);
+    }
   };
-  int stage = 0;
+  weights w0, w1, w2;
+  int stage = 0, kb = 0;
   request.four_scales(0);
 #pragma unroll
   for (int r = 0; r < request.N; ++r) request.rows(0, 0, r);
 #pragma unroll
   for (int r = 0; r < request.N; ++r) request.rows(1, min(1, kbs - 1), r);
 #pragma unroll
-  for (int i = 0; i < 8; ++i) load(now, pieces, i);
-  now_scales = weight_scales[0] >> scale_shift;
+  for (int i = 0; i < 8; ++i) w0.load(pieces, i);
+  w0.scales = weight_scales[0];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) w1.load(pieces + (size_t)min(1, kbs - 1) * QG_FP8_PIECE, i);
+  w1.scales = weight_scales[min(1, kbs - 1)];
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
   __builtin_amdgcn_s_barrier();
   asm volatile("" ::: "memory");
   read(0, 0, 0, 0);
   read(0, 0, 1, 1);
-  for (int kb = 0; kb < kbs; ++kb) {
+  // (three turns are one piece of code: nothing that is on its way can change its registers)
+  auto turn = [&](auto phase, weights& now, weights& last) {
+    constexpr int first = decltype(phase)::value * 8;
     const int ahead = stage + 2 >= STAGES ? stage + 2 - STAGES : stage + 2, after = stage + 1 == STAGES ? 0 : stage + 1;
-    const int next_kb = min(kb + 1, kbs - 1), rows_kb = min(kb + 2, kbs - 1);   // (past the end: the last block again, not used)
-    const uint8_t* const next_piece = pieces + (size_t)next_kb * QG_FP8_PIECE;
+    const int rows_kb = min(kb + 2, kbs - 1);   // (past the end: the last block again, not used)
+    const uint8_t* const last_piece = pieces + (size_t)rows_kb * QG_FP8_PIECE;
     if ((kb & 3) == 1 && kb + 3 < kbs) request.four_scales(kb + 3);
-    next_scales = weight_scales[next_kb];
+    const unsigned scales = now.scales >> scale_shift;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      if (i + 2 < 8) read(stage, kb, i + 2, (i + 2) % RING);
-      if (i == 6) {
-        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+      if (i + 2 < 8) read(stage, kb, i + 2, (first + i + 2) % RING);
+      if (i == 6) {  // the rows that were requested in the turn before: behind them came its 9 loads, and 8 requests and 4 loads of this turn
+        asm volatile("s_waitcnt vmcnt(21) lgkmcnt(0)" ::: "memory");
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
-        read(after, kb + 1, 0, 2);   // (fragment 8, as it were: the ring goes on)
       }
-      if (i == 7) read(after, kb + 1, 1, 0);
-      request.rows(ahead, rows_kb, i);
-      load(next, next_piece, i);
-      const unsigned s = xs[i % RING];
+      if (i >= 6) read(after, kb + 1, i - 6, (first + i + 2) % RING);
+      if (i < 2) {
+#pragma unroll
+        for (int r = 0; r < 4; ++r) request.rows(ahead, rows_kb, 4 * i + r);
+      }
+      if (i >= 4) {
+        last.load(last_piece, 2 * i - 8);
+        last.load(last_piece, 2 * i - 7);
+        if (i == 7) last.scales = weight_scales[rows_kb];
+      }
+      constexpr int at_phase = first;
+      const int at = (at_phase + i) % RING;
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        const i8v r = both(x[i % RING][h][0], x[i % RING][h][1]);
-        add_product<0>(acc.c[i][0], both(now[0][h][0], now[0][h][1]), r, now_scales, s);
-        add_product<1>(acc.c[i][1], both(now[1][h][0], now[1][h][1]), r, now_scales, s);
+        const i8v r = both(x[at][h][0], x[at][h][1]);
+        add_product<0>(acc.c[i][0], both(now.x[0][h][0], now.x[0][h][1]), r, scales, xs[at]);
+        add_product<1>(acc.c[i][1], both(now.x[1][h][0], now.x[1][h][1]), r, scales, xs[at]);
       }
       __builtin_amdgcn_sched_barrier(0);
     }
-    // the ring starts with fragment 0 again
-    u4 t[2][2];
-    unsigned ts = xs[2];
+    stage = after;
+    ++kb;
+  };
+#pragma unroll 1
+  for (int rest = kbs % 3; rest > 0; --rest) {  // turns that do not make three: what is on its way is waited for, and moves on
+    turn(std::integral_constant<int, 0>(), w0, w2);
+    w0 = w1;
+    w1 = w2;
+    const u4 t[2][2] = {{x[2][0][0], x[2][0][1]}, {x[2][1][0], x[2][1][1]}};
+    const unsigned ts = xs[2];
 #pragma unroll
     for (int h = 0; h < 2; ++h)
 #pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        t[h][e] = x[2][h][e];
-        x[1][h][e] = x[0][h][e];
-        x[0][h][e] = t[h][e];
-      }
+      for (int e = 0; e < 2; ++e) x[1][h][e] = x[0][h][e], x[0][h][e] = t[h][e];
     xs[1] = xs[0];
     xs[0] = ts;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) now[i >> 2][i >> 1 & 1][i & 1] = next[i >> 2][i >> 1 & 1][i & 1];
-    now_scales = next_scales >> scale_shift;
-    stage = after;
+  }
+#pragma unroll 1
+  while (kb < kbs) {
+    turn(std::integral_constant<int, 0>(), w0, w2);
+    turn(std::integral_constant<int, 1>(), w1, w0);
+    turn(std::integral_constant<int, 2>(), w2, w1);
   }
   asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_nop 15\n\ts_nop 15" ::: "memory");   // (what was requested past the end; the last products)
 #pragma unroll
