@@ -633,7 +633,7 @@ int qg_kv4_attention(const qg_kv4_cache* c, const qg_kv4_attention_params* p, vo
  * of eight neighbours in K to the largest of them, drop what lies 2^-13 below it, and
  * sum the rest in fp32: about 2e-5 of a result's typical size.  With wide_sums = 1 a
  * product runs on the bf16 cores instead, all sums fp32, at half the rate where there
- * are many rows (up to 64 rows every product does).  A result is rounded once. */
+ * are many rows (with few, up to 64 at least, every product does).  A result is rounded once. */
 
 /* A matrix [tokens][channels] with unit channel stride; the stride counts elements,
  * any sign, any alignment that the element type has by itself. */
@@ -680,8 +680,8 @@ typedef struct {
 int qg_fp8_pack(const qg_matrix* b, const qg_matrix* up, int k, int n, int dtype, const qg_fp8_weight* w,
                 const qg_fp8_weight* transposed, void* stream);
 
-/* Up to this many tokens the products below take activations as they are and put them
- * into 8 bits on the way (the result is the same). */
+/* Up to this many tokens, and with k a multiple of 16, the products below take activations as
+ * they are and put them into 8 bits on the way (the result is the same). */
 #define QG_FP8_FEW 16
 
 #define QG_SILU 0         /* g / (1 + exp(-g))                                  */

@@ -59,13 +59,11 @@ int check_workspace(void* workspace, size_t bytes) {
 constexpr int COUNTERS = QG_FP8_COUNTER_BYTES / 4;
 constexpr long long PARTIALS = (32 << 20) / 4;  // floats
 
-// Workgroups that share K: `parts` without, `floats` of sums each, `wanted` workgroups in all, at least `least` blocks of K each
-void deal(qg_fp8_product_args* a, void* workspace, long long parts, long long floats, int wanted, int least) {
+// K in `slices` parts, each whole quads of blocks, for `parts` workgroups that leave `floats` of sums each
+void deal(qg_fp8_product_args* a, void* workspace, long long parts, long long floats, long long slices) {
   a->slices = 1;
   a->slice_kb = a->w.kb;
   if (!workspace || parts > COUNTERS) return;
-  long long slices = wanted / parts;
-  if (slices > a->w.kb / least) slices = a->w.kb / least;
   if (slices > PARTIALS / (parts * floats)) slices = PARTIALS / (parts * floats);
   if (slices < 2) return;
   a->slice_kb = qg_fp8_up((a->w.kb + (int)slices - 1) / (int)slices, 4);
@@ -73,25 +71,53 @@ void deal(qg_fp8_product_args* a, void* workspace, long long parts, long long fl
   a->counters = static_cast<int*>(workspace);
   a->partial = reinterpret_cast<float*>(a->counters + COUNTERS);
 }
+long long at_most(long long a, long long b) { return a < b ? a : b; }
+
+// ---- which kernel, and how K is dealt.  Measured in graphs, weights of 600 MB in turn where they are large, every form on each shape (us, K x N).
+//
+// The streaming kernel, up to 64 rows and beyond where its workgroups of 32 rows x 64 slots have little to do: 200 rows of 4096 x 4096 17.9
+// (tiles 19.2), 300 rows 25.0 (19.8), 300 rows of 2816 x 1024 7.7 (23).  Up to 16 rows it has one row fragment, beyond two.
+//   Weight fragments: four a workgroup where that makes enough workgroups; two otherwise, rather than K dealt over workgroups, whose sums
+//   meet in memory (1 row of 4096 x 4096: 6.8 in two, 7.6 in four dealt twice; 16 rows of 1024 x 8192: 5.0 in four, 5.3 in two).
+//   A long K is dealt: 1 row of 10240 x 4096 12.6 in four slices, 13.6 whole; 16 rows 13.3 and 14.8; 8192 x 8192 16.3 and 17.8.
+//   Waves: four where there is a workgroup for every CU or a short K, eight otherwise (16 rows of 8192 x 8192: 16.6 with four, 17.2).
+bool streams(const qg_fp8_product_args& a) {
+  return a.tokens <= 64 || (a.tokens <= 1024 && (a.tokens + 31ll) / 32 * a.w.groups * a.w.kb <= 16000);
+}
+qg_fp8_stream_form stream_form(qg_fp8_product_args* a, void* workspace) {
+  qg_fp8_stream_form f = {a->tokens <= 16 ? 1 : 2, 4, 8};
+  const long long blocks = (a->tokens + 16 * f.rows - 1) / (16 * f.rows), units = blocks * a->w.groups;
+  const bool dealt = workspace && a->w.kb > 40;
+  if (!dealt && units < (f.rows == 1 ? 80 : 150)) f.fragments = 2;
+  if (f.rows == 1 && (dealt ? a->tokens > 8 : a->w.kb < 16 || units * (4 / f.fragments) >= 256)) f.waves = 4;
+  deal(a, workspace, units * (4 / f.fragments), f.rows * f.fragments * 256ll, dealt ? at_most((256 + units - 1) / units, a->w.kb / 16) : 1);
+  return f;
+}
+
+// Tiles: 256 rows where that leaves few CUs without one; 64 rows rather than 128 up to 160 of them (300 rows of 4096 x 4096 19.8 and 26.7,
+// 512 rows of 8192 x 8192 54 and 46).  Sums that meet in memory cost as much as several blocks of K, so K is dealt only while that fills
+// the CUs, and in pieces of eight blocks at least (300 rows of 1024 x 1024 12 whole, 17 in two).
+int tile_form(qg_fp8_product_args* a, int wide_sums, void* workspace) {
+  const long long columns = a->w.groups / 4;
+  auto tiles = [&](int rows) { return (a->tokens + rows - 1ll) / rows * columns; };
+  a->slices = 1;
+  a->slice_kb = a->w.kb;
+  if (!wide_sums && tiles(256) >= 200) return 16;
+  const int fragments = tiles(64) <= 160 ? 4 : 8;
+  const long long n = tiles(16 * fragments);
+  deal(a, workspace, n, fragments * 4096ll, at_most(256 / n, at_most(4, a->w.kb / 8)));
+  return fragments;
+}
 
 int product(const qg_fp8_product_args& args, int end, int wide_sums, void* workspace, hipStream_t s) {
   qg_fp8_product_args a = args;
-  const bool plain_out = a.out.data != nullptr && end != QG_FP8_GATED_BACK;
-  if (plain_out && a.tokens <= 64) {
-    const int rf = a.tokens <= 16 ? 1 : a.tokens <= 32 ? 2 : 4;
-    const int fragments = a.w.groups >= 256 ? 4 : 2, waves = rf == 4 ? 4 : 8;
-    const long long sets = (long long)a.w.groups * (4 / fragments);
-    deal(&a, workspace, sets, (long long)rf * fragments * 256, 256, 2 * waves);
-    if (sets * a.slices > 0x3fffffll) return QG_EUNSUPPORTED;
-    return done(qg_launch_fp8_stream(a, end == QG_FP8_GATED, fragments, waves, s));
+  if (a.out.data != nullptr && end != QG_FP8_GATED_BACK && streams(a)) {
+    const qg_fp8_stream_form f = stream_form(&a, workspace);
+    if ((a.tokens + 15ll) / 16 * a.w.groups * 4 * a.slices > 0x3fffffll) return QG_EUNSUPPORTED;
+    return done(qg_launch_fp8_stream(a, end == QG_FP8_GATED, f, s));
   }
-  const long long columns = a.w.groups / 4;
-  const int fragments = !wide_sums && (a.tokens + 255ll) / 256 * columns >= 200 ? 16 : a.tokens <= 64 ? 4 : 8;
-  const long long rows = (a.tokens + 16ll * fragments - 1) / (16 * fragments);
-  a.slices = 1;
-  a.slice_kb = a.w.kb;
-  if (fragments < 16) deal(&a, workspace, rows * columns, fragments * 4096ll, 256, 4);
-  if (rows * columns * a.slices > 0x7fffffll) return QG_EUNSUPPORTED;
+  const int fragments = tile_form(&a, wide_sums, workspace);
+  if ((a.tokens + 16ll * fragments - 1) / (16 * fragments) * (a.w.groups / 4) * a.slices > 0x7fffffll) return QG_EUNSUPPORTED;
   return done(qg_launch_fp8_tile(a, end, fragments, wide_sums, s));
 }
 
@@ -108,7 +134,7 @@ int check_product(const qg_fp8_weight* w, const qg_fp8_product* p, qg_fp8_produc
   } else {
     if (!p->x_rows.data) return QG_ENULL;
     if (!known(p->x_dtype)) return QG_EINVAL;
-    if (p->tokens > QG_FP8_FEW) return QG_EUNSUPPORTED;
+    if (p->tokens > QG_FP8_FEW || w->k % 16 != 0) return QG_EUNSUPPORTED;
     if ((rc = check_rows(p->x_rows, p->x_dtype, &a->x)) != QG_OK) return rc;
     a->x_type = p->x_dtype;
   }

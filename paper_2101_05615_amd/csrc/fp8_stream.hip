@@ -14,23 +14,20 @@ template <int X>
 struct raw_half {  // 16 channels of a token as they are
   static constexpr int N = X == QG_F32 ? 16 : 8;
   unsigned d[N];
-  __device__ inline void load(const qg_fp8_rows& x, int row, bool there, int channels, int first) {
+  __device__ inline void load(const qg_fp8_rows& x, int row, int channels, int first) {
     typedef typename qg_elem<X>::t T;
-    const T* from = static_cast<const T*>(x.data) + row * x.stride + first;
-    if (there && first + 16 <= channels) {
-      typedef u4 any __attribute__((aligned(2)));
+    const T* from = static_cast<const T*>(x.data) + row * x.stride + (first < channels ? first : 0);  // (channels: a multiple of 16)
+    typedef u4 any __attribute__((aligned(2)));
 #pragma unroll
-      for (int i = 0; i < N / 4; ++i) {
-        const u4 v = reinterpret_cast<const any*>(from)[i];
+    for (int i = 0; i < N / 4; ++i) {
+      const u4 v = reinterpret_cast<const any*>(from)[i];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) d[4 * i + j] = v[j];
-      }
-    } else {
-      T v[16];
-#pragma unroll
-      for (int i = 0; i < 16; ++i) v[i] = there && first + i < channels ? from[i] : (T)0.0f;
-      __builtin_memcpy(d, v, sizeof(v));
+      for (int j = 0; j < 4; ++j) d[4 * i + j] = v[j];
     }
+  }
+  __device__ inline void cut(bool there) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) d[i] = there ? d[i] : 0u;
   }
   // the bits in fp32 of the largest size
   __device__ inline unsigned top() const {
@@ -76,13 +73,14 @@ struct batch {
 
 template <int RF, int NF, int WAVES, int X, bool GATED>
 __global__ __launch_bounds__(64 * WAVES) void qg_fp8_stream_kernel(qg_fp8_product_args p) {
-  constexpr int U = NF == 2 && RF == 1 ? 2 : 1;  // blocks of a batch
+  constexpr int U = RF > 1 || NF == 4 ? 1 : 2;  // blocks of a batch
   constexpr int SETS = 4 / NF;
   __shared__ f4 sums[WAVES][RF * NF][64];
   __shared__ int ticket;
   const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   const int m = lane & 15, g = lane >> 4;
-  const int sets = p.w.groups * SETS, set = (int)blockIdx.x % sets, slice = (int)blockIdx.x / sets;
+  const int sets = p.w.groups * SETS, set = (int)blockIdx.x % sets, rest = (int)blockIdx.x / sets;
+  const int blocks = (p.tokens + 16 * RF - 1) / (16 * RF), row0 = rest % blocks * (16 * RF), slice = rest / blocks;
   const int group = set / SETS, first = set % SETS * NF;
   const int k0 = slice * p.slice_kb, k1 = min(k0 + p.slice_kb, p.w.kb);
   const uint8_t* const pieces = p.w.pieces + (size_t)group * p.w.kb * QG_FP8_PIECE + first * 2048 + lane * 16;
@@ -105,16 +103,15 @@ __global__ __launch_bounds__(64 * WAVES) void qg_fp8_stream_kernel(qg_fp8_produc
       b.ws[u] = weight_scales[at] >> (8 * first);
 #pragma unroll
       for (int i = 0; i < RF; ++i) {
-        const int row = 16 * i + m;
-        const bool there = row < p.tokens;
+        const int row = min(row0 + 16 * i + m, p.tokens - 1);   // (rows behind the last: that one again, not written)
         if constexpr (X == HELD) {
-          const uint8_t* from = p.x8.codes + (size_t)(there ? row : 0) * p.x8.pitch + (size_t)at * 128 + g * 16;
+          const uint8_t* from = p.x8.codes + (size_t)row * p.x8.pitch + (size_t)at * 128 + g * 16;
 #pragma unroll
-          for (int h = 0; h < 2; ++h) b.x[u][i][h] = there ? *reinterpret_cast<const u4*>(from + 64 * h) : (u4){0u, 0u, 0u, 0u};
-          b.xs[u][i] = there ? p.x8.scales[(size_t)row * p.x8.scale_pitch + at] : 0u;
+          for (int h = 0; h < 2; ++h) b.x[u][i][h] = *reinterpret_cast<const u4*>(from + 64 * h);
+          b.xs[u][i] = p.x8.scales[(size_t)row * p.x8.scale_pitch + at];
         } else {
 #pragma unroll
-          for (int h = 0; h < 2; ++h) b.raw[u][h].load(p.x, row, there, p.w.k, at * 128 + 64 * h + 16 * g);
+          for (int h = 0; h < 2; ++h) b.raw[u][h].load(p.x, row, p.w.k, at * 128 + 64 * h + 16 * g);
         }
       }
     }
@@ -124,6 +121,11 @@ __global__ __launch_bounds__(64 * WAVES) void qg_fp8_stream_kernel(qg_fp8_produc
     for (int u = 0; u < U; ++u) {
       if (kb + u * WAVES >= k1) break;
       if constexpr (X != HELD) {
+        const int at = kb + u * WAVES;
+        if ((at + 1) * 128 > p.w.k) {
+#pragma unroll
+          for (int h = 0; h < 2; ++h) b.raw[u][h].cut(at * 128 + 64 * h + 16 * g < p.w.k);
+        }
         b.xs[u][0] = scale_byte(max_over_quads(umax(b.raw[u][0].top(), b.raw[u][1].top())));
 #pragma unroll
         for (int h = 0; h < 2; ++h) b.x[u][0][h] = b.raw[u][h].codes(scale_of(b.xs[u][0]));
@@ -173,7 +175,8 @@ __global__ __launch_bounds__(64 * WAVES) void qg_fp8_stream_kernel(qg_fp8_produc
     }
   }
   if (p.slices > 1) {  // through memory, past the L2s that the XCDs do not share; the last one to arrive adds them in order
-    float* const mine = p.partial + (size_t)set * p.slices * (ITEMS * PER * 4);
+    const int part = set * blocks + rest % blocks;
+    float* const mine = p.partial + (size_t)part * p.slices * (ITEMS * PER * 4);
 #pragma unroll
     for (int t = 0; t < TURNS; ++t) {
       const int item = (int)threadIdx.x + t * 64 * WAVES;
@@ -184,10 +187,10 @@ __global__ __launch_bounds__(64 * WAVES) void qg_fp8_stream_kernel(qg_fp8_produc
     }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();
-    if (threadIdx.x == 0) ticket = __hip_atomic_fetch_add(p.counters + set, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    if (threadIdx.x == 0) ticket = __hip_atomic_fetch_add(p.counters + part, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     __syncthreads();
     if (ticket != p.slices - 1) return;
-    if (threadIdx.x == 0) __hip_atomic_store(p.counters + set, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);  // ready for the next call
+    if (threadIdx.x == 0) __hip_atomic_store(p.counters + part, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);  // ready for the next call
 #pragma unroll
     for (int t = 0; t < TURNS; ++t) {
       const int item = (int)threadIdx.x + t * 64 * WAVES;
@@ -213,7 +216,7 @@ __global__ __launch_bounds__(64 * WAVES) void qg_fp8_stream_kernel(qg_fp8_produc
     const int item = (int)threadIdx.x + t * 64 * WAVES;
     if (item >= ITEMS) break;
     const int part = item / 64, of = item % 64, i = part / (NF / PER), j = part % (NF / PER);
-    const int row = 16 * i + (of & 15);
+    const int row = row0 + 16 * i + (of & 15);
     const int column = GATED ? group * 32 + 8 * (of >> 4) + 4 * (first / 2 + j) : group * 64 + 16 * (of >> 4) + 4 * (first + j);
     if (row >= p.tokens || column >= p.channels) continue;
     float v[4];
@@ -231,31 +234,27 @@ __global__ __launch_bounds__(64 * WAVES) void qg_fp8_stream_kernel(qg_fp8_produc
 
 template <int RF, int NF, int WAVES, int X, bool GATED>
 hipError_t launch(const qg_fp8_product_args& a, hipStream_t s) {
-  const unsigned sets = (unsigned)(a.w.groups * (4 / NF));
-  hipLaunchKernelGGL((qg_fp8_stream_kernel<RF, NF, WAVES, X, GATED>), dim3(sets * (unsigned)a.slices), dim3(64 * WAVES), 0, s, a);
+  const unsigned sets = (unsigned)(a.w.groups * (4 / NF)), blocks = (unsigned)((a.tokens + 16 * RF - 1) / (16 * RF));
+  hipLaunchKernelGGL((qg_fp8_stream_kernel<RF, NF, WAVES, X, GATED>), dim3(sets * blocks * (unsigned)a.slices), dim3(64 * WAVES), 0, s, a);
   return hipGetLastError();
 }
 
-template <int NF, int WAVES, bool GATED>
-hipError_t launch_rows(const qg_fp8_product_args& a, hipStream_t s) {
-  if (a.x.data) {
-    return a.x_type == QG_F32    ? launch<1, NF, WAVES, QG_F32, GATED>(a, s)
-           : a.x_type == QG_BF16 ? launch<1, NF, WAVES, QG_BF16, GATED>(a, s)
-                                 : launch<1, NF, WAVES, QG_F16, GATED>(a, s);
-  }
-  if (a.tokens <= 16) return launch<1, NF, WAVES, HELD, GATED>(a, s);
-  if (a.tokens <= 32) return launch<2, NF, WAVES, HELD, GATED>(a, s);
-  return launch<4, NF, 4, HELD, GATED>(a, s);
+template <int RF, int NF, int WAVES, int X>
+hipError_t launch(const qg_fp8_product_args& a, int gated, hipStream_t s) {
+  return gated ? launch<RF, NF, WAVES, X, true>(a, s) : launch<RF, NF, WAVES, X, false>(a, s);
 }
-template <bool GATED>
-hipError_t launch_waves(const qg_fp8_product_args& a, int fragments, int waves, hipStream_t s) {
-  if (waves == 4) return fragments == 4 ? launch_rows<4, 4, GATED>(a, s) : launch_rows<2, 4, GATED>(a, s);
-  return fragments == 4 ? launch_rows<4, 8, GATED>(a, s) : launch_rows<2, 8, GATED>(a, s);
+template <int NF, int WAVES>
+hipError_t launch_few(const qg_fp8_product_args& a, int gated, hipStream_t s) {
+  if (!a.x.data) return launch<1, NF, WAVES, HELD>(a, gated, s);
+  return a.x_type == QG_F32    ? launch<1, NF, WAVES, QG_F32>(a, gated, s)
+         : a.x_type == QG_BF16 ? launch<1, NF, WAVES, QG_BF16>(a, gated, s)
+                               : launch<1, NF, WAVES, QG_F16>(a, gated, s);
 }
 
 }  // namespace
 
-hipError_t qg_launch_fp8_stream(const qg_fp8_product_args& a, int gated, int fragments, int waves, hipStream_t s) {
-  if (gated) return launch_waves<true>(a, fragments, waves, s);
-  return launch_waves<false>(a, fragments, waves, s);
+hipError_t qg_launch_fp8_stream(const qg_fp8_product_args& a, int gated, const qg_fp8_stream_form& f, hipStream_t s) {
+  if (f.rows == 2) return f.fragments == 4 ? launch<2, 4, 8, HELD>(a, gated, s) : launch<2, 2, 8, HELD>(a, gated, s);
+  if (f.fragments == 4) return f.waves == 4 ? launch_few<4, 4>(a, gated, s) : launch_few<4, 8>(a, gated, s);
+  return f.waves == 4 ? launch_few<2, 4>(a, gated, s) : launch_few<2, 8>(a, gated, s);
 }

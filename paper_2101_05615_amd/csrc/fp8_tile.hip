@@ -307,6 +307,43 @@ struct row_requests {
   }
 };
 
+// The matrix instructions, in place and in this order: the compiler moves 256 accumulators about between turns, and gathers the products of several
+// turns behind each other.  It does not know how long a result takes: whoever reads one waits (19 cycles of 4 after the last one).  Nor does it
+// know that operands are to be two cycles old if they were computed; in the shadow of the product before, waiting is free.
+template <int BYTE>  // 0 or 2, of scale_a
+__device__ inline void add_product(f16v& c, i8v a, i8v b, unsigned scale_a, unsigned scale_b) {
+  if (BYTE == 2) {
+    asm volatile("s_nop 1\n\tv_mfma_scale_f32_32x32x64_f8f6f4 %0, %1, %2, %0, %3, %4 op_sel_hi:[1,0,0]" : "+a"(c) : "v"(a), "v"(b), "v"(scale_a), "v"(scale_b));
+  } else {
+    asm volatile("s_nop 1\n\tv_mfma_scale_f32_32x32x64_f8f6f4 %0, %1, %2, %0, %3, %4 op_sel_hi:[0,0,0]" : "+a"(c) : "v"(a), "v"(b), "v"(scale_a), "v"(scale_b));
+  }
+}
+#define QG_ADD_PRODUCT(select) \
+  asm volatile("s_nop 1\n\tv_mfma_scale_f32_16x16x128_f8f6f4 %0, %1, %2, %0, %3, %4 " select : "+a"(c) : "v"(a), "v"(b), "v"(scale_a), "v"(scale_b))
+__device__ inline void add_product(f4& c, i8v a, i8v b, int byte, unsigned scale_a, unsigned scale_b) {
+  switch (byte) {  // (a constant)
+    case 0: QG_ADD_PRODUCT("op_sel_hi:[0,0,0]"); break;
+    case 1: QG_ADD_PRODUCT("op_sel:[1,0,0] op_sel_hi:[0,0,0]"); break;
+    case 2: QG_ADD_PRODUCT("op_sel_hi:[1,0,0]"); break;
+    default: QG_ADD_PRODUCT("op_sel:[1,0,0] op_sel_hi:[1,0,0]");
+  }
+}
+#undef QG_ADD_PRODUCT
+// Four row fragments' products with one of rows, a quarter of the block at a time: no product waits for the one before
+__device__ inline void add_products(f4 (&c)[4], const wide (&a)[4], const wide& b) {
+#pragma unroll
+  for (int k = 0; k < 4; ++k)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      if (j == 0) {
+        asm volatile("s_nop 1\n\tv_mfma_f32_16x16x32_bf16 %0, %1, %2, %0" : "+a"(c[j]) : "v"(a[j].x[k]), "v"(b.x[k]));
+      } else {
+        asm volatile("v_mfma_f32_16x16x32_bf16 %0, %1, %2, %0" : "+a"(c[j]) : "v"(a[j].x[k]), "v"(b.x[k]));
+      }
+    }
+}
+__device__ inline void products_done() { asm volatile("s_nop 15\n\ts_nop 15" ::: "memory"); }
+
 // One block of K a turn, in both kernels.  The weights are requested two turns before their own, and the compiler's wait for them at its
 // start -- no more than the loads of the turn between may still be on their way -- takes the rows in that were requested in front of those.  The
 // barrier behind which the other waves' rows of the next block may be read comes late in a turn, when nobody waits at it, and two fragments
@@ -377,6 +414,10 @@ __global__ __launch_bounds__(256, 1) void qg_fp8_tile_kernel(qg_fp8_product_args
     if constexpr (WIDE) {
 #pragma unroll
       for (int j = 0; j < 4; ++j) w[j] = wide(now.x[j][0], now.x[j][1], scale_of(now.scales >> (8 * j) & 255u));
+#pragma unroll
+      for (int j = 0; j < 4; ++j)  // (made here, more than two cycles before they are used)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) asm volatile("" : "+v"(w[j].x[k]));
     }
 #pragma unroll
     for (int i = 0; i < MF; ++i) {
@@ -394,12 +435,11 @@ __global__ __launch_bounds__(256, 1) void qg_fp8_tile_kernel(qg_fp8_product_args
       if (i >= MF - 2) read(after, kb + 1, i - (MF - 2));
       if constexpr (WIDE) {
         const wide r(x[i % RING][0], x[i % RING][1], scale_of(xs[i % RING]));
-#pragma unroll
-        for (int j = 0; j < 4; ++j) acc.c[i][j] = wide_product(w[j], r, acc.c[i][j]);
+        add_products(acc.c[i], w, r);
       } else {
         const i8v r = both(x[i % RING][0], x[i % RING][1]);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) acc.c[i][j] = matrix_product(both(now.x[j][0], now.x[j][1]), r, acc.c[i][j], j, now.scales, xs[i % RING]);
+        for (int j = 0; j < 4; ++j) add_product(acc.c[i][j], both(now.x[j][0], now.x[j][1]), r, j, now.scales, xs[i % RING]);
       }
       __builtin_amdgcn_sched_barrier(0);
     }
@@ -419,6 +459,11 @@ __global__ __launch_bounds__(256, 1) void qg_fp8_tile_kernel(qg_fp8_product_args
     turn(w2, w1);
   }
   asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");   // (what was requested past the end)
+  products_done();
+#pragma unroll
+  for (int i = 0; i < MF; ++i)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) asm volatile("" : "+a"(acc.c[i][j]));
 
   if (p.slices > 1) {  // sums of the slices through memory, past the L2s that the XCDs do not share; the last one to arrive adds them in order
     const int tile = at.row_tile * column_tiles + at.column_tile;
@@ -454,18 +499,6 @@ __global__ __launch_bounds__(256, 1) void qg_fp8_tile_kernel(qg_fp8_product_args
     }
   }
   finish<A, END>(p, acc, at, wave, lane, lds);
-}
-
-// The matrix instruction in place: with all 256 accumulator registers in use the compiler moves them about between turns.  It does not
-// know how long the result takes: whoever reads it waits (19 cycles of 4 after the last one).  Nor does it know that the operands are to be
-// two cycles old if they were computed; in the shadow of the product before, waiting is free.
-template <int HIGH>
-__device__ inline void add_product(f16v& c, i8v a, i8v b, unsigned scale_a, unsigned scale_b) {
-  if (HIGH) {  // byte 2 of scale_a
-    asm volatile("s_nop 1\n\tv_mfma_scale_f32_32x32x64_f8f6f4 %0, %1, %2, %0, %3, %4 op_sel_hi:[1,0,0]" : "+a"(c) : "v"(a), "v"(b), "v"(scale_a), "v"(scale_b));
-  } else {
-    asm volatile("s_nop 1\n\tv_mfma_scale_f32_32x32x64_f8f6f4 %0, %1, %2, %0, %3, %4 op_sel_hi:[0,0,0]" : "+a"(c) : "v"(a), "v"(b), "v"(scale_a), "v"(scale_b));
-  }
 }
 
 template <int END>
@@ -563,7 +596,7 @@ __global__ __launch_bounds__(256, 1) void qg_fp8_tile256_kernel(qg_fp8_product_a
       for (int h = 0; h < 2; ++h) {
         const i8v r = both(x[at][h][0], x[at][h][1]);
         add_product<0>(acc.c[i][0], both(now.x[0][h][0], now.x[0][h][1]), r, scales, xs[at]);
-        add_product<1>(acc.c[i][1], both(now.x[1][h][0], now.x[1][h][1]), r, scales, xs[at]);
+        add_product<2>(acc.c[i][1], both(now.x[1][h][0], now.x[1][h][1]), r, scales, xs[at]);
       }
       __builtin_amdgcn_sched_barrier(0);
     }
@@ -590,7 +623,8 @@ __global__ __launch_bounds__(256, 1) void qg_fp8_tile256_kernel(qg_fp8_product_a
     turn(std::integral_constant<int, 1>(), w1, w0);
     turn(std::integral_constant<int, 2>(), w2, w1);
   }
-  asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_nop 15\n\ts_nop 15" ::: "memory");   // (what was requested past the end; the last products)
+  asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");   // (what was requested past the end)
+  products_done();
 #pragma unroll
   for (int i = 0; i < 8; ++i) asm volatile("" : "+a"(acc.c[i][0]), "+a"(acc.c[i][1]));
   finish<A, END>(p, acc, at, wave, lane, lds);

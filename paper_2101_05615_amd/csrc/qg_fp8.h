@@ -96,7 +96,10 @@ hipError_t qg_launch_fp8_dequantize(const qg_fp8_held& x, int type, int tokens, 
 hipError_t qg_launch_fp8_pack(const qg_fp8_pack_args& a, int type, hipStream_t s);
 enum qg_fp8_end { QG_FP8_PLAIN, QG_FP8_GATED, QG_FP8_GATED_BACK };
 hipError_t qg_launch_fp8_tile(const qg_fp8_product_args& a, int end, int row_fragments, int wide_sums, hipStream_t s);
-hipError_t qg_launch_fp8_stream(const qg_fp8_product_args& a, int gated, int fragments, int waves, hipStream_t s);
+struct qg_fp8_stream_form {
+  int rows, fragments, waves;  // row and weight fragments of a workgroup, and the waves that share its K
+};
+hipError_t qg_launch_fp8_stream(const qg_fp8_product_args& a, int gated, const qg_fp8_stream_form& f, hipStream_t s);
 hipError_t qg_launch_fp8_gradient(const qg_fp8_gradient_args& a, int tile, hipStream_t s);
 
 #ifdef __HIPCC__

@@ -208,7 +208,7 @@ def _product(x, w, dtype, activation=0, bias=None, ws=None, out=None, wide_sums=
         held = x
     else:
         _check_rows(x)
-        held = None if tokens <= FEW else quantize(x)
+        held = None if tokens <= FEW and k % 16 == 0 else quantize(x)
     if held is not None:
         p.x = held._desc
     else:
