@@ -211,6 +211,7 @@ __global__ __launch_bounds__(64 * WAVES) void qg_fp8_stream_kernel(qg_fp8_produc
       }
     }
   }
+  const activation act(p.activation);
 #pragma unroll
   for (int t = 0; t < TURNS; ++t) {
     const int item = (int)threadIdx.x + t * 64 * WAVES;
@@ -223,7 +224,7 @@ __global__ __launch_bounds__(64 * WAVES) void qg_fp8_stream_kernel(qg_fp8_produc
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
       if (GATED) {
-        v[r] = activate<false>(p.activation, s[t][0][r], nullptr) * s[t][PER - 1][r];
+        v[r] = act.operator()<false>(s[t][0][r], nullptr) * s[t][PER - 1][r];
       } else {
         v[r] = s[t][0][r] + (p.bias && column + r < p.channels ? p.bias[column + r] : 0.0f);
       }

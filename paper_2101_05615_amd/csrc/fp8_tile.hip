@@ -141,125 +141,179 @@ __device__ inline void finish_plain(const qg_fp8_product_args& p, A& acc, const 
   }
 }
 
-template <int TYPE>
-__device__ inline void get(const qg_fp8_rows& from, int row, int column, int columns, float* v) {
-  typedef typename qg_elem<TYPE>::t T;
-  const T* in = static_cast<const T*>(from.data) + row * from.stride + column;
-  if (column + 8 <= columns) {
-    qg_load<TYPE, 8>(in, v);
-  } else {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = column + i < columns ? qg_elem<TYPE>::up(in[i]) : 0.0f;
-  }
-}
-
-__device__ inline void put_codes(const qg_fp8_held& to, int row, int column, const f4* v, float power) {
-  const u2 w = {codes_of(v[0][0], v[0][1], v[0][2], v[0][3], power), codes_of(v[1][0], v[1][1], v[1][2], v[1][3], power)};
-  *reinterpret_cast<u2*>(to.codes + (size_t)row * to.pitch + column) = w;
-}
-
-// h, and in the backward pass dg and du, from g and u.  The accumulators go through LDS, so that one piece of code serves all items in turn
-// (the activations are long); so do the results that become 8-bit floats, until the largest size of their block is known: a block of
-// 128 columns is what the four waves have of a row together.
-constexpr int ITEM_F4 = 6 * 64;  // of an item's place: 24 numbers a lane
+// h as numbers: the accumulators go through LDS, so that one piece of code serves all items in turn
+constexpr int ITEM_F4 = 4 * 64;  // of an item's place: 16 numbers a lane
 template <typename A>
-constexpr int batch_of() { return A::ITEMS == 16 ? 4 : 2; }  // (two workgroups of the smaller tiles share a CU's LDS)
-template <typename A>
-constexpr int gated_lds() { return batch_of<A>() * 4 * ITEM_F4 * 16 + 3 * (batch_of<A>() / (A::ITEMS * A::FRAGMENT / A::ROWS)) * A::FRAGMENT * 4; }
+constexpr int batch_of() { return A::ITEMS < 4 ? A::ITEMS : 4; }
 
-template <typename A, bool BACK>
+template <typename A>
 __device__ inline void finish_gated(const qg_fp8_product_args& p, A& acc, const place& at, int wave, int lane, f4* lds) {
-  constexpr int BATCH = batch_of<A>(), PER_ROW = A::ITEMS * A::FRAGMENT / A::ROWS, ROWS = BATCH / PER_ROW * A::FRAGMENT;
-  const int group = at.column_tile * 4 + wave, padded = at.column_tiles * 128, last_row = p.tokens - 1;
-  f4* const mine = lds + wave * BATCH * ITEM_F4 + lane;
-  unsigned* const tops = reinterpret_cast<unsigned*>(lds + 4 * BATCH * ITEM_F4);  // [3][ROWS]
-  const bool held = BACK || p.out.data == nullptr;
+  constexpr int BATCH = batch_of<A>(), PER_ROW = A::ITEMS * A::FRAGMENT / A::ROWS;
+  const int group = at.column_tile * 4 + wave;
+  const activation act(p.activation);
+  f4* const mine = lds + wave * BATCH * ITEM_F4 + lane;   // (a wave's own)
   each<0, A::ITEMS / BATCH>([&](auto batch) {
     constexpr int b0 = decltype(batch)::value * BATCH;
     const int row0 = at.row_tile * A::ROWS + b0 / PER_ROW * A::FRAGMENT;
-    __syncthreads();
-    for (int e = (int)threadIdx.x; e < 3 * ROWS; e += 256) tops[e] = 0u;
     each<0, BATCH>([&](auto item) {
       constexpr int t = decltype(item)::value;
       acc.template here<b0 + t>();
 #pragma unroll
       for (int j = 0; j < 4; ++j) mine[t * ITEM_F4 + j * 64] = acc.template quad<b0 + t>(j);
     });
-    __syncthreads();
-    float dh[8];
-    auto fetch = [&](int t) {
-      const int row = min(row0 + A::row(t, lane), last_row), column = group * 32 + 8 * A::quarter(t, lane);
-      if (p.dh_type == QG_F32) get<QG_F32>(p.dh, row, column, p.channels, dh);
-      if (p.dh_type == QG_BF16) get<QG_BF16>(p.dh, row, column, p.channels, dh);
-      if (p.dh_type == QG_F16) get<QG_F16>(p.dh, row, column, p.channels, dh);
-    };
-    if (BACK) fetch(0);
 #pragma unroll 1
     for (int t = 0; t < BATCH; ++t) {
-      f4* const place = mine + t * ITEM_F4;
-      const int in_batch = A::row(t, lane), row = row0 + in_batch, column = group * 32 + 8 * A::quarter(t, lane);
-      f4 h[2], dg[2], du[2];
-      (void)dg;
-      (void)du;
-      unsigned top_h = 0u, top_g = 0u, top_u = 0u;
+      const f4* const from = mine + t * ITEM_F4;
+      const int row = row0 + A::row(t, lane), column = group * 32 + 8 * A::quarter(t, lane);
+      float h[8];
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const float gate = place[j / 4 * 2 * 64][j % 4], up = place[(j / 4 * 2 + 1) * 64][j % 4];
-        float slope = 0.0f;
-        const float a = activate<BACK>(p.activation, gate, &slope);
-        h[j / 4][j % 4] = a * up;
-        top_h = umax(top_h, size_bits(a * up));
-        if (BACK) {
-          dg[j / 4][j % 4] = dh[j] * up * slope;
-          du[j / 4][j % 4] = dh[j] * a;
-          top_g = umax(top_g, size_bits(dh[j] * up * slope));
-          top_u = umax(top_u, size_bits(dh[j] * a));
-        }
+      for (int j = 0; j < 8; ++j) h[j] = act.template operator()<false>(from[j / 4 * 2 * 64][j % 4], nullptr) * from[(j / 4 * 2 + 1) * 64][j % 4];
+      if (row < p.tokens && column < p.channels) put<8>(p.out_type, p.out, row, column, p.channels, h);
+    }
+  });
+}
+
+__device__ inline void put_codes(const qg_fp8_held& to, int row, int column, const float* v, float power) {
+  const u2 w = {codes_of(v[0], v[1], v[2], v[3], power), codes_of(v[4], v[5], v[6], v[7], power)};
+  *reinterpret_cast<u2*>(to.codes + (size_t)row * to.pitch + column) = w;
+}
+__device__ inline unsigned top_of(const float* v) {
+  unsigned top = 0u;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) top = umax(top, size_bits(v[i]));
+  return top;
+}
+
+// A lane's eight of dh, on their way.  Behind the last column: zeros.  (A chunk that the last column cuts is requested where it ends there, and
+// moved: by the same number of columns for everybody.  There are at least 8 columns.)
+struct dh_line {
+  u4 low, high;
+  __device__ inline void load(const qg_fp8_product_args& p, int row, int column) {
+    const long long from = row * p.dh.stride + min(column, p.channels - 8);
+    typedef u4 any __attribute__((aligned(2)));
+    if (p.dh_type == QG_F32) {
+      const any* at = reinterpret_cast<const any*>(static_cast<const float*>(p.dh.data) + from);
+      low = at[0];
+      high = at[1];
+    } else {
+      low = *reinterpret_cast<const any*>(static_cast<const _Float16*>(p.dh.data) + from);
+    }
+  }
+  __device__ inline void numbers(const qg_fp8_product_args& p, int column, bool cut, float* v) const {
+    if (p.dh_type == QG_F32) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const unsigned bits = i < 4 ? low[i & 3] : high[i & 3];
+        v[i] = __builtin_bit_cast(float, bits);
       }
-      if (BACK && t + 1 < BATCH) fetch(t + 1);
-      if (!held) {
-        if (row <= last_row && column < p.channels) put<8>(p.out_type, p.out, row, column, p.channels, reinterpret_cast<const float*>(h));
-        continue;
-      }
-      place[0] = h[0];
-      place[64] = h[1];
-      atomicMax(tops + in_batch, top_h);
-      if (BACK) {
-        place[2 * 64] = dg[0];
-        place[3 * 64] = dg[1];
-        place[4 * 64] = du[0];
-        place[5 * 64] = du[1];
-        atomicMax(tops + ROWS + in_batch, top_g);
-        atomicMax(tops + 2 * ROWS + in_batch, top_u);
+    } else if (p.dh_type == QG_BF16) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] = __builtin_bit_cast(float, i & 1 ? low[i / 2] & 0xffff0000u : low[i / 2] << 16);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const unsigned pair = low[i];
+        const h2 x = __builtin_bit_cast(h2, pair);
+        v[2 * i] = (float)x[0];
+        v[2 * i + 1] = (float)x[1];
       }
     }
-    if (!held) return;
+    if (cut) {
+      const int by = column + 8 - p.channels;  // of a lane that is cut: 1 .. 7
+#pragma unroll
+      for (int bit = 4; bit > 0; bit >>= 1) {
+        const bool move = by > 0 && by < 8 && (by & bit);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = move ? (i + bit < 8 ? v[i + bit] : 0.0f) : v[i];
+      }
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] = by >= 8 ? 0.0f : v[i];
+    }
+  }
+};
+
+// h in 8 bits, and in the backward pass dg and du: a block of 128 columns is what the four waves have of a row together, so its largest size
+// meets in LDS while the numbers stay in registers, a batch of items at a time.
+template <typename A, bool BACK>
+__device__ inline void finish_held(const qg_fp8_product_args& p, A& acc, const place& at, int wave, int lane, unsigned* tops) {  // [3][A::ROWS]
+  constexpr int BATCH = BACK ? (A::ITEMS < 4 ? A::ITEMS : 4) : A::ITEMS < 8 ? A::ITEMS : 8;
+  const int group = at.column_tile * 4 + wave, padded = at.column_tiles * 128, last_row = p.tokens - 1, row0 = at.row_tile * A::ROWS;
+  const activation act(p.activation);
+  const bool cut = BACK && (at.column_tile + 1) * 128 > p.channels;
+  for (int e = (int)threadIdx.x; e < (BACK ? 3 : 1) * A::ROWS; e += 256) tops[e] = 0u;
+  dh_line dh[BATCH];
+  if constexpr (BACK) {
+    each<0, BATCH>([&](auto item) {
+      constexpr int t = decltype(item)::value;
+      dh[t].load(p, min(row0 + A::row(t, lane), last_row), group * 32 + 8 * A::quarter(t, lane));
+    });
+  }
+  __syncthreads();
+  each<0, A::ITEMS / BATCH>([&](auto batch) {
+    constexpr int b0 = decltype(batch)::value * BATCH;
+    float h[BATCH][8], dg[BACK ? BATCH : 1][8], du[BACK ? BATCH : 1][8];
+    (void)dg;
+    (void)du;
+    auto compute = [&](auto by_erf) {
+      constexpr bool ERF = decltype(by_erf)::value;
+      each<0, BATCH>([&](auto item) {
+        constexpr int t = decltype(item)::value;
+        const int in_tile = A::row(b0 + t, lane);
+        float d[8];
+        if constexpr (BACK) dh[t].numbers(p, group * 32 + 8 * A::quarter(b0 + t, lane), cut, d);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const float gate = acc.template quad<b0 + t>(j / 4 * 2)[j % 4], up = acc.template quad<b0 + t>(j / 4 * 2 + 1)[j % 4];
+          float slope = 0.0f;
+          const float a = ERF ? act.by_erf<BACK>(gate, &slope) : act.by_logistic<BACK>(gate, &slope);
+          h[t][j] = a * up;
+          if constexpr (BACK) {
+            dg[t][j] = d[j] * up * slope;
+            du[t][j] = d[j] * a;
+          }
+        }
+        atomicMax(tops + in_tile, top_of(h[t]));
+        if constexpr (BACK) {
+          atomicMax(tops + A::ROWS + in_tile, top_of(dg[t]));
+          atomicMax(tops + 2 * A::ROWS + in_tile, top_of(du[t]));
+        }
+      });
+    };
+    each<0, BATCH>([&](auto item) { acc.template here<b0 + decltype(item)::value>(); });
+    if (act.erf) {
+      compute(std::true_type());
+    } else {
+      compute(std::false_type());
+    }
+    if constexpr (BACK && b0 + BATCH < A::ITEMS) {  // the next batch's
+      each<0, BATCH>([&](auto item) {
+        constexpr int t = b0 + BATCH + decltype(item)::value;
+        dh[t - b0 - BATCH].load(p, min(row0 + A::row(t, lane), last_row), group * 32 + 8 * A::quarter(t, lane));
+      });
+    }
     __syncthreads();
-#pragma unroll 1
-    for (int t = 0; t < BATCH; ++t) {
-      const f4* const place = mine + t * ITEM_F4;
-      const int in_batch = A::row(t, lane), row = row0 + in_batch, quarter = A::quarter(t, lane), column = group * 32 + 8 * quarter;
-      if (row > last_row) continue;
-      const f4 h[2] = {place[0], place[64]};
-      const unsigned byte = scale_byte(tops[in_batch]);
-      put_codes(p.out8, row, column, h, scale_of(byte));
+    each<0, BATCH>([&](auto item) {
+      constexpr int t = decltype(item)::value;
+      const int in_tile = A::row(b0 + t, lane), row = row0 + in_tile, quarter = A::quarter(b0 + t, lane), column = group * 32 + 8 * quarter;
+      if (row > last_row) return;
       const bool first = wave == 0 && quarter == 0;
+      const unsigned byte = scale_byte(tops[in_tile]);
+      put_codes(p.out8, row, column, h[t], scale_of(byte));
       if (first) p.out8.scales[(size_t)row * p.out8.scale_pitch + at.column_tile] = (uint8_t)byte;
-      if (BACK) {
-        const f4 dg[2] = {place[2 * 64], place[3 * 64]}, du[2] = {place[4 * 64], place[5 * 64]};
-        const unsigned byte_g = scale_byte(tops[ROWS + in_batch]), byte_u = scale_byte(tops[2 * ROWS + in_batch]);
-        put_codes(p.dgu8, row, column, dg, scale_of(byte_g));
-        put_codes(p.dgu8, row, padded + column, du, scale_of(byte_u));
+      if constexpr (BACK) {
+        const unsigned byte_g = scale_byte(tops[A::ROWS + in_tile]), byte_u = scale_byte(tops[2 * A::ROWS + in_tile]);
+        put_codes(p.dgu8, row, column, dg[t], scale_of(byte_g));
+        put_codes(p.dgu8, row, padded + column, du[t], scale_of(byte_u));
         if (first) {
-          uint8_t* scales = p.dgu8.scales + (size_t)row * p.dgu8.scale_pitch;
-          scales[at.column_tile] = (uint8_t)byte_g;
-          scales[at.column_tiles + at.column_tile] = (uint8_t)byte_u;
+          uint8_t* scales = p.dgu8.scales + (size_t)row * p.dgu8.scale_pitch + at.column_tile;
+          scales[0] = (uint8_t)byte_g;
+          scales[at.column_tiles] = (uint8_t)byte_u;
         }
         __bf16* to = p.dgu + (size_t)row * 2 * padded + column;
-        qg_store<QG_BF16, 8>(to, reinterpret_cast<const float*>(dg));
-        qg_store<QG_BF16, 8>(to + padded, reinterpret_cast<const float*>(du));
+        qg_store<QG_BF16, 8>(to, dg[t]);
+        qg_store<QG_BF16, 8>(to + padded, du[t]);
       }
-    }
+    });
   });
 }
 
@@ -268,13 +322,16 @@ __device__ inline void finish(const qg_fp8_product_args& p, A& acc, const place&
   __syncthreads();
   if constexpr (END == QG_FP8_PLAIN) {
     finish_plain<A>(p, acc, at, wave, lane, reinterpret_cast<float*>(lds));
+  } else if constexpr (END == QG_FP8_GATED) {
+    finish_gated<A>(p, acc, at, wave, lane, reinterpret_cast<f4*>(lds));
   } else {
-    finish_gated<A, END == QG_FP8_GATED_BACK>(p, acc, at, wave, lane, reinterpret_cast<f4*>(lds));
+    finish_held<A, END == QG_FP8_GATED_BACK>(p, acc, at, wave, lane, reinterpret_cast<unsigned*>(lds));
   }
 }
 template <typename A, int END>
 constexpr int lds_bytes() {
-  constexpr int loop = STAGES * A::ROWS * 128 + 2 * A::ROWS * 4, end = END == QG_FP8_PLAIN ? A::ROWS * 64 : gated_lds<A>();
+  constexpr int loop = STAGES * A::ROWS * 128 + 2 * A::ROWS * 4;
+  constexpr int end = END == QG_FP8_PLAIN ? A::ROWS * 64 : END == QG_FP8_GATED ? batch_of<A>() * 4 * ITEM_F4 * 16 : 3 * A::ROWS * 4;
   return loop > end ? loop : end;
 }
 
@@ -656,6 +713,7 @@ hipError_t launch(const qg_fp8_product_args& a, int row_fragments, hipStream_t s
 
 hipError_t qg_launch_fp8_tile(const qg_fp8_product_args& a, int end, int row_fragments, int wide_sums, hipStream_t s) {
   if (end == QG_FP8_GATED_BACK) return launch<QG_FP8_GATED_BACK, false>(a, row_fragments, s);
+  if (end == QG_FP8_GATED && a.out.data == nullptr) return wide_sums ? launch<QG_FP8_GATED_HELD, true>(a, row_fragments, s) : launch<QG_FP8_GATED_HELD, false>(a, row_fragments, s);
   if (wide_sums) return end == QG_FP8_PLAIN ? launch<QG_FP8_PLAIN, true>(a, row_fragments, s) : launch<QG_FP8_GATED, true>(a, row_fragments, s);
   return end == QG_FP8_PLAIN ? launch<QG_FP8_PLAIN, false>(a, row_fragments, s) : launch<QG_FP8_GATED, false>(a, row_fragments, s);
 }

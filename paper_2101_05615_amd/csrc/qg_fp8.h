@@ -94,7 +94,7 @@ struct qg_fp8_pack_args {
 hipError_t qg_launch_fp8_quantize(const qg_fp8_rows& x, int type, int tokens, int channels, const qg_fp8_held& to, hipStream_t s);
 hipError_t qg_launch_fp8_dequantize(const qg_fp8_held& x, int type, int tokens, int channels, const qg_fp8_rows& to, hipStream_t s);
 hipError_t qg_launch_fp8_pack(const qg_fp8_pack_args& a, int type, hipStream_t s);
-enum qg_fp8_end { QG_FP8_PLAIN, QG_FP8_GATED, QG_FP8_GATED_BACK };
+enum qg_fp8_end { QG_FP8_PLAIN, QG_FP8_GATED, QG_FP8_GATED_HELD, QG_FP8_GATED_BACK };
 hipError_t qg_launch_fp8_tile(const qg_fp8_product_args& a, int end, int row_fragments, int wide_sums, hipStream_t s);
 struct qg_fp8_stream_form {
   int rows, fragments, waves;  // row and weight fragments of a workgroup, and the waves that share its K
@@ -198,33 +198,48 @@ __device__ inline i8v both(u4 low, u4 high) {
   return x;
 }
 
-// ---- activations: value and slope, in fp32
-constexpr float SQRT_HALF = 0.70710678118654752f, INV_SQRT_2PI = 0.39894228040143268f, TANH_R = 0.79788456080286536f, TANH_C = 0.044715f;
+// ---- activations: value and slope, in fp32.  All are g p(z) with p between 0 and 1.
+//   p = 1 / (1 + exp(-z)), z = g (linear + cubic g^2): silu with (1, 0); the tanh form of gelu, (1 + tanh y) / 2 = 1 / (1 + exp(-2 y)), with
+//   twice sqrt(2 / pi) (1, 0.044715); relu with the largest number there is, p being 0 or 1 from 1e-36 on
+//   gelu: p = erfc(-g / sqrt 2) / 2
+// slope = p + g p'.  exp(-z) may be infinite: p is 0 then.
+struct activation {
+  bool erf;
+  float linear, cubic;
+  __device__ inline explicit activation(int kind) : erf(kind == QG_GELU) {
+    linear = kind == QG_RELU ? 3.4028234e38f : kind == QG_GELU_TANH ? 1.5957691216057308f : 1.0f;
+    cubic = kind == QG_GELU_TANH ? 1.5957691216057308f * 0.044715f : 0.0f;
+  }
+  template <bool SLOPE>
+  __device__ inline float operator()(float g, float* slope) const { return erf ? by_erf<SLOPE>(g, slope) : by_logistic<SLOPE>(g, slope); }
 
-// 1 / (1 + exp(-z)): of z far below zero exp(-z) is infinite and the result 0
-__device__ inline float logistic(float z) { return 1.0f / (1.0f + __expf(-z)); }
-
-template <bool SLOPE>
-__device__ inline float activate(int kind, float g, float* slope) {
-  if (kind == QG_SILU) {
-    const float p = logistic(g);
-    if (SLOPE) *slope = p * (1.0f + g * (1.0f - p));
+  template <bool SLOPE>
+  __device__ inline float by_logistic(float g, float* slope) const {
+    const float square = fminf(g * g, 1e8f);  // (far out p no longer changes, and an infinity would meet a 0)
+    const float p = __builtin_amdgcn_rcpf(1.0f + __expf(-g * (linear + cubic * square)));
+    const float a = g * p;
+    if (SLOPE) *slope = p + a * (1.0f - p) * (linear + 3.0f * cubic * square);
+    return a;
+  }
+  // erfc x = t exp(-x^2 + polynomial in t), t = 1 / (1 + x / 2), x >= 0: the Chebyshev fit of Press et al., Numerical Recipes (erfcc), 1.2e-7 off
+  template <bool SLOPE>
+  __device__ inline float by_erf(float g, float* slope) const {
+    const float x = __builtin_fabsf(g) * 0.70710678118654752f, t = __builtin_amdgcn_rcpf(1.0f + 0.5f * x), square = x * x;
+    float y = 0.17087277f;
+    y = -0.82215223f + t * y;
+    y = 1.48851587f + t * y;
+    y = -1.13520398f + t * y;
+    y = 0.27886807f + t * y;
+    y = -0.18628806f + t * y;
+    y = 0.09678418f + t * y;
+    y = 0.37409196f + t * y;
+    y = 1.00002368f + t * y;
+    y = -1.26551223f + t * y;
+    const float tail = 0.5f * t * __expf(y - square), p = g > 0.0f ? 1.0f - tail : tail;
+    if (SLOPE) *slope = p + g * __expf(-square) * 0.39894228040143268f;
     return g * p;
   }
-  if (kind == QG_GELU) {
-    const float p = 0.5f * erfcf(-g * SQRT_HALF);
-    if (SLOPE) *slope = p + g * __expf(-0.5f * g * g) * INV_SQRT_2PI;
-    return g * p;
-  }
-  if (kind == QG_GELU_TANH) {  // (1 + tanh z) / 2 = 1 / (1 + exp(-2 z))
-    const float p = logistic(2.0f * TANH_R * (g + TANH_C * g * g * g));
-    // (far out p (1 - p) is 0, and the square must not be infinite beside it)
-    if (SLOPE) *slope = p + 2.0f * g * p * (1.0f - p) * TANH_R * (1.0f + 3.0f * TANH_C * fminf(g * g, 1e8f));
-    return g * p;
-  }
-  if (SLOPE) *slope = g > 0.0f ? 1.0f : g <= 0.0f ? 0.0f : g;  // (of a NaN: NaN)
-  return g > 0.0f ? g : g <= 0.0f ? 0.0f : g;
-}
+};
 
 template <int FIRST, int LAST, typename F>
 __device__ inline void each(F&& f) {  // f(0), f(1) ... with constants
