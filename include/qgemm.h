@@ -731,9 +731,10 @@ int qg_fp8_gated_backward(const qg_fp8_weight* w, const qg_fp8_product* p, const
 
 /* The gradient of the weights of x B: out [k][n] = x^T dy, from x in 8 bits and dy
  * [tokens][n] of type dy_dtype: sums of exact products in fp32, every bit of dy used.
- * No tokens: zeros. */
-int qg_fp8_weight_gradient(const qg_fp8_blocks* x, const qg_rows* dy, int dy_dtype, int n, const qg_rows* out, int dtype,
-                           void* workspace, size_t workspace_bytes, void* stream);
+ * No tokens: zeros.  dy2 and out2 (both or NULL): a second pair of the same sizes and
+ * types in the same launch, as of the two matrices of a gated block. */
+int qg_fp8_weight_gradient(const qg_fp8_blocks* x, const qg_rows* dy, const qg_rows* dy2, int dy_dtype, int n, const qg_rows* out,
+                           const qg_rows* out2, int dtype, void* workspace, size_t workspace_bytes, void* stream);
 
 const char* qg_status_string(int code);
 

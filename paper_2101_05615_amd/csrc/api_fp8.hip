@@ -134,8 +134,8 @@ int check_product(const qg_fp8_weight* w, const qg_fp8_product* p, qg_fp8_produc
   } else {
     if (!p->x_rows.data) return QG_ENULL;
     if (!known(p->x_dtype)) return QG_EINVAL;
-    if (p->tokens > QG_FP8_FEW || w->k % 16 != 0) return QG_EUNSUPPORTED;
     if ((rc = check_rows(p->x_rows, p->x_dtype, &a->x)) != QG_OK) return rc;
+    if (p->tokens > QG_FP8_FEW || w->k % 16 != 0) return QG_EUNSUPPORTED;
     a->x_type = p->x_dtype;
   }
   return check_workspace(p->workspace, p->workspace_bytes);
@@ -274,9 +274,9 @@ int qg_fp8_gated_backward(const qg_fp8_weight* w, const qg_fp8_product* p, const
   return product(a, QG_FP8_GATED_BACK, 0, p->workspace, static_cast<hipStream_t>(stream));
 }
 
-int qg_fp8_weight_gradient(const qg_fp8_blocks* x, const qg_rows* dy, int dy_dtype, int n, const qg_rows* out, int dtype,
-                           void* workspace, size_t workspace_bytes, void* stream) {
-  if (!x || !dy || !out) return QG_ENULL;
+int qg_fp8_weight_gradient(const qg_fp8_blocks* x, const qg_rows* dy, const qg_rows* dy2, int dy_dtype, int n, const qg_rows* out,
+                           const qg_rows* out2, int dtype, void* workspace, size_t workspace_bytes, void* stream) {
+  if (!x || !dy || !out || !dy2 != !out2) return QG_ENULL;
   if (!known(dy_dtype) || !known(dtype) || !extents_ok(1, n)) return QG_EINVAL;
   qg_fp8_gradient_args a = {};
   int rc = check_blocks(x, x->tokens, x->channels, &a.x8);
@@ -284,19 +284,20 @@ int qg_fp8_weight_gradient(const qg_fp8_blocks* x, const qg_rows* dy, int dy_dty
   if ((rc = check_workspace(workspace, workspace_bytes)) != QG_OK) return rc;
   if (x->tokens && (rc = check_rows(*dy, dy_dtype, &a.dy)) != QG_OK) return rc;
   if ((rc = check_rows(*out, dtype, &a.out)) != QG_OK) return rc;
+  if (x->tokens && dy2 && (rc = check_rows(*dy2, dy_dtype, &a.dy2)) != QG_OK) return rc;
+  if (out2 && (rc = check_rows(*out2, dtype, &a.out2)) != QG_OK) return rc;
   a.dy_type = dy_dtype;
   a.out_type = dtype;
   a.tokens = x->tokens;
   a.k = x->channels;
   a.n = n;
-  const int tile = (long long)((a.k + 255) / 256) * ((n + 255) / 256) >= 200 ? 256 : 128;
-  const long long tiles = (long long)((a.k + tile - 1) / tile) * ((a.n + tile - 1) / tile);
+  auto tiles_of = [&](long long tile) { return (a.k + tile - 1) / tile * ((n + tile - 1) / tile) * (out2 ? 2 : 1); };
+  const int tile = tiles_of(256) >= 200 ? 256 : 128;
+  const long long tiles = tiles_of(tile);
   a.slices = 1;
-  a.slice_tokens = qg_fp8_up(a.tokens, 64);
-  if (workspace && tile == 128 && tiles <= COUNTERS) {
-    long long slices = 512 / tiles;
-    if (slices > a.tokens / 256) slices = a.tokens / 256;
-    if (slices > PARTIALS / (tiles * tile * tile)) slices = PARTIALS / (tiles * tile * tile);
+  a.slice_tokens = a.tokens;
+  if (workspace && tile == 128 && tiles <= COUNTERS) {  // tokens over workgroups, 256 each at least
+    const long long slices = at_most(at_most(512 / tiles, a.tokens / 256), PARTIALS / (tiles * tile * tile));
     if (slices > 1) {
       a.slice_tokens = qg_fp8_up((a.tokens + (int)slices - 1) / (int)slices, 64);
       a.slices = (a.tokens + a.slice_tokens - 1) / a.slice_tokens;

@@ -84,15 +84,11 @@ struct dy_line {
   }
 };
 
-template <int TILE>
+// In place and in this order: the compiler moves 256 accumulators about, and gathers the products of several stages behind each other.  It does not
+// know how long the result takes, which whoever reads it waits for, nor that operands are to be two cycles old if they were computed (free
+// in the shadow of the product before).
 __device__ inline void add_product(f16v& c, b8 a, b8 b) {
-  if constexpr (TILE == 256) {
-    // in place: with all 256 accumulator registers in use the compiler moves them about.  It does not know how long the result takes, which
-    // whoever reads it waits for, nor that operands are to be two cycles old if they were computed (free in the shadow of the product before).
-    asm volatile("s_nop 1\n\tv_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+a"(c) : "v"(a), "v"(b));
-  } else {
-    c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
-  }
+  asm volatile("s_nop 1\n\tv_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+a"(c) : "v"(a), "v"(b));
 }
 
 // TS tokens of a stage; CW columns a thread: 256 threads cover TILE columns x TS tokens in blocks of CW x 8.  A wave has TILE / 2 squared of
@@ -114,7 +110,9 @@ __global__ __launch_bounds__(256, TILE == 256 || PARTS > 1 ? 1 : 2) void qg_fp8_
   if (at >= tiles) return;
   const int panel = at / (8 * column_tiles), in_panel = at - panel * 8 * column_tiles;
   const int panel_rows = min(8, row_tiles - panel * 8);
-  const int row_tile = panel * 8 + in_panel % panel_rows, column_tile = in_panel / panel_rows;
+  const int row_tile = panel * 8 + in_panel % panel_rows, all_columns = in_panel / panel_rows;
+  const int second = 2 * all_columns >= column_tiles && p.out2.data != nullptr, column_tile = second ? all_columns - column_tiles / 2 : all_columns;
+  const qg_fp8_rows &dy = second ? p.dy2 : p.dy, &out = second ? p.out2 : p.out;
   const int t0 = slice * p.slice_tokens, t1 = min(t0 + p.slice_tokens, p.tokens);
 
   // what this thread fetches: columns c0 .. of both operands, tokens 8 * tb .. of a stage
@@ -128,34 +126,37 @@ __global__ __launch_bounds__(256, TILE == 256 || PARTS > 1 ? 1 : 2) void qg_fp8_
   // addresses: what all threads share, which moves on token by token, and this thread's part
   const unsigned x_mine = (unsigned)(8 * tb) * (unsigned)p.x8.pitch + (unsigned)xc;
   const unsigned s_mine = (unsigned)(8 * tb) * (unsigned)p.x8.scale_pitch + (unsigned)(xc / QG_FP8_BLOCK);
-  const T* const y_base = static_cast<const T*>(p.dy.data) + (long long)(t0 + 8 * tb) * p.dy.stride + yc;
-  unsigned xraw[8][CW / 4], xs[8];
-  dy_line<TYPE, PARTS, CW> y[8];
-  auto fetch_x = [&](const uint8_t* src, const uint8_t* scale, int i) {
+  const T* const y_base = static_cast<const T*>(dy.data) + (long long)(t0 + 8 * tb) * dy.stride + yc;
+  struct tokens {  // this thread's part of a stage, on its way
+    unsigned x[8][CW / 4], scale[8];
+    dy_line<TYPE, PARTS, CW> y[8];
+  };
+  tokens even, odd;
+  auto fetch_x = [&](tokens& to, const uint8_t* src, const uint8_t* scale, int i) {
     if constexpr (CW == 8) {
       const u2 v = from_memory<u2>(src);
-      xraw[i][0] = v[0];
-      xraw[i][1] = v[1];
+      to.x[i][0] = v[0];
+      to.x[i][1] = v[1];
     } else {
-      xraw[i][0] = from_memory<unsigned>(src);
+      to.x[i][0] = from_memory<unsigned>(src);
     }
-    xs[i] = from_memory<uint8_t>(scale);
+    to.scale[i] = from_memory<uint8_t>(scale);
   };
-  auto fetch = [&](int from, int i, bool inside) {  // token i of this thread's eight
+  auto fetch = [&](tokens& to, int from, int i, bool inside) {  // token i of this thread's eight
     const uint8_t* const src = p.x8.codes + (long long)(from + i) * p.x8.pitch + x_mine;
     const uint8_t* const scale = p.x8.scales + (long long)(from + i) * p.x8.scale_pitch + s_mine;
-    const T* dy = y_base + (long long)(from - t0 + i) * p.dy.stride;
-    if (inside && !narrow) {
-      fetch_x(src, scale, i);
-      y[i].load(dy);
+    const T* line = y_base + (long long)(from - t0 + i) * dy.stride;
+    if (inside) {
+      fetch_x(to, src, scale, i);
+      to.y[i].load(line);
     } else {
       const bool there = from + 8 * tb + i < t1;   // (a token behind the last: zeros)
-      fetch_x(there ? src : no_numbers, there ? scale : no_numbers, i);
-      dy = there ? dy : reinterpret_cast<const T*>(no_numbers);
+      fetch_x(to, there ? src : no_numbers, there ? scale : no_numbers, i);
+      line = there ? line : reinterpret_cast<const T*>(no_numbers);
       if (narrow) {
-        y[i].load_some(dy, p.n - 1);
+        to.y[i].load_some(line, p.n - 1);
       } else {
-        y[i].load(dy);
+        to.y[i].load(line);
       }
     }
   };
@@ -174,15 +175,15 @@ __global__ __launch_bounds__(256, TILE == 256 || PARTS > 1 ? 1 : 2) void qg_fp8_
     *reinterpret_cast<u4*>(plane + to) = (u4){a0, a1, a2, a3};
   };
   constexpr int SLICES = 6 + 2 * PARTS;
-  auto store = [&](uint8_t* stage, int pair, int slice) {
+  auto store = [&](const tokens& of, uint8_t* stage, int pair, int slice) {
     if (slice < 2 || slice == 4 || slice == 5) {
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const int k = slice % 2 * 4 + i;
         if (slice < 2) {
-          line[k] = widened(xraw[k][pair / 2], scale_of(xs[k]), pair & 1);
+          line[k] = widened(of.x[k][pair / 2], scale_of(of.scale[k]), pair & 1);
         } else {
-          y[k].split(pair, part[k]);
+          of.y[k].split(pair, part[k]);
         }
       }
     } else if (slice == 2) {
@@ -214,72 +215,103 @@ __global__ __launch_bounds__(256, TILE == 256 || PARTS > 1 ? 1 : 2) void qg_fp8_
     return *reinterpret_cast<const b8*>(plane + (f * STEPS + step) * 1024 + (operand_at ^ (unsigned)((2 * f & 7) * 16)));
   };
   if (t0 < t1) {
+    // An even number of stages: behind the last token come zeros.  A stage is requested two and a half stages before it is multiplied, and in
+    // registers for one and a half of them; the operands of a stage's first products are read behind a barrier in the stage before, where
+    // all of it has long been in LDS and nobody waits.
+    constexpr int PRODUCTS = GROUPS * PARTS * F, PIECES = PAIRS * SLICES;
+    constexpr int MOVE = PARTS == 1 ? PRODUCTS * 3 / 8 : PRODUCTS / 2, REQUEST = PRODUCTS / 8 < 8 ? PRODUCTS / 4 : 8;
+    b8 x[2][F], g[3][PARTS];
+    auto read_x = [&](const uint8_t* stage, int s, int i) { x[s & 1][i] = operand(stage, wr * F + i, s); };
+    auto read_g = [&](const uint8_t* stage, int to, int group) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) fetch(t0, i, t0 + TS <= t1);
+      for (int q = 0; q < PARTS; ++q) g[to][q] = operand(stage + (1 + q) * PLANE, wc * F + group % F, group / F);
+    };
+    auto fetch_all = [&](tokens& to, int from) {
 #pragma unroll
-    for (int u = 0; u < PAIRS; ++u)
-#pragma unroll
-      for (int e = 0; e < SLICES; ++e) store(lds, u, e);
-    if (t0 + TS < t1) {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) fetch(t0 + TS, i, t0 + 2 * TS <= t1);
-    }
-    int now = 0;
-#pragma unroll 1
-    for (int from = t0; from < t1; from += TS, now ^= 1) {
-      // (past the end: the last stage's numbers again, into the half that nobody reads any more)
-      const int ahead = min(from + 2 * TS, t0 + (t1 - 1 - t0) / TS * TS);
-      const bool inside = !narrow && ahead + TS <= t1;
-      __syncthreads();
+      for (int i = 0; i < 8; ++i) fetch(to, from, i, !narrow && from + TS <= t1);
+    };
+    auto multiply = [&](auto which, tokens& next, int from) {
+      constexpr int now = decltype(which)::value, RING0 = now * GROUPS % 3;
       const uint8_t* const stage = lds + now * STAGE;
-      uint8_t* const other = lds + (now ^ 1) * STAGE;
-      b8 x[2][F], g[2][PARTS];
-#pragma unroll
-      for (int i = 0; i < F; ++i) x[0][i] = operand(stage, wr * F + i, 0);
-#pragma unroll
-      for (int q = 0; q < PARTS; ++q) g[0][q] = operand(stage + (1 + q) * PLANE, wc * F, 0);
-      // The matrix instructions of a stage, one by one: first with pieces of the next stage's way to LDS, then with the requests of the stage
-      // behind it, which have the rest of this stage to arrive
-      constexpr int PRODUCTS = GROUPS * PARTS * F, PIECES = PAIRS * SLICES;
-      constexpr int MOVE = PARTS == 1 ? PRODUCTS * 3 / 8 : PRODUCTS / 2, REQUEST = PRODUCTS / 8 < 8 ? PRODUCTS / 4 : 8;
+      uint8_t* const other = lds + (1 - now) * STAGE;
+      const int ahead = from + 3 * TS;
+      const bool inside = !narrow && ahead + TS <= t1;
+      // The matrix instructions, one by one: first with pieces of the next stage's way to LDS, then with the requests that take its registers
       each<0, PRODUCTS>([&](auto number) {
         constexpr int n = decltype(number)::value, group = n / (PARTS * F), q = n / F % PARTS, i = n % F, s = group / F, j = group % F;
         if constexpr (n % (PARTS * F) == 0) {
-          if constexpr (group + 1 < GROUPS) {
+          if constexpr (group == GROUPS - 2) {
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+            __builtin_amdgcn_s_barrier();
+            asm volatile("" ::: "memory");
 #pragma unroll
-            for (int k = 0; k < PARTS; ++k) g[(group + 1) & 1][k] = operand(stage + (1 + k) * PLANE, wc * F + (group + 1) % F, (group + 1) / F);
+            for (int k = 0; k < F; ++k) read_x(other, 0, k);
           }
-          if constexpr (s + 1 < STEPS) x[(s + 1) & 1][j] = operand(stage, wr * F + j, s + 1);  // a part of the next step's rows with every group
+          if constexpr (group + 2 < GROUPS) read_g(stage, (RING0 + group + 2) % 3, group + 2);
+          if constexpr (group + 2 >= GROUPS) read_g(other, (RING0 + group + 2) % 3, group + 2 - GROUPS);
+          if constexpr (s + 1 < STEPS && j < 2) {  // the next step's rows
+#pragma unroll
+            for (int k = 0; k < F / 2; ++k) read_x(stage, s + 1, j * (F / 2) + k);
+          }
         }
         if constexpr (n < MOVE) {
-          constexpr int first = n * PIECES / MOVE, last = (n + 1) * PIECES / MOVE;
-          each<first, last>([&](auto piece) {
+          each<n * PIECES / MOVE, (n + 1) * PIECES / MOVE>([&](auto piece) {
             constexpr int e = decltype(piece)::value;
-            store(other, e / SLICES, e % SLICES);
+            store(next, other, e / SLICES, e % SLICES);
           });
         } else if constexpr (n < MOVE + REQUEST) {
           constexpr int first = (n - MOVE) * 8 / REQUEST, last = (n - MOVE + 1) * 8 / REQUEST;
           if (inside) {
-            each<first, last>([&](auto token) { fetch(ahead, decltype(token)::value, true); });
+            each<first, last>([&](auto token) { fetch(next, ahead, decltype(token)::value, true); });
           } else {
-            each<first, last>([&](auto token) { fetch(ahead, decltype(token)::value, false); });
+            each<first, last>([&](auto token) { fetch(next, ahead, decltype(token)::value, false); });
           }
         }
-        add_product<TILE>(c[i][j], g[group & 1][q], x[s & 1][i]);
+        add_product(c[i][j], g[(RING0 + group) % 3][q], x[s & 1][i]);
         __builtin_amdgcn_sched_barrier(0);
       });
+    };
+    static_assert(STEPS % 2 == 0 && F % 2 == 0 && GROUPS / 2 * PARTS * F >= MOVE, "the next stage is in LDS when it is read");
+    fetch_all(even, t0);
+    fetch_all(odd, t0 + TS);
+#pragma unroll
+    for (int u = 0; u < PAIRS; ++u)
+#pragma unroll
+      for (int e = 0; e < SLICES; ++e) store(even, lds, u, e);
+    fetch_all(even, t0 + 2 * TS);
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < F; ++k) read_x(lds, 0, k);
+    read_g(lds, 0, 0);
+    read_g(lds, 1, 1);
+#pragma unroll 1
+    for (int from = t0; from < t1; from += 2 * TS) {
+      multiply(std::integral_constant<int, 0>(), odd, from);
+      multiply(std::integral_constant<int, 1>(), even, from + TS);
+      if constexpr (2 * GROUPS % 3 != 0) {  // the ring starts at 0 again
+        constexpr int at = 2 * GROUPS % 3;
+        b8 t[2][PARTS];
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+#pragma unroll
+          for (int q = 0; q < PARTS; ++q) t[k][q] = g[(at + k) % 3][q];
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+#pragma unroll
+          for (int q = 0; q < PARTS; ++q) g[k][q] = t[k][q];
+      }
     }
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    __syncthreads();   // (nobody reads what the end writes over)
   }
-  if constexpr (TILE == 256) {
-    asm volatile("s_nop 15\n\ts_nop 15" ::: "memory");
+  asm volatile("s_nop 15\n\ts_nop 15" ::: "memory");
 #pragma unroll
-    for (int i = 0; i < F; ++i)
+  for (int i = 0; i < F; ++i)
 #pragma unroll
-      for (int j = 0; j < F; ++j) asm volatile("" : "+a"(c[i][j]));
-  }
+    for (int j = 0; j < F; ++j) asm volatile("" : "+a"(c[i][j]));
   // a lane has, of fragment (i, j), row 32 i + lane % 32 and the columns 32 j + 8 (e / 4) + 4 (lane / 32) + e % 4
   if (TILE == 128 && p.slices > 1) {  // sums of the slices through memory; the last one to arrive adds them in order
-    const int tile = row_tile * column_tiles + column_tile;
+    const int tile = row_tile * column_tiles + all_columns;
     const size_t step = (size_t)TILE * TILE;
     float* const mine = p.partial + (size_t)tile * p.slices * step + (size_t)wave * (F * F * 1024) + lane * 4;
 #pragma unroll
@@ -329,14 +361,14 @@ __global__ __launch_bounds__(256, TILE == 256 || PARTS > 1 ? 1 : 2) void qg_fp8_
       for (int e = 0; e < 4; ++e) {
         const int column = column_tile * TILE + (wc * F + j) * 32 + 8 * e + 4 * (lane >> 5);
         const float v[4] = {c[i][j][4 * e], c[i][j][4 * e + 1], c[i][j][4 * e + 2], c[i][j][4 * e + 3]};
-        if (column < p.n) put<4>(p.out_type, p.out, row, column, p.n, v);
+        if (column < p.n) put<4>(p.out_type, out, row, column, p.n, v);
       }
   }
 }
 
 template <int TILE, int TYPE, int PARTS>
 hipError_t launch(const qg_fp8_gradient_args& a, hipStream_t s) {
-  const int rows = (a.k + TILE - 1) / TILE, columns = (a.n + TILE - 1) / TILE;
+  const int rows = (a.k + TILE - 1) / TILE, columns = (a.n + TILE - 1) / TILE * (a.out2.data ? 2 : 1);
   const unsigned per = (unsigned)(((long long)rows * columns + 7) / 8);
   hipLaunchKernelGGL((qg_fp8_gradient_kernel<TILE, TYPE, PARTS>), dim3(per * 8 * (unsigned)a.slices), dim3(256), 0, s, a, rows, columns);
   return hipGetLastError();

@@ -70,7 +70,7 @@ struct qg_fp8_product_args {
 
 struct qg_fp8_gradient_args {
   qg_fp8_held x8;
-  qg_fp8_rows dy, out;
+  qg_fp8_rows dy, out, dy2, out2;  // out2.data null: one matrix; otherwise both in one launch
   int dy_type, out_type;
   int tokens, k, n;
   int slices, slice_tokens;  // a multiple of 64

@@ -64,7 +64,7 @@ def _declare():
     lib.qg_fp8_matmul.argtypes = [P(_WeightDesc), P(_Product), vp]
     lib.qg_fp8_gated.argtypes = [P(_WeightDesc), P(_Product), P(_BlocksDesc), vp]
     lib.qg_fp8_gated_backward.argtypes = [P(_WeightDesc), P(_Product), P(_Rows), i, vp, P(_BlocksDesc), P(_BlocksDesc), vp]
-    lib.qg_fp8_weight_gradient.argtypes = [P(_BlocksDesc), P(_Rows), i, i, P(_Rows), i, vp, sz, vp]
+    lib.qg_fp8_weight_gradient.argtypes = [P(_BlocksDesc), P(_Rows), P(_Rows), i, i, P(_Rows), P(_Rows), i, vp, sz, vp]
 
 
 _declare()
@@ -283,23 +283,32 @@ def gated_backward(x, w, dh, activation="silu", workspace=None):
 
 def weight_gradient(x, dy, dtype=None, out=None, workspace=None):
     """x^T dy [in, out]: the gradient of the weights of x B from x in 8 bits (Blocks) and the gradient dy [tokens, out] of the product.
-    dtype: of the result, by default dy's."""
-    _no_gradient("weight_gradient", dy, out)
-    assert isinstance(x, Blocks) and x.device == dy.device
-    _check_rows(dy, x.shape[0])
-    dtype = dtype if dtype is not None else out.dtype if out is not None else dy.dtype
-    if out is None:
-        out = torch.empty((x.shape[1], dy.shape[1]), dtype=dtype, device=dy.device)
-    else:
-        _check_rows(out, x.shape[1], dy.shape[1])
-        assert out.dtype == dtype and out.device == dy.device
+    dtype: of the result, by default dy's.  dy may be a pair of tensors: two results, in one kernel."""
+    pair = isinstance(dy, (tuple, list))
+    dys = tuple(dy) if pair else (dy,)
+    outs = (None,) * len(dys) if out is None else tuple(out) if pair else (out,)
+    assert isinstance(x, Blocks) and 1 <= len(dys) <= 2 and len(outs) == len(dys)
+    _no_gradient("weight_gradient", *dys, *outs)
+    dtype = dtype if dtype is not None else outs[0].dtype if outs[0] is not None else dys[0].dtype
+    done = []
+    for d, o in zip(dys, outs):
+        _check_rows(d, x.shape[0], dys[0].shape[1])
+        assert d.dtype == dys[0].dtype and x.device == d.device
+        if o is None:
+            o = torch.empty((x.shape[1], d.shape[1]), dtype=dtype, device=d.device)
+        else:
+            _check_rows(o, x.shape[1], d.shape[1])
+            assert o.dtype == dtype and o.device == d.device
+        done.append(o)
     ws, size = None, 0
     if workspace is not None:
-        assert workspace.is_cuda and workspace.is_contiguous() and workspace.device == dy.device
+        assert workspace.is_cuda and workspace.is_contiguous() and workspace.device == x.device
         ws, size = workspace.data_ptr(), workspace.numel() * workspace.element_size()
-    _check(lib.qg_fp8_weight_gradient(x._ref, ctypes.byref(_rows(dy)), _TYPES[dy.dtype], dy.shape[1], ctypes.byref(_rows(out)), _TYPES[dtype],
+    rows = [ctypes.byref(_rows(t)) for t in (*dys, *done)]
+    second = (rows[1], rows[3]) if pair and len(dys) == 2 else (None, None)
+    _check(lib.qg_fp8_weight_gradient(x._ref, rows[0], second[0], _TYPES[dys[0].dtype], dys[0].shape[1], rows[len(dys)], second[1], _TYPES[dtype],
                                       ws, size, _stream()), "qg_fp8_weight_gradient")
-    return out
+    return tuple(done) if pair else done[0]
 
 
 def feed_forward(x, w_in, w_out, activation="silu", dtype=None, out=None, workspace=None):
@@ -367,8 +376,12 @@ class _GatedMlp(torch.autograd.Function):
         dgu, dgu8, h8 = gated_backward(ctx.x8, ctx.w_in, dh, ctx.activation, workspace=ws)
         del dh
         dx = matmul(dgu8, ctx.w_in.transposed, dtype=ctx.types[0], workspace=ws) if need[0] else None
-        dgate = weight_gradient(ctx.x8, dgu[:, 0, :n], dtype=ctx.types[1], workspace=ws) if need[1] else None
-        dup = weight_gradient(ctx.x8, dgu[:, 1, :n], dtype=ctx.types[1], workspace=ws) if need[2] else None
+        dgate = dup = None
+        if need[1] and need[2]:
+            dgate, dup = weight_gradient(ctx.x8, (dgu[:, 0, :n], dgu[:, 1, :n]), dtype=ctx.types[1], workspace=ws)
+        elif need[1] or need[2]:
+            one = weight_gradient(ctx.x8, dgu[:, 0 if need[1] else 1, :n], dtype=ctx.types[1], workspace=ws)
+            dgate, dup = (one, None) if need[1] else (None, one)
         ddown = weight_gradient(h8, dy, dtype=ctx.types[2], workspace=ws) if need[3] else None
         return dx, dgate, dup, ddown, None, None
 

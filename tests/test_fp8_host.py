@@ -103,6 +103,7 @@ def common_refusals(fp8, call, gated):
     assert call(**raw) == EUNSUPPORTED                                            # more than QG_FP8_FEW tokens
     assert call(**raw, x_dtype=9, tokens=3) == EINVAL
     assert call(x=none, x_rows=fp8._Rows(FAKE + 2, 300), tokens=3) == EALIGN
+    assert call(**raw, tokens=3) == EUNSUPPORTED                                  # 300 channels are no multiple of 16
     assert call(workspace=FAKE, workspace_bytes=fp8.WORKSPACE_BYTES - 1) == EWORKSPACE
     assert call(workspace=FAKE + 4, workspace_bytes=fp8.WORKSPACE_BYTES) == EALIGN
     assert call(tokens=0, x=none, out=fp8._Rows(None, 0)) == 0
@@ -141,18 +142,21 @@ def test_gated_backward_refusals(fp8):
     assert call(both=blocks(fp8, 40, 400)) == EINVAL and call(held=blocks(fp8, 40, 256)) == EINVAL
     raw = dict(x=fp8._BlocksDesc(None, None, 0, 0), x_rows=fp8._Rows(FAKE, 300), tokens=3, both=blocks(fp8, 3, 512), held=blocks(fp8, 3, 200))
     assert call(**raw) == EUNSUPPORTED
+    assert call(w=weight(fp8, 300, 7, 1), held=blocks(fp8, 40, 7), both=blocks(fp8, 40, 256)) == EUNSUPPORTED   # fewer than 8 columns
     wide = (1 << 20) - 100
     assert call(w=weight(fp8, 300, wide, 1)) == EINVAL                            # the pair's gradient would have too many channels
 
 
 def test_weight_gradient_refusals(fp8):
-    def call(x=blocks(fp8), dy=rows(fp8), dy_dtype=0, n=200, out=rows(fp8), dtype=0, ws=None, size=0):
-        return fp8.lib.qg_fp8_weight_gradient(x, dy, dy_dtype, n, out, dtype, ws, size, None)
+    def call(x=blocks(fp8), dy=rows(fp8), dy_dtype=0, n=200, out=rows(fp8), dtype=0, ws=None, size=0, dy2=None, out2=None):
+        return fp8.lib.qg_fp8_weight_gradient(x, dy, dy2, dy_dtype, n, out, out2, dtype, ws, size, None)
 
     assert call(x=None) == ENULL and call(dy=None) == ENULL and call(out=None) == ENULL
     assert call(dy=rows(fp8, None)) == ENULL and call(out=rows(fp8, None)) == ENULL and call(x=blocks(fp8, codes=None)) == ENULL
     assert call(dy_dtype=3) == EINVAL and call(dtype=3) == EINVAL and call(n=0) == EINVAL and call(n=(1 << 20) + 1) == EINVAL
     assert call(dy=rows(fp8, FAKE + 2)) == EALIGN and call(out=rows(fp8, FAKE + 2)) == EALIGN
+    assert call(dy2=rows(fp8)) == ENULL and call(out2=rows(fp8)) == ENULL and call(dy2=rows(fp8, FAKE + 2), out2=rows(fp8)) == EALIGN
+    assert call(dy2=rows(fp8), out2=rows(fp8, None)) == ENULL
     assert call(ws=FAKE, size=100) == EWORKSPACE and call(ws=FAKE + 4, size=fp8.WORKSPACE_BYTES) == EALIGN
 
 

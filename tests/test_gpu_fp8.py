@@ -320,6 +320,24 @@ def test_weight_gradient(env, T, K, N, dtype):
     assert (ws[:fp8.COUNTER_BYTES] == 0).all()
 
 
+@pytest.mark.parametrize("T,K,N", [(70, 200, 130), (2100, 140, 200), (65, 2600, 2700)])
+def test_weight_gradients_of_a_pair(env, T, K, N):
+    """Two in one launch: the same bits as one by one where the tiles are the same, and always within the bound."""
+    fp8, torch, dev = env
+    rng = np.random.default_rng(T)
+    x = tensor(torch, dev, inputs(rng, T, K), "bfloat16")
+    both = torch.from_numpy(inputs(rng, T, 2 * N, 0.01)).to(dev).to(torch.bfloat16)
+    dys, xq, ws = (both[:, :N], both[:, N:]), fp8.quantize(x), fp8.workspace(dev)
+    got = fp8.weight_gradient(xq, dys, dtype=torch.float32, workspace=ws)
+    x8 = ref.held(f64(x))
+    for y, dy in zip(got, dys):
+        want, mass = x8.T @ f64(dy), np.abs(x8).T @ np.abs(f64(dy))
+        bound = mass * ((64 + 32 + T / 16 * 3) * 2.0 ** -23)
+        compare(f64(y), want, bound + ref.rounding(np.abs(want) + bound, "float32"), "pair")
+    if T == 70:
+        assert all(torch.equal(y, fp8.weight_gradient(xq, dy, dtype=torch.float32)) for y, dy in zip(got, dys))
+
+
 def test_weight_gradient_infinite(env):
     """An infinity in dy stays one (the parts of a number are finite but the first)."""
     fp8, torch, dev = env
