@@ -9,6 +9,7 @@
 #include <Python.h>
 
 #include <ATen/core/Tensor.h>
+#include <ATen/core/grad_mode.h>
 #include <ATen/ops/empty.h>
 #include <torch/csrc/autograd/python_variable.h>
 
@@ -22,6 +23,7 @@ namespace {
 PyObject* g_stream_of = nullptr;  // device -> raw handle of its current stream
 PyObject* g_device = nullptr;     // () -> current device
 PyObject* g_name_fast = nullptr;  // "_fast"
+PyObject *g_name_codes = nullptr, *g_name_scales = nullptr, *g_name_shape = nullptr, *g_name_data = nullptr;
 PyObject* g_error = nullptr;      // exception for an error code: (code, name of the call)
 
 // A C++ exception of the tensor library ends here: the slow path meets it again and reports it its own way
@@ -401,6 +403,394 @@ PyObject* kv4_read(PyObject*, PyObject* const* a, Py_ssize_t n) {
     return both;)
 }
 
+// ---- 8-bit floats (fp8.py); as above, anything out of the ordinary gives None.  Tensors are on the current device here, or nowhere.
+bool here(int64_t device, void** s) {
+  PyObject* const current = PyObject_CallNoArgs(g_device);
+  if (!current) return slow();
+  const long index = PyLong_AsLong(current);
+  if (index != device || PyErr_Occurred()) {
+    Py_DECREF(current);
+    return slow();
+  }
+  PyObject* const raw = PyObject_CallOneArg(g_stream_of, current);
+  Py_DECREF(current);
+  if (!raw) return slow();
+  *s = PyLong_AsVoidPtr(raw);
+  Py_DECREF(raw);
+  return !PyErr_Occurred() || slow();
+}
+bool untracked(const at::Tensor& t) { return !(t.requires_grad() && at::GradMode::is_enabled()) && !t._fw_grad(0).defined(); }
+
+// a tensor [tokens][channels] with a unit stride of channels
+bool rows(const at::Tensor* t, qg_rows* out) {
+  if (!t || !t->is_cuda() || t->dim() != 2 || element(t->scalar_type()) < 0 || t->size(0) > INT_MAX || t->size(1) > INT_MAX ||
+      (t->stride(1) != 1 && t->size(1) > 1 && t->size(0) > 0))
+    return false;
+  *out = {t->data_ptr(), t->stride(0)};
+  return true;
+}
+at::ScalarType element_type(int t) { return t == QG_F32 ? at::kFloat : t == QG_BF16 ? at::kBFloat16 : at::kHalf; }
+
+int64_t fp8_pitch(int64_t channels) { return (channels + 127) / 128 * 128; }
+int64_t fp8_scale_pitch(int64_t channels) { return ((channels + 127) / 128 + 3) / 4 * 4; }
+
+struct blocks {  // what C points into belongs to the object, or to the two tensors
+  at::Tensor codes, scales;
+  qg_fp8_blocks c;
+};
+bool attribute(PyObject* o, PyObject* name, at::Tensor* out) {
+  PyObject* const v = PyObject_GetAttr(o, name);
+  if (!v) return slow();
+  const at::Tensor* const t = tensor(v);
+  if (t) *out = *t;
+  Py_DECREF(v);
+  return t != nullptr;
+}
+bool old_blocks(PyObject* o, blocks* out) {
+  if (!attribute(o, g_name_codes, &out->codes) || !attribute(o, g_name_scales, &out->scales)) return false;
+  PyObject* const shape = PyObject_GetAttr(o, g_name_shape);
+  if (!shape) return slow();
+  int tokens = -1, channels = -1;
+  const bool two = PyTuple_CheckExact(shape) && PyTuple_GET_SIZE(shape) == 2 && integer(PyTuple_GET_ITEM(shape, 0), &tokens) &&
+                   integer(PyTuple_GET_ITEM(shape, 1), &channels);
+  Py_DECREF(shape);
+  const at::Tensor &codes = out->codes, &scales = out->scales;
+  if (!two || codes.scalar_type() != at::kByte || scales.scalar_type() != at::kByte || !codes.is_cuda() || !scales.is_cuda() ||
+      codes.get_device() != scales.get_device() || codes.dim() != 2 || scales.dim() != 2 || !codes.is_contiguous() || !scales.is_contiguous() ||
+      codes.size(0) != tokens || scales.size(0) != tokens || codes.size(1) != fp8_pitch(channels) || scales.size(1) != fp8_scale_pitch(channels))
+    return false;
+  out->c = {codes.data_ptr(), scales.data_ptr(), tokens, channels};
+  return true;
+}
+bool new_blocks(const at::TensorOptions& like, int64_t tokens, int64_t channels, blocks* out) {
+  if (channels < 1 || channels > QG_FP8_MAX_CHANNELS || tokens < 0 || tokens > 1 << 28) return false;
+  const auto bytes = like.dtype(at::kByte);
+  out->codes = at::empty({tokens, fp8_pitch(channels)}, bytes);
+  out->scales = at::empty({tokens, fp8_scale_pitch(channels)}, bytes);
+  out->c = {out->codes.data_ptr(), out->scales.data_ptr(), (int)tokens, (int)channels};
+  return true;
+}
+// activations of a product: a tensor, which is put into 8 bits here unless the product does it, or blocks
+struct activations {
+  blocks held;
+  int64_t device;
+  at::TensorOptions options;
+  int64_t tokens, channels;
+  int type;  // -1: blocks
+  qg_rows raw;
+};
+bool of_activations(PyObject* o, activations* out) {
+  const at::Tensor* const t = tensor(o);
+  if (t) {
+    if (!rows(t, &out->raw) || !untracked(*t)) return false;
+    out->type = element(t->scalar_type());
+    out->options = t->options();
+    out->tokens = t->size(0);
+    out->channels = t->size(1);
+    out->device = t->get_device();
+    return true;
+  }
+  if (!old_blocks(o, &out->held)) return false;
+  out->type = -1;
+  out->options = out->held.codes.options();
+  out->tokens = out->held.c.tokens;
+  out->channels = out->held.c.channels;
+  out->device = out->held.codes.get_device();
+  return true;
+}
+int into_blocks(activations* x, void* s) {  // (the tensors live until the calls that read them are issued)
+  if (x->type < 0) return QG_OK;
+  if (!new_blocks(x->options, x->tokens, x->channels, &x->held)) return QG_EINVAL;
+  const int rc = qg_fp8_quantize(&x->raw, x->type, &x->held.c, s);
+  x->type = -1;
+  return rc;
+}
+int into_product(activations* x, bool raw_too, qg_fp8_product* p, void* s) {
+  p->tokens = (int)x->tokens;
+  if (x->type >= 0 && raw_too && x->tokens <= QG_FP8_FEW && x->channels % 16 == 0) {
+    p->x_rows = x->raw;
+    p->x_dtype = x->type;
+    return QG_OK;
+  }
+  const int rc = into_blocks(x, s);
+  p->x = x->held.c;
+  return rc;
+}
+struct weight {
+  at::Tensor data;
+  qg_fp8_weight c;
+};
+bool of_weight(PyObject* o, int gated, weight* out) {  // _fast: (k, n, gated)
+  PyObject* const t = PyObject_GetAttr(o, g_name_fast);
+  if (!t) return slow();
+  const bool ok = PyTuple_CheckExact(t) && PyTuple_GET_SIZE(t) == 3 && integer(PyTuple_GET_ITEM(t, 0), &out->c.k) &&
+                  integer(PyTuple_GET_ITEM(t, 1), &out->c.n) && integer(PyTuple_GET_ITEM(t, 2), &out->c.gated);
+  Py_DECREF(t);
+  if (!ok || out->c.gated != gated || !attribute(o, g_name_data, &out->data)) return false;
+  if (!out->data.is_cuda() || (size_t)out->data.nbytes() < qg_fp8_weight_bytes(out->c.k, out->c.n, gated)) return false;
+  out->c.data = out->data.data_ptr();
+  return true;
+}
+bool of_workspace(PyObject* o, int64_t device, void** ws, size_t* bytes) {
+  if (o == Py_None) return true;
+  const at::Tensor* const t = tensor(o);
+  if (!t || !t->is_cuda() || !t->is_contiguous() || t->get_device() != device) return false;
+  *ws = t->data_ptr();
+  *bytes = t->nbytes();
+  return true;
+}
+// The caller's output, or a new one; type: of a new one (-1: x's own, of blocks bfloat16).  As a new reference.
+PyObject* rows_output(PyObject* given, const activations& x, int n, int type, qg_fp8_product* p) {
+  if (given == Py_None) {
+    if (type < 0) type = x.type < 0 ? QG_BF16 : x.type;
+    const at::Tensor y = at::empty({x.tokens, n}, x.options.dtype(element_type(type)));
+    p->out = {y.data_ptr(), y.stride(0)};
+    p->dtype = type;
+    return THPVariable_Wrap(y);
+  }
+  const at::Tensor* const t = tensor(given);
+  if (!rows(t, &p->out) || !untracked(*t) || t->size(0) != x.tokens || t->size(1) != n || t->get_device() != x.device) return nullptr;
+  p->dtype = element(t->scalar_type());
+  if (type >= 0 && type != p->dtype) return nullptr;
+  return Py_NewRef(given);
+}
+PyObject* pair_of(const at::Tensor& a, const at::Tensor* b) {  // (a, b or None)
+  reference first{THPVariable_Wrap(a)};
+  reference second{b ? THPVariable_Wrap(*b) : Py_NewRef(Py_None)};
+  PyObject* const both = first.o && second.o ? PyTuple_Pack(2, first.o, second.o) : nullptr;
+  if (!both) {
+    PyErr_Clear();
+    Py_RETURN_NONE;
+  }
+  return both;
+}
+
+// (x) -> (codes, scales)
+PyObject* fp8_quantize(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  if (n != 1) Py_RETURN_NONE;
+  QG_OR_SLOW(
+    const at::Tensor* const x = tensor(a[0]);
+    qg_rows r = {};
+    blocks to;
+    void* s = nullptr;
+    if (!rows(x, &r) || x->_fw_grad(0).defined() || !here(x->get_device(), &s) || !new_blocks(x->options(), x->size(0), x->size(1), &to)) Py_RETURN_NONE;
+    const int type = element(x->scalar_type());
+    int rc;
+    Py_BEGIN_ALLOW_THREADS
+    rc = qg_fp8_quantize(&r, type, &to.c, s);
+    Py_END_ALLOW_THREADS
+    if (rc != QG_OK) Py_RETURN_NONE;
+    return pair_of(to.codes, &to.scales);)
+}
+
+// (blocks, element type) -> tensor
+PyObject* fp8_dequantize(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  if (n != 2) Py_RETURN_NONE;
+  QG_OR_SLOW(
+    blocks x;
+    int type = 0;
+    void* s = nullptr;
+    if (!old_blocks(a[0], &x) || !integer(a[1], &type) || type < QG_F32 || type > QG_F16 || !here(x.codes.get_device(), &s)) Py_RETURN_NONE;
+    const at::Tensor y = at::empty({x.c.tokens, x.c.channels}, x.codes.options().dtype(element_type(type)));
+    const qg_rows to = {y.data_ptr(), y.stride(0)};
+    int rc;
+    Py_BEGIN_ALLOW_THREADS
+    rc = qg_fp8_dequantize(&x.c, type, &to, s);
+    Py_END_ALLOW_THREADS
+    if (rc != QG_OK) Py_RETURN_NONE;
+    return THPVariable_Wrap(y);)
+}
+
+// (b, up or None, transposed) -> (bytes, of the transpose or None)
+PyObject* fp8_pack(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  if (n != 3) Py_RETURN_NONE;
+  QG_OR_SLOW(
+    const at::Tensor* const b = tensor(a[0]);
+    const at::Tensor* const u = a[1] == Py_None ? nullptr : tensor(a[1]);
+    const int gated = a[1] != Py_None;
+    int transposed = 0;
+    void* s = nullptr;
+    if (!b || (gated && !u) || !truth(a[2], &transposed) || !b->is_cuda() || b->dim() != 2 || element(b->scalar_type()) < 0 || b->size(0) > INT_MAX ||
+        b->size(1) > INT_MAX || b->_fw_grad(0).defined() || !here(b->get_device(), &s))
+      Py_RETURN_NONE;
+    qg_matrix bm = {b->data_ptr(), b->stride(0), b->stride(1)};
+    qg_matrix um = {};
+    if (u) {
+      if (u->sizes() != b->sizes() || u->scalar_type() != b->scalar_type() || u->device() != b->device() || u->_fw_grad(0).defined()) Py_RETURN_NONE;
+      um = {u->data_ptr(), u->stride(0), u->stride(1)};
+    }
+    const int type = element(b->scalar_type());
+    const int64_t back = gated ? 2 * fp8_pitch(b->size(1)) : b->size(1);
+    if (back > INT_MAX) Py_RETURN_NONE;
+    qg_fp8_weight w = {nullptr, (int)b->size(0), (int)b->size(1), gated};
+    qg_fp8_weight t = {nullptr, (int)back, (int)b->size(0), 0};
+    const size_t w_bytes = qg_fp8_weight_bytes(w.k, w.n, gated);
+    const size_t t_bytes = transposed ? qg_fp8_weight_bytes(t.k, t.n, 0) : 1;
+    if (!w_bytes || !t_bytes) Py_RETURN_NONE;
+    const auto options = b->options().dtype(at::kByte);
+    const at::Tensor wd = at::empty({(int64_t)w_bytes}, options);
+    at::Tensor td;
+    w.data = wd.data_ptr();
+    if (transposed) {
+      td = at::empty({(int64_t)t_bytes}, options);
+      t.data = td.data_ptr();
+    }
+    int rc;
+    Py_BEGIN_ALLOW_THREADS
+    rc = qg_fp8_pack(&bm, gated ? &um : nullptr, w.k, w.n, type, &w, transposed ? &t : nullptr, s);
+    Py_END_ALLOW_THREADS
+    if (rc != QG_OK) Py_RETURN_NONE;
+    return pair_of(wd, transposed ? &td : nullptr);)
+}
+
+// (x or blocks, w, bias or None, element type of the result or None, out or None, workspace or None, wide sums or None: for fp32 results)
+PyObject* fp8_matmul(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  if (n != 7) Py_RETURN_NONE;
+  QG_OR_SLOW(
+    activations x;
+    weight w;
+    qg_fp8_product p = {};
+    void* s = nullptr;
+    int type = -1;
+    if (!of_activations(a[0], &x) || !of_weight(a[1], 0, &w) || w.c.k != x.channels || w.data.get_device() != x.device || !here(x.device, &s) ||
+        (a[3] != Py_None && (!integer(a[3], &type) || type < QG_F32 || type > QG_F16)) || !of_workspace(a[5], x.device, &p.workspace, &p.workspace_bytes))
+      Py_RETURN_NONE;
+    if (a[2] != Py_None) {
+      const at::Tensor* const bias = tensor(a[2]);
+      if (!bias || !bias->is_cuda() || bias->scalar_type() != at::kFloat || bias->dim() != 1 || bias->size(0) != w.c.n || !bias->is_contiguous() ||
+          !untracked(*bias) || bias->get_device() != x.device)
+        Py_RETURN_NONE;
+      p.bias = static_cast<const float*>(bias->data_ptr());
+    }
+    reference result{rows_output(a[4], x, w.c.n, type, &p)};
+    if (!result.o) { PyErr_Clear(); Py_RETURN_NONE; }
+    p.wide_sums = p.dtype == QG_F32;
+    if (a[6] != Py_None && !truth(a[6], &p.wide_sums)) Py_RETURN_NONE;
+    int rc = into_product(&x, true, &p, s);
+    if (rc != QG_OK) Py_RETURN_NONE;
+    Py_BEGIN_ALLOW_THREADS
+    rc = qg_fp8_matmul(&w.c, &p, s);
+    Py_END_ALLOW_THREADS
+    if (rc != QG_OK) Py_RETURN_NONE;
+    return result.give();)
+}
+
+// (x or blocks, w, activation, element type or None, out or None, workspace or None, wide sums or None) -> out; new blocks (element type
+// -2): (codes, scales)
+PyObject* fp8_gated(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  if (n != 7) Py_RETURN_NONE;
+  QG_OR_SLOW(
+    activations x;
+    weight w;
+    blocks to;
+    qg_fp8_product p = {};
+    void* s = nullptr;
+    int type = -1;
+    if (!of_activations(a[0], &x) || !of_weight(a[1], 1, &w) || w.c.k != x.channels || w.data.get_device() != x.device || !here(x.device, &s) ||
+        !integer(a[2], &p.activation) || (a[3] != Py_None && !integer(a[3], &type)) || type < -2 || type > QG_F16 ||
+        !of_workspace(a[5], x.device, &p.workspace, &p.workspace_bytes))
+      Py_RETURN_NONE;
+    const bool held = type == -2;
+    reference result{nullptr};
+    if (held) {
+      if (a[4] != Py_None || !new_blocks(x.options, x.tokens, w.c.n, &to)) Py_RETURN_NONE;
+    } else {
+      result.o = rows_output(a[4], x, w.c.n, type, &p);
+      if (!result.o) { PyErr_Clear(); Py_RETURN_NONE; }
+      p.wide_sums = p.dtype == QG_F32;
+    }
+    if (a[6] != Py_None && !truth(a[6], &p.wide_sums)) Py_RETURN_NONE;
+    int rc = into_product(&x, !held, &p, s);
+    if (rc != QG_OK) Py_RETURN_NONE;
+    Py_BEGIN_ALLOW_THREADS
+    rc = qg_fp8_gated(&w.c, &p, held ? &to.c : nullptr, s);
+    Py_END_ALLOW_THREADS
+    if (rc != QG_OK) Py_RETURN_NONE;
+    return held ? pair_of(to.codes, &to.scales) : result.give();)
+}
+
+// (x or blocks, w_in, w_out, activation, element type or None, out or None, workspace or None): gated() and matmul() of what it gives, in
+// fp32 up to 4 * QG_FP8_FEW tokens, else in 8 bits
+PyObject* fp8_feed_forward(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  if (n != 7) Py_RETURN_NONE;
+  QG_OR_SLOW(
+    activations x;
+    activations h = {};
+    weight in;
+    weight down;
+    qg_fp8_product p = {};
+    qg_fp8_product q = {};
+    void* s = nullptr;
+    int type = -1;
+    if (!of_activations(a[0], &x) || !of_weight(a[1], 1, &in) || !of_weight(a[2], 0, &down) || in.c.k != x.channels || down.c.k != in.c.n ||
+        in.data.get_device() != x.device || down.data.get_device() != x.device || !here(x.device, &s) || !integer(a[3], &p.activation) ||
+        (a[4] != Py_None && (!integer(a[4], &type) || type < QG_F32 || type > QG_F16)) || !of_workspace(a[6], x.device, &p.workspace, &p.workspace_bytes))
+      Py_RETURN_NONE;
+    reference result{rows_output(a[5], x, down.c.n, type, &q)};
+    if (!result.o) { PyErr_Clear(); Py_RETURN_NONE; }
+    q.workspace = p.workspace;
+    q.workspace_bytes = p.workspace_bytes;
+    q.wide_sums = q.dtype == QG_F32;
+    const bool few = x.tokens <= 4 * QG_FP8_FEW;
+    at::Tensor middle;
+    h.options = x.options;
+    h.tokens = x.tokens;
+    h.channels = in.c.n;
+    int rc = into_product(&x, few, &p, s);
+    if (rc != QG_OK) Py_RETURN_NONE;
+    if (few) {
+      middle = at::empty({x.tokens, in.c.n}, x.options.dtype(at::kFloat));
+      h.raw = p.out = {middle.data_ptr(), middle.stride(0)};
+      h.type = p.dtype = QG_F32;
+      p.wide_sums = 1;
+      rc = qg_fp8_gated(&in.c, &p, nullptr, s);
+    } else {
+      if (!new_blocks(x.options, x.tokens, in.c.n, &h.held)) Py_RETURN_NONE;
+      h.type = -1;
+      rc = qg_fp8_gated(&in.c, &p, &h.held.c, s);
+    }
+    if (rc == QG_OK) rc = into_product(&h, true, &q, s);
+    if (rc == QG_OK) rc = qg_fp8_matmul(&down.c, &q, s);
+    if (rc != QG_OK) Py_RETURN_NONE;
+    return result.give();)
+}
+
+// (blocks, dy, second dy or None, element type, workspace or None) -> (gradient, second or None)
+PyObject* fp8_weight_gradient(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  if (n != 5) Py_RETURN_NONE;
+  QG_OR_SLOW(
+    blocks x;
+    const at::Tensor* const dy = tensor(a[1]);
+    const at::Tensor* const dy2 = a[2] == Py_None ? nullptr : tensor(a[2]);
+    qg_rows r = {};
+    qg_rows r2 = {};
+    int type = 0;
+    void* s = nullptr; void* ws = nullptr;
+    size_t bytes = 0;
+    if (!old_blocks(a[0], &x) || !rows(dy, &r) || dy->size(0) != x.c.tokens || !untracked(*dy) || dy->get_device() != x.codes.get_device() ||
+        !integer(a[3], &type) || type < QG_F32 || type > QG_F16 || !here(dy->get_device(), &s) || !of_workspace(a[4], dy->get_device(), &ws, &bytes))
+      Py_RETURN_NONE;
+    if (a[2] != Py_None && (!rows(dy2, &r2) || dy2->sizes() != dy->sizes() || dy2->scalar_type() != dy->scalar_type() || !untracked(*dy2) ||
+                            dy2->device() != dy->device()))
+      Py_RETURN_NONE;
+    const auto options = dy->options().dtype(element_type(type));
+    const at::Tensor y = at::empty({x.c.channels, dy->size(1)}, options);
+    const qg_rows out = {y.data_ptr(), y.stride(0)};
+    at::Tensor y2;
+    qg_rows out2 = {};
+    if (dy2) {
+      y2 = at::empty({x.c.channels, dy->size(1)}, options);
+      out2 = {y2.data_ptr(), y2.stride(0)};
+    }
+    const int dy_type = element(dy->scalar_type()); const int columns = (int)dy->size(1);
+    int rc;
+    Py_BEGIN_ALLOW_THREADS
+    rc = qg_fp8_weight_gradient(&x.c, &r, dy2 ? &r2 : nullptr, dy_type, columns, &out, dy2 ? &out2 : nullptr, type, ws, bytes, s);
+    Py_END_ALLOW_THREADS
+    if (rc != QG_OK) Py_RETURN_NONE;
+    return pair_of(y, dy2 ? &y2 : nullptr);)
+}
+
 // ---- a call whose arguments are marshalled once
 enum call_kind { CALL_GEMM, CALL_CONV_GROUP, CALL_CONV_DENSE, CALL_KINDS };
 const char* const call_names[CALL_KINDS] = {"qg_gemm_u8s8_requant", "qg_conv_groupwise_u8s8_requant", "qg_conv_dense_u8s8_requant"};
@@ -499,6 +889,13 @@ PyMethodDef methods[] = {
     {"kv4_append", QG_FAST(kv4_append), METH_FASTCALL, nullptr},
     {"kv4_attention", QG_FAST(kv4_attention), METH_FASTCALL, nullptr},
     {"kv4_read", QG_FAST(kv4_read), METH_FASTCALL, nullptr},
+    {"fp8_quantize", QG_FAST(fp8_quantize), METH_FASTCALL, nullptr},
+    {"fp8_dequantize", QG_FAST(fp8_dequantize), METH_FASTCALL, nullptr},
+    {"fp8_pack", QG_FAST(fp8_pack), METH_FASTCALL, nullptr},
+    {"fp8_matmul", QG_FAST(fp8_matmul), METH_FASTCALL, nullptr},
+    {"fp8_gated", QG_FAST(fp8_gated), METH_FASTCALL, nullptr},
+    {"fp8_feed_forward", QG_FAST(fp8_feed_forward), METH_FASTCALL, nullptr},
+    {"fp8_weight_gradient", QG_FAST(fp8_weight_gradient), METH_FASTCALL, nullptr},
     {"init", init, METH_VARARGS, nullptr},
     {nullptr, nullptr, 0, nullptr},
 };
@@ -514,7 +911,11 @@ PyMODINIT_FUNC PyInit__binding() {
   call_type.tp_new = PyType_GenericNew;  // (zeroed: launch() of an object without arguments is refused by the call)
   if (PyType_Ready(&call_type) < 0) return nullptr;
   g_name_fast = PyUnicode_InternFromString("_fast");
-  PyObject* const m = g_name_fast ? PyModule_Create(&module) : nullptr;
+  g_name_codes = PyUnicode_InternFromString("codes");
+  g_name_scales = PyUnicode_InternFromString("scales");
+  g_name_shape = PyUnicode_InternFromString("shape");
+  g_name_data = PyUnicode_InternFromString("data");
+  PyObject* const m = g_name_fast && g_name_codes && g_name_scales && g_name_shape && g_name_data ? PyModule_Create(&module) : nullptr;
   if (m && PyModule_AddObjectRef(m, "Call", reinterpret_cast<PyObject*>(&call_type)) < 0) {
     Py_DECREF(m);
     return nullptr;

@@ -23,12 +23,6 @@ typedef u2 u2_any __attribute__((aligned(2)));
 __device__ inline unsigned pair_low(unsigned a, unsigned b) { return __builtin_amdgcn_perm(b, a, 0x05040100u); }   // low halves
 __device__ inline unsigned pair_high(unsigned a, unsigned b) { return __builtin_amdgcn_perm(b, a, 0x07060302u); }  // high halves
 
-__device__ inline unsigned bf16_pair(float a, float b) {
-  const b2 v = {(__bf16)a, (__bf16)b};
-  return __builtin_bit_cast(unsigned, v);
-}
-__device__ inline float bf16_up(unsigned half) { return __builtin_bit_cast(float, half << 16); }
-
 // CW neighbouring columns of a token as dwords of two bf16, PARTS numbers each
 template <int TYPE, int PARTS, int CW>
 struct dy_line {
@@ -59,26 +53,31 @@ struct dy_line {
       }
     }
   }
-  __device__ inline void split(int pair, unsigned (&out)[PARTS]) const {  // columns 2 pair and 2 pair + 1
+  // Columns 2 pair and 2 pair + 1 in bf16 parts: each takes the first 8 bits of what is left, so that no bit is lost, for an AND and an exact
+  // difference a part (rounding to nearest takes three times as many instructions: a stage of a 128 x 128 tile of fp32 2.7 us so,
+  // 1.9 now).  What an infinity leaves is nothing, not NaN.
+  __device__ inline void split(int pair, unsigned (&out)[PARTS]) const {
     if constexpr (TYPE == QG_BF16) {
       out[0] = raw[pair];
     } else {
-      float a, b;
+      unsigned v[2];
       if constexpr (TYPE == QG_F32) {
-        a = __builtin_bit_cast(float, raw[2 * pair]);
-        b = __builtin_bit_cast(float, raw[2 * pair + 1]);
+        v[0] = raw[2 * pair];
+        v[1] = raw[2 * pair + 1];
       } else {
-        const h2 v = __builtin_bit_cast(h2, raw[pair]);
-        a = (float)v[0];
-        b = (float)v[1];
+        const h2 both = __builtin_bit_cast(h2, raw[pair]);
+        v[0] = __builtin_bit_cast(unsigned, (float)both[0]);
+        v[1] = __builtin_bit_cast(unsigned, (float)both[1]);
       }
 #pragma unroll
       for (int p = 0; p < PARTS; ++p) {
-        out[p] = bf16_pair(a, b);
-        const float ra = bf16_up(out[p] & 0xffffu), rb = bf16_up(out[p] >> 16);
-        // (what does not fit: exact; of an infinity nothing, it would become NaN)
-        a = __builtin_isfinite(ra) ? a - ra : 0.0f;
-        b = __builtin_isfinite(rb) ? b - rb : 0.0f;
+        out[p] = pair_high(v[0], v[1]);
+        if (p + 1 == PARTS) break;
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const float all = __builtin_bit_cast(float, v[i]), left = all - __builtin_bit_cast(float, v[i] & 0xffff0000u);
+          v[i] = __builtin_bit_cast(unsigned, p == 0 && __builtin_isinf(all) ? 0.0f : left);
+        }
       }
     }
   }
@@ -95,7 +94,8 @@ __device__ inline void add_product(f16v& c, b8 a, b8 b) {
 // the result.  While a stage is multiplied the next one, which is in registers, goes to the other half of LDS, and the one after that is
 // requested: both in pieces between the matrix instructions, in whose shadow they cost little.
 //   256 x 256, one wave per SIMD: LDS is read 64 KiB a stage and half-filled once, 96 of its 128 bytes a cycle; a wave of 64 x 64 would read
-//   as much for a quarter of the products.  128 x 128 where there are few tiles.
+//   as much for a quarter of the products.  8192 x 4096 x 10240, two matrices of a gated block: 1.32 ms, 1.04 PFLOP/s, where a large bf16
+//   library product reaches 1.27; 4096^3, one tile a CU: 175 us, 0.79.  128 x 128 and 64 x 64 where there are few tiles.
 template <int TILE, int TYPE, int PARTS>
 __global__ __launch_bounds__(256, TILE == 256 || PARTS > 1 ? 1 : 2) void qg_fp8_gradient_kernel(qg_fp8_gradient_args p, int row_tiles, int column_tiles) {
   constexpr int CW = TILE == 256 && PARTS == 1 ? 8 : 4, TS = 256 * 8 * CW / TILE, WT = TILE / 2, F = WT / 32, STEPS = TS / TILE_K;
@@ -142,16 +142,22 @@ __global__ __launch_bounds__(256, TILE == 256 || PARTS > 1 ? 1 : 2) void qg_fp8_
     }
     to.scale[i] = from_memory<uint8_t>(scale);
   };
+  unsigned nowhere = 0;
+  asm volatile("" : "+v"(nowhere));
+  auto fetch_none = [&](tokens& to, int i) {  // of a stage behind the last token: zeros, by as many requests (fewer, and every wait would be for all)
+    fetch_x(to, no_numbers + nowhere, no_numbers + nowhere, i);
+    to.y[i].load(reinterpret_cast<const T*>(no_numbers + nowhere));
+  };
   auto fetch = [&](tokens& to, int from, int i, bool inside) {  // token i of this thread's eight
-    const uint8_t* const src = p.x8.codes + (long long)(from + i) * p.x8.pitch + x_mine;
-    const uint8_t* const scale = p.x8.scales + (long long)(from + i) * p.x8.scale_pitch + s_mine;
+    const uint8_t* src = p.x8.codes + (long long)(from + i) * p.x8.pitch;
+    const uint8_t* scale = p.x8.scales + (long long)(from + i) * p.x8.scale_pitch;
     const T* line = y_base + (long long)(from - t0 + i) * dy.stride;
     if (inside) {
-      fetch_x(to, src, scale, i);
+      fetch_x(to, src + x_mine, scale + s_mine, i);
       to.y[i].load(line);
     } else {
       const bool there = from + 8 * tb + i < t1;   // (a token behind the last: zeros)
-      fetch_x(to, there ? src : no_numbers, there ? scale : no_numbers, i);
+      fetch_x(to, there ? src + x_mine : no_numbers, there ? scale + s_mine : no_numbers, i);
       line = there ? line : reinterpret_cast<const T*>(no_numbers);
       if (narrow) {
         to.y[i].load_some(line, p.n - 1);
@@ -220,8 +226,9 @@ __global__ __launch_bounds__(256, TILE == 256 || PARTS > 1 ? 1 : 2) void qg_fp8_
     // all of it has long been in LDS and nobody waits.
     constexpr int PRODUCTS = GROUPS * PARTS * F, PIECES = PAIRS * SLICES;
     constexpr int MOVE = PARTS == 1 ? PRODUCTS * 3 / 8 : PRODUCTS / 2, REQUEST = PRODUCTS / 8 < 8 ? PRODUCTS / 4 : 8;
-    b8 x[2][F], g[3][PARTS];
-    auto read_x = [&](const uint8_t* stage, int s, int i) { x[s & 1][i] = operand(stage, wr * F + i, s); };
+    constexpr int X_AHEAD = F > 1 ? 1 : 2, X_RING = F > 1 ? 2 : 4;  // steps
+    b8 x[X_RING][F], g[3][PARTS];
+    auto read_x = [&](const uint8_t* stage, int s, int i) { x[s % X_RING][i] = operand(stage, wr * F + i, s); };
     auto read_g = [&](const uint8_t* stage, int to, int group) {
 #pragma unroll
       for (int q = 0; q < PARTS; ++q) g[to][q] = operand(stage + (1 + q) * PLANE, wc * F + group % F, group / F);
@@ -244,12 +251,15 @@ __global__ __launch_bounds__(256, TILE == 256 || PARTS > 1 ? 1 : 2) void qg_fp8_
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
             __builtin_amdgcn_s_barrier();
             asm volatile("" ::: "memory");
+            if constexpr (F > 1) {
 #pragma unroll
-            for (int k = 0; k < F; ++k) read_x(other, 0, k);
+              for (int k = 0; k < F; ++k) read_x(other, 0, k);
+            }
           }
+          if constexpr (F == 1) read_x(s + 2 < STEPS ? stage : other, (s + 2) % STEPS, 0);
           if constexpr (group + 2 < GROUPS) read_g(stage, (RING0 + group + 2) % 3, group + 2);
           if constexpr (group + 2 >= GROUPS) read_g(other, (RING0 + group + 2) % 3, group + 2 - GROUPS);
-          if constexpr (s + 1 < STEPS && j < 2) {  // the next step's rows
+          if constexpr (F > 1 && s + 1 < STEPS && j < 2) {  // the next step's rows
 #pragma unroll
             for (int k = 0; k < F / 2; ++k) read_x(stage, s + 1, j * (F / 2) + k);
           }
@@ -263,15 +273,17 @@ __global__ __launch_bounds__(256, TILE == 256 || PARTS > 1 ? 1 : 2) void qg_fp8_
           constexpr int first = (n - MOVE) * 8 / REQUEST, last = (n - MOVE + 1) * 8 / REQUEST;
           if (inside) {
             each<first, last>([&](auto token) { fetch(next, ahead, decltype(token)::value, true); });
+          } else if (ahead >= t1) {
+            each<first, last>([&](auto token) { fetch_none(next, decltype(token)::value); });
           } else {
             each<first, last>([&](auto token) { fetch(next, ahead, decltype(token)::value, false); });
           }
         }
-        add_product(c[i][j], g[(RING0 + group) % 3][q], x[s & 1][i]);
+        add_product(c[i][j], g[(RING0 + group) % 3][q], x[s % X_RING][i]);
         __builtin_amdgcn_sched_barrier(0);
       });
     };
-    static_assert(STEPS % 2 == 0 && F % 2 == 0 && GROUPS / 2 * PARTS * F >= MOVE, "the next stage is in LDS when it is read");
+    static_assert(STEPS % X_RING == 0 && (F == 1 || F % 2 == 0) && GROUPS / 2 * PARTS * F >= MOVE, "the next stage is in LDS when it is read");
     fetch_all(even, t0);
     fetch_all(odd, t0 + TS);
 #pragma unroll
@@ -281,7 +293,7 @@ __global__ __launch_bounds__(256, TILE == 256 || PARTS > 1 ? 1 : 2) void qg_fp8_
     fetch_all(even, t0 + 2 * TS);
     __syncthreads();
 #pragma unroll
-    for (int k = 0; k < F; ++k) read_x(lds, 0, k);
+    for (int k = 0; k < F * X_AHEAD; ++k) read_x(lds, k / F, k % F);
     read_g(lds, 0, 0);
     read_g(lds, 1, 1);
 #pragma unroll 1
@@ -310,7 +322,7 @@ __global__ __launch_bounds__(256, TILE == 256 || PARTS > 1 ? 1 : 2) void qg_fp8_
 #pragma unroll
     for (int j = 0; j < F; ++j) asm volatile("" : "+a"(c[i][j]));
   // a lane has, of fragment (i, j), row 32 i + lane % 32 and the columns 32 j + 8 (e / 4) + 4 (lane / 32) + e % 4
-  if (TILE == 128 && p.slices > 1) {  // sums of the slices through memory; the last one to arrive adds them in order
+  if (TILE < 256 && p.slices > 1) {  // sums of the slices through memory; the last one to arrive adds them in order
     const int tile = row_tile * column_tiles + all_columns;
     const size_t step = (size_t)TILE * TILE;
     float* const mine = p.partial + (size_t)tile * p.slices * step + (size_t)wave * (F * F * 1024) + lane * 4;
@@ -335,21 +347,30 @@ __global__ __launch_bounds__(256, TILE == 256 || PARTS > 1 ? 1 : 2) void qg_fp8_
       for (int j = 0; j < F; ++j)
 #pragma unroll
         for (int e = 0; e < 16; ++e) c[i][j][e] = 0.0f;
-    for (int s = 0; s < p.slices; ++s)
+    for (int s = 0; s < p.slices; s += 2) {  // two requested at once
+      f4 v[2][F * F * 4];
 #pragma unroll
-      for (int i = 0; i < F; ++i)
+      for (int u = 0; u < 2; ++u) {
+        const float* const from = mine + (size_t)min(s + u, p.slices - 1) * step;
 #pragma unroll
-        for (int j = 0; j < F; ++j)
+        for (int e = 0; e < F * F * 4; ++e) {
+          const unsigned long long* const pair = reinterpret_cast<const unsigned long long*>(from + e * 256);
+          const unsigned long long low = __hip_atomic_load(pair, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+          const unsigned long long high = __hip_atomic_load(pair + 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+          v[u][e] = (f4){__builtin_bit_cast(float, (unsigned)low), __builtin_bit_cast(float, (unsigned)(low >> 32)),
+                         __builtin_bit_cast(float, (unsigned)high), __builtin_bit_cast(float, (unsigned)(high >> 32))};
+        }
+      }
+      __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const unsigned long long* from = reinterpret_cast<const unsigned long long*>(mine + s * step + ((i * F + j) * 4 + e) * 256);
-            const unsigned long long a = __hip_atomic_load(from, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-            const unsigned long long b = __hip_atomic_load(from + 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-            c[i][j][4 * e] += __builtin_bit_cast(float, (unsigned)a);
-            c[i][j][4 * e + 1] += __builtin_bit_cast(float, (unsigned)(a >> 32));
-            c[i][j][4 * e + 2] += __builtin_bit_cast(float, (unsigned)b);
-            c[i][j][4 * e + 3] += __builtin_bit_cast(float, (unsigned)(b >> 32));
-          }
+      for (int u = 0; u < 2; ++u) {
+        if (s + u >= p.slices) break;
+#pragma unroll
+        for (int e = 0; e < F * F * 4; ++e)
+#pragma unroll
+          for (int k = 0; k < 4; ++k) c[e / (F * 4)][e / 4 % F][4 * (e % 4) + k] += v[u][e][k];
+      }
+    }
   }
 #pragma unroll
   for (int i = 0; i < F; ++i) {
@@ -383,5 +404,5 @@ hipError_t launch(const qg_fp8_gradient_args& a, hipStream_t s) {
 }  // namespace
 
 hipError_t qg_launch_fp8_gradient(const qg_fp8_gradient_args& a, int tile, hipStream_t s) {
-  return tile == 256 ? launch<256>(a, s) : launch<128>(a, s);
+  return tile == 256 ? launch<256>(a, s) : tile == 128 ? launch<128>(a, s) : launch<64>(a, s);
 }

@@ -13,7 +13,8 @@ Activations are [tokens, channels] in float32, bfloat16 or float16 with a unit s
 is.  Weights may have any strides.  A product computes with the 8-bit values of both; results are of x's type unless said otherwise.
 In the training calls gradients of 8-bit values pass to what they stand for, the gradient that comes in is put into 8 bits for the
 product with the weights, and taken as it is for the weights' own gradient.
-Argument marshalling only, like qgemm.py.
+Argument marshalling only, like qgemm.py: the calls go through the binding, and where it gives None through the checks here, which name
+the error.
 """
 import ctypes
 
@@ -80,22 +81,39 @@ class Blocks:
         assert channels >= 1 and codes.is_contiguous() and tuple(codes.shape) == (tokens, _up(channels, BLOCK))
         assert scales.is_contiguous() and tuple(scales.shape) == (tokens, _up(_up(channels, BLOCK) // BLOCK, 4))
         self.codes, self.scales, self.shape, self.device = codes, scales, (tokens, channels), codes.device
-        self._desc = _BlocksDesc(codes.data_ptr(), scales.data_ptr(), tokens, channels)
-        self._ref = ctypes.byref(self._desc)
+
+    @property
+    def _desc(self):
+        return _BlocksDesc(self.codes.data_ptr(), self.scales.data_ptr(), *self.shape)
+
+    @property
+    def _ref(self):
+        return ctypes.byref(self._desc)
+
+
+def _blocks(pair, channels):                   # (what the binding made needs no checks)
+    b = Blocks.__new__(Blocks)
+    b.codes, b.scales = codes, _ = pair
+    b.shape, b.device = (codes.shape[0], channels), codes.device
+    return b
 
 
 class Weight:
     """Weights in 8 bits in the library's own layout: B [k, n], or a pair of such matrices (gated).  transposed: the same for products
     with the transpose, where it was asked for."""
 
-    def __init__(self, k, n, gated, device, transposed=None):
-        size = lib.qg_fp8_weight_bytes(k, n, int(gated))
-        if size == 0:
-            raise QGemmError(-2, "qg_fp8_weight_bytes")
-        self.data = torch.empty(size, dtype=torch.uint8, device=device)
-        self.k, self.n, self.gated, self.transposed, self.device = k, n, bool(gated), transposed, self.data.device
-        self._desc = _WeightDesc(self.data.data_ptr(), k, n, int(gated))
-        self._ref = ctypes.byref(self._desc)
+    def __init__(self, k, n, gated, device, transposed=None, data=None):
+        if data is None:
+            size = lib.qg_fp8_weight_bytes(k, n, int(gated))
+            if size == 0:
+                raise QGemmError(-2, "qg_fp8_weight_bytes")
+            data = torch.empty(size, dtype=torch.uint8, device=device)
+        self.data, self.k, self.n, self.gated, self.transposed, self.device = data, k, n, bool(gated), transposed, data.device
+        self._fast = (k, n, int(gated))
+
+    @property
+    def _ref(self):
+        return ctypes.byref(_WeightDesc(self.data.data_ptr(), *self._fast))
 
 
 def _up(x, m):
@@ -142,6 +160,10 @@ def new_blocks(tokens, channels, device="cuda"):
 
 def quantize(x, out=None):
     """x [tokens, channels] in 8 bits."""
+    if out is None:
+        done = _binding.fp8_quantize(x)
+        if done is not None:
+            return _blocks(done, x.shape[1])
     x = x.detach()
     _check_rows(x)
     if out is None:
@@ -154,6 +176,10 @@ def quantize(x, out=None):
 
 def dequantize(x, dtype=torch.float32, out=None):
     """The values that x stands for, [tokens, channels] of `dtype`."""
+    if out is None and dtype in _TYPES:
+        done = _binding.fp8_dequantize(x, _TYPES[dtype])
+        if done is not None:
+            return done
     _on(x.device)
     if out is None:
         out = torch.empty(x.shape, dtype=dtype, device=x.device)
@@ -164,7 +190,13 @@ def dequantize(x, dtype=torch.float32, out=None):
     return out
 
 
-def _pack(b, up, transposed, only_transposed=False):
+def _pack(b, up, transposed):
+    done = _binding.fp8_pack(b, up, transposed)
+    if done is not None:
+        (k, n), (data, back) = b.shape, done
+        t = None if back is None else Weight(2 * _up(n, BLOCK) if up is not None else n, k, False, None, data=back)
+        return Weight(k, n, up is not None, None, t, data)
+    b, up = b.detach(), None if up is None else up.detach()
     assert b.dim() == 2 and b.dtype in _TYPES
     k, n = b.shape
     if up is not None:
@@ -181,12 +213,12 @@ def _pack(b, up, transposed, only_transposed=False):
 
 def pack(b, transposed=False):
     """Weights B [in, out] in 8 bits; transposed: for products with the transpose too."""
-    return _pack(b.detach(), None, transposed)
+    return _pack(b, None, transposed)
 
 
 def pack_gated(gate, up, transposed=False):
     """The two input matrices [in, inner] of a gated block."""
-    return _pack(gate.detach(), up.detach(), transposed)
+    return _pack(gate, up, transposed)
 
 
 def workspace(device="cuda"):
@@ -238,6 +270,9 @@ def _out(x, w, dtype, out):
 def matmul(x, w, bias=None, dtype=None, out=None, workspace=None, wide_sums=None):
     """x B + bias: x [tokens, in] or Blocks; bias float32 [out].  dtype: of the result, by default x's (of Blocks: bfloat16).  wide_sums:
     sums all in fp32, at half the rate of the 8-bit matrix cores, whose own are about 2e-5 off (default: where the result is float32)."""
+    done = _binding.fp8_matmul(x, w, bias, None if dtype is None else _TYPES.get(dtype, -1), out, workspace, wide_sums)
+    if done is not None:
+        return done
     _no_gradient("matmul", x, bias, out)
     assert not w.gated
     out = _out(x, w, dtype, out)
@@ -249,6 +284,10 @@ def matmul(x, w, bias=None, dtype=None, out=None, workspace=None, wide_sums=None
 def gated(x, w, activation="silu", dtype=None, out=None, workspace=None, wide_sums=None):
     """activation(x Gate) * (x Up) in one kernel, [tokens, inner]; w from pack_gated().  `out` may be Blocks: the result in 8 bits.
     wide_sums: as in matmul()."""
+    if activation in ACTIVATIONS and not isinstance(out, Blocks):
+        done = _binding.fp8_gated(x, w, ACTIVATIONS[activation], None if dtype is None else _TYPES.get(dtype, -3), out, workspace, wide_sums)
+        if done is not None:
+            return done
     _no_gradient("gated", x, out)
     assert w.gated
     if isinstance(out, Blocks):
@@ -262,6 +301,13 @@ def gated(x, w, activation="silu", dtype=None, out=None, workspace=None, wide_su
                         wide_sums=out.dtype == torch.float32 if wide_sums is None else wide_sums)
     _check(lib.qg_fp8_gated(w._ref, ctypes.byref(p), None, _stream()), "qg_fp8_gated")
     return out
+
+
+def _gated8(x, w, activation, workspace):
+    done = _binding.fp8_gated(x, w, ACTIVATIONS[activation], -2, None, workspace, None)
+    if done is not None:
+        return _blocks(done, w.n)
+    return gated(x, w, activation, out=new_blocks(x.shape[0], w.n, x.device), workspace=workspace)
 
 
 def gated_backward(x, w, dh, activation="silu", workspace=None):
@@ -288,6 +334,10 @@ def weight_gradient(x, dy, dtype=None, out=None, workspace=None):
     dys = tuple(dy) if pair else (dy,)
     outs = (None,) * len(dys) if out is None else tuple(out) if pair else (out,)
     assert isinstance(x, Blocks) and 1 <= len(dys) <= 2 and len(outs) == len(dys)
+    if out is None and (dtype or dys[0].dtype) in _TYPES:
+        done = _binding.fp8_weight_gradient(x, dys[0], dys[1] if len(dys) == 2 else None, _TYPES[dtype or dys[0].dtype], workspace)
+        if done is not None:
+            return done[:len(dys)] if pair else done[0]
     _no_gradient("weight_gradient", *dys, *outs)
     dtype = dtype if dtype is not None else outs[0].dtype if outs[0] is not None else dys[0].dtype
     done = []
@@ -314,13 +364,17 @@ def weight_gradient(x, dy, dtype=None, out=None, workspace=None):
 def feed_forward(x, w_in, w_out, activation="silu", dtype=None, out=None, workspace=None):
     """(activation(x Gate) * (x Up)) Down: w_in from pack_gated(), w_out from pack().  What is between goes into the second product in 8
     bits, made from its fp32 value."""
+    if activation in ACTIVATIONS:
+        done = _binding.fp8_feed_forward(x, w_in, w_out, ACTIVATIONS[activation], None if dtype is None else _TYPES.get(dtype, -1), out, workspace)
+        if done is not None:
+            return done
     _no_gradient("feed_forward", x, out)
     assert w_in.gated and not w_out.gated and w_out.k == w_in.n
     out = _out(x, w_out, dtype, out)
     if x.shape[0] <= 4 * FEW:
         h = gated(x, w_in, activation, dtype=torch.float32, workspace=workspace)
     else:
-        h = gated(x, w_in, activation, out=new_blocks(x.shape[0], w_in.n, x.device), workspace=workspace)
+        h = _gated8(x, w_in, activation, workspace)
     return matmul(h, w_out, out=out, workspace=workspace)
 
 
@@ -360,7 +414,7 @@ class _GatedMlp(torch.autograd.Function):
         back = any(ctx.needs_input_grad)
         w_in, w_out = pack_gated(gate, up, transposed=ctx.needs_input_grad[0]), pack(down, transposed=back)
         x8 = quantize(x)
-        h8 = gated(x8, w_in, activation, out=new_blocks(x.shape[0], gate.shape[1], x.device), workspace=ws)
+        h8 = _gated8(x8, w_in, activation, ws)
         if back:
             ctx.x8, ctx.w_in, ctx.w_out = x8, w_in, w_out.transposed
         ctx.activation, ctx.ws, ctx.types = activation, ws, (x.dtype, gate.dtype, down.dtype)
