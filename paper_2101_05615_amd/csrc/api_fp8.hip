@@ -292,10 +292,10 @@ int qg_fp8_weight_gradient(const qg_fp8_blocks* x, const qg_rows* dy, const qg_r
   a.k = x->channels;
   a.n = n;
   auto tiles_of = [&](long long tile) { return (a.k + tile - 1) / tile * ((n + tile - 1) / tile) * (out2 ? 2 : 1); };
-  // Large tiles where they are enough for the chip, small ones where these are at most one a CU: 4096^3 175 us with 256 x 256 and 237 with
+  // Large tiles where they are enough for the chip, small ones where these are at most one a CU: 4096^3 140 us with 256 x 256 and 237 with
   // 128 x 128; 777 x 1000 x 520 fp32 19 us with 64 x 64 and 21 with 128 x 128, split over tokens.  Between: 300 x 2800 x 1024 fp16
   // 17 us with 128 x 128, 29 with 64 x 64.
-  const int tile = tiles_of(256) >= 200 ? 256 : tiles_of(64) <= 256 ? 64 : 128;
+  const int tile = n < 8 || tiles_of(64) <= 256 ? 64 : tiles_of(256) >= 200 ? 256 : 128;
   const long long tiles = tiles_of(tile);
   a.slices = 1;
   a.slice_tokens = a.tokens;

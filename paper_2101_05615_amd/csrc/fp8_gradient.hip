@@ -13,7 +13,6 @@ typedef float f16v __attribute__((ext_vector_type(16)));
 
 constexpr int TILE_K = 16;  // tokens of a matrix instruction
 
-__device__ const uint8_t no_numbers[64] __attribute__((aligned(16))) = {};
 // (said to be in memory, or the compiler takes a selected address for one that could lie in LDS)
 template <typename V>
 __device__ inline V from_memory(const void* p) { return *(const __attribute__((address_space(1))) V*)p; }
@@ -52,6 +51,10 @@ struct dy_line {
         asm volatile("" : "+v"(raw[i]));  // (put together here, not wherever they are used)
       }
     }
+  }
+  __device__ inline void keep(bool all) {
+#pragma unroll
+    for (int i = 0; i < BYTES / 4; ++i) raw[i] = all ? raw[i] : 0u;
   }
   // Columns 2 pair and 2 pair + 1 in bf16 parts: each takes the first 8 bits of what is left, so that no bit is lost, for an AND and an exact
   // difference a part (rounding to nearest takes three times as many instructions: a stage of a 128 x 128 tile of fp32 2.7 us so,
@@ -94,9 +97,10 @@ __device__ inline void add_product(f16v& c, b8 a, b8 b) {
 // the result.  While a stage is multiplied the next one, which is in registers, goes to the other half of LDS, and the one after that is
 // requested: both in pieces between the matrix instructions, in whose shadow they cost little.
 //   256 x 256, one wave per SIMD: LDS is read 64 KiB a stage and half-filled once, 96 of its 128 bytes a cycle; a wave of 64 x 64 would read
-//   as much for a quarter of the products.  8192 x 4096 x 10240, two matrices of a gated block: 1.32 ms, 1.04 PFLOP/s, where a large bf16
-//   library product reaches 1.27; 4096^3, one tile a CU: 175 us, 0.79.  128 x 128 and 64 x 64 where there are few tiles.
-template <int TILE, int TYPE, int PARTS>
+//   as much for a quarter of the products.  8192 x 4096 x 10240 685 us, 1.0 PFLOP/s, where a large bf16 library product reaches 1.27;
+//   4096^3, one tile a CU, 140 us, 0.98.  What is left is the clock under this load (1.8 of 2.4 GHz) and waves that do all in turn.  128 x 128 and 64 x 64 where there are few tiles.
+// NARROW: fewer columns of dy than a thread brings at a time.
+template <int TILE, int TYPE, int PARTS, bool NARROW>
 __global__ __launch_bounds__(256, TILE == 256 || PARTS > 1 ? 1 : 2) void qg_fp8_gradient_kernel(qg_fp8_gradient_args p, int row_tiles, int column_tiles) {
   constexpr int CW = TILE == 256 && PARTS == 1 ? 8 : 4, TS = 256 * 8 * CW / TILE, WT = TILE / 2, F = WT / 32, STEPS = TS / TILE_K;
   constexpr int PLANE = TILE * TS * 2, STAGE = PLANE * (1 + PARTS), PAIRS = CW / 2, GROUPS = STEPS * F;
@@ -120,58 +124,56 @@ __global__ __launch_bounds__(256, TILE == 256 || PARTS > 1 ? 1 : 2) void qg_fp8_
   const int c0 = t % CHUNKS * CW, tb = t / CHUNKS;
   // (chunks that would end behind the last column end there: two threads bring the same columns, and what lies behind is never written)
   const int cx = min(c0, p.x8.pitch - CW - row_tile * TILE), cy = max(min(c0, p.n - CW - column_tile * TILE), 0);
-  const bool narrow = p.n < CW;
   const int xc = row_tile * TILE + cx, yc = column_tile * TILE + cy;
   typedef typename qg_elem<TYPE>::t T;
-  // addresses: what all threads share, which moves on token by token, and this thread's part
-  const unsigned x_mine = (unsigned)(8 * tb) * (unsigned)p.x8.pitch + (unsigned)xc;
-  const unsigned s_mine = (unsigned)(8 * tb) * (unsigned)p.x8.scale_pitch + (unsigned)(xc / QG_FP8_BLOCK);
-  const T* const y_base = static_cast<const T*>(dy.data) + (long long)(t0 + 8 * tb) * dy.stride + yc;
+  // A thread requests its eight tokens of a stage wherever they are: those behind the last token are the last eight again, whose part that
+  // other threads have becomes zeros on the way to LDS.  So every stage makes the same requests, and waits are for exactly those they mean.
+  const int count = min(8, t1 - t0), back = t1 - count;
   struct tokens {  // this thread's part of a stage, on its way
     unsigned x[8][CW / 4], scale[8];
     dy_line<TYPE, PARTS, CW> y[8];
   };
   tokens even, odd;
-  auto fetch_x = [&](tokens& to, const uint8_t* src, const uint8_t* scale, int i) {
-    if constexpr (CW == 8) {
-      const u2 v = from_memory<u2>(src);
-      to.x[i][0] = v[0];
-      to.x[i][1] = v[1];
+  auto fetch = [&](tokens& to, int from, int i, int part) {  // of token i of this thread's eight of the stage that begins at `from`
+    const int shared = min(from, back), row = shared + min(i, count - 1);          // the same in all threads
+    const unsigned further = (unsigned)(min(from + 8 * tb, back) - shared);        // this thread's part
+    if (part == 0) {
+      const uint8_t* const src = p.x8.codes + (long long)row * p.x8.pitch + (further * (unsigned)p.x8.pitch + (unsigned)xc);
+      if constexpr (CW == 8) {
+        const u2 v = from_memory<u2>(src);
+        to.x[i][0] = v[0];
+        to.x[i][1] = v[1];
+      } else {
+        to.x[i][0] = from_memory<unsigned>(src);
+      }
+    } else if (part == 1) {
+      to.scale[i] = from_memory<uint8_t>(p.x8.scales + (long long)row * p.x8.scale_pitch + (further * (unsigned)p.x8.scale_pitch + (unsigned)(xc / QG_FP8_BLOCK)));
     } else {
-      to.x[i][0] = from_memory<unsigned>(src);
-    }
-    to.scale[i] = from_memory<uint8_t>(scale);
-  };
-  unsigned nowhere = 0;
-  asm volatile("" : "+v"(nowhere));
-  auto fetch_none = [&](tokens& to, int i) {  // of a stage behind the last token: zeros, by as many requests (fewer, and every wait would be for all)
-    fetch_x(to, no_numbers + nowhere, no_numbers + nowhere, i);
-    to.y[i].load(reinterpret_cast<const T*>(no_numbers + nowhere));
-  };
-  auto fetch = [&](tokens& to, int from, int i, bool inside) {  // token i of this thread's eight
-    const uint8_t* src = p.x8.codes + (long long)(from + i) * p.x8.pitch;
-    const uint8_t* scale = p.x8.scales + (long long)(from + i) * p.x8.scale_pitch;
-    const T* line = y_base + (long long)(from - t0 + i) * dy.stride;
-    if (inside) {
-      fetch_x(to, src + x_mine, scale + s_mine, i);
-      to.y[i].load(line);
-    } else {
-      const bool there = from + 8 * tb + i < t1;   // (a token behind the last: zeros)
-      fetch_x(to, there ? src + x_mine : no_numbers, there ? scale + s_mine : no_numbers, i);
-      line = there ? line : reinterpret_cast<const T*>(no_numbers);
-      if (narrow) {
+      const T* const line = static_cast<const T*>(dy.data) + (further * dy.stride + yc) + row * dy.stride;
+      if constexpr (NARROW) {
         to.y[i].load_some(line, p.n - 1);
       } else {
         to.y[i].load(line);
       }
     }
   };
-  // A stage's planes: [32 columns][TS / 16 steps][2 halves of 8 tokens][32 columns, turned by the number of their 16][8 tokens]: the 16 lanes
-  // whose 16 bytes are written, or read, at a time go through all banks.  Two columns of this thread's eight tokens go there in SLICES
-  // pieces.
+  auto clear = [&](tokens& of, int from) {  // what is not this thread's
+    const int skip = from + 8 * tb - back;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const bool keep = i >= skip && i < count;
+#pragma unroll
+      for (int k = 0; k < CW / 4; ++k) of.x[i][k] = keep ? of.x[i][k] : 0u;
+      of.scale[i] = keep ? of.scale[i] : 0u;
+      of.y[i].keep(keep);
+    }
+  };
+  // A stage's planes: [32 columns][TS / 16 steps][2 halves of 8 tokens][32 columns, turned about][8 tokens]: 8 lanes, or 16, whose 16 bytes are
+  // written or read at a time go through all banks.  Two columns of this thread's eight tokens go there in SLICES pieces.
+  constexpr int TURN = CW == 8 ? 6 : 5;
   auto place_of = [&](int column) {
-    const int f = column / 32;
-    return (unsigned)((f * STEPS + tb / 2) * 1024 + (tb & 1) * 512 + ((column % 32) ^ (column >> 4 & 7)) * 16);
+    const int f = column / 32, turn = (column >> 3 & 7) ^ (column >> TURN & 1) * 8;
+    return (unsigned)((f * STEPS + tb / 2) * 1024 + (tb & 1) * 512 + ((column % 32) ^ turn) * 16);
   };
   unsigned x_place[CW], y_place[CW];
 #pragma unroll
@@ -216,16 +218,17 @@ __global__ __launch_bounds__(256, TILE == 256 || PARTS > 1 ? 1 : 2) void qg_fp8_
 #pragma unroll
       for (int e = 0; e < 16; ++e) c[i][j][e] = 0.0f;
   const int wr = wave >> 1, wc = wave & 1;
-  const unsigned operand_at = (unsigned)((lane >> 5) * 512 + ((lane & 31) ^ (lane >> 4 & 1)) * 16);
+  const unsigned operand_at = (unsigned)((lane >> 5) * 512 + ((lane & 31) ^ (lane >> 3 & 3)) * 16);
   auto operand = [&](const uint8_t* plane, int f, int step) {
-    return *reinterpret_cast<const b8*>(plane + (f * STEPS + step) * 1024 + (operand_at ^ (unsigned)((2 * f & 7) * 16)));
+    return *reinterpret_cast<const b8*>(plane + (f * STEPS + step) * 1024 + (operand_at ^ (unsigned)(((4 * f & 7) ^ (32 * f >> TURN & 1) * 8) * 16)));
   };
   if (t0 < t1) {
     // An even number of stages: behind the last token come zeros.  A stage is requested two and a half stages before it is multiplied, and in
     // registers for one and a half of them; the operands of a stage's first products are read behind a barrier in the stage before, where
     // all of it has long been in LDS and nobody waits.
     constexpr int PRODUCTS = GROUPS * PARTS * F, PIECES = PAIRS * SLICES;
-    constexpr int MOVE = PARTS == 1 ? PRODUCTS * 3 / 8 : PRODUCTS / 2, REQUEST = PRODUCTS / 8 < 8 ? PRODUCTS / 4 : 8;
+    // Both spread out: a burst of requests holds the matrix instructions up (4096^3: all within an eighth of the products 149 us, 140 so).
+    constexpr int MOVE = PRODUCTS * 3 / 8, REQUEST = PRODUCTS * 3 / 8;
     constexpr int X_AHEAD = F > 1 ? 1 : 2, X_RING = F > 1 ? 2 : 4;  // steps
     b8 x[X_RING][F], g[3][PARTS];
     auto read_x = [&](const uint8_t* stage, int s, int i) { x[s % X_RING][i] = operand(stage, wr * F + i, s); };
@@ -235,14 +238,15 @@ __global__ __launch_bounds__(256, TILE == 256 || PARTS > 1 ? 1 : 2) void qg_fp8_
     };
     auto fetch_all = [&](tokens& to, int from) {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) fetch(to, from, i, !narrow && from + TS <= t1);
+      for (int i = 0; i < 24; ++i) fetch(to, from, i / 3, i % 3);
+      __builtin_amdgcn_sched_barrier(0);  // (in this order, or the loop waits for more than it needs)
     };
     auto multiply = [&](auto which, tokens& next, int from) {
       constexpr int now = decltype(which)::value, RING0 = now * GROUPS % 3;
       const uint8_t* const stage = lds + now * STAGE;
       uint8_t* const other = lds + (1 - now) * STAGE;
       const int ahead = from + 3 * TS;
-      const bool inside = !narrow && ahead + TS <= t1;
+      if (from + 2 * TS > t1) clear(next, from + TS);
       // The matrix instructions, one by one: first with pieces of the next stage's way to LDS, then with the requests that take its registers
       each<0, PRODUCTS>([&](auto number) {
         constexpr int n = decltype(number)::value, group = n / (PARTS * F), q = n / F % PARTS, i = n % F, s = group / F, j = group % F;
@@ -270,22 +274,17 @@ __global__ __launch_bounds__(256, TILE == 256 || PARTS > 1 ? 1 : 2) void qg_fp8_
             store(next, other, e / SLICES, e % SLICES);
           });
         } else if constexpr (n < MOVE + REQUEST) {
-          constexpr int first = (n - MOVE) * 8 / REQUEST, last = (n - MOVE + 1) * 8 / REQUEST;
-          if (inside) {
-            each<first, last>([&](auto token) { fetch(next, ahead, decltype(token)::value, true); });
-          } else if (ahead >= t1) {
-            each<first, last>([&](auto token) { fetch_none(next, decltype(token)::value); });
-          } else {
-            each<first, last>([&](auto token) { fetch(next, ahead, decltype(token)::value, false); });
-          }
+          constexpr int first = (n - MOVE) * 24 / REQUEST, last = (n - MOVE + 1) * 24 / REQUEST;
+          each<first, last>([&](auto number) { fetch(next, ahead, decltype(number)::value / 3, decltype(number)::value % 3); });
         }
         add_product(c[i][j], g[(RING0 + group) % 3][q], x[s % X_RING][i]);
         __builtin_amdgcn_sched_barrier(0);
       });
     };
-    static_assert(STEPS % X_RING == 0 && (F == 1 || F % 2 == 0) && GROUPS / 2 * PARTS * F >= MOVE, "the next stage is in LDS when it is read");
+    static_assert(STEPS % X_RING == 0 && (F == 1 || F % 2 == 0) && (GROUPS - 2) * PARTS * F >= MOVE && MOVE + REQUEST <= PRODUCTS, "the next stage is in LDS when it is read");
     fetch_all(even, t0);
     fetch_all(odd, t0 + TS);
+    if (t0 + TS > t1) clear(even, t0);
 #pragma unroll
     for (int u = 0; u < PAIRS; ++u)
 #pragma unroll
@@ -387,22 +386,23 @@ __global__ __launch_bounds__(256, TILE == 256 || PARTS > 1 ? 1 : 2) void qg_fp8_
   }
 }
 
-template <int TILE, int TYPE, int PARTS>
+template <int TILE, int TYPE, int PARTS, bool NARROW>
 hipError_t launch(const qg_fp8_gradient_args& a, hipStream_t s) {
   const int rows = (a.k + TILE - 1) / TILE, columns = (a.n + TILE - 1) / TILE * (a.out2.data ? 2 : 1);
   const unsigned per = (unsigned)(((long long)rows * columns + 7) / 8);
-  hipLaunchKernelGGL((qg_fp8_gradient_kernel<TILE, TYPE, PARTS>), dim3(per * 8 * (unsigned)a.slices), dim3(256), 0, s, a, rows, columns);
+  hipLaunchKernelGGL((qg_fp8_gradient_kernel<TILE, TYPE, PARTS, NARROW>), dim3(per * 8 * (unsigned)a.slices), dim3(256), 0, s, a, rows, columns);
   return hipGetLastError();
 }
-template <int TILE>
+template <int TILE, bool NARROW = false>
 hipError_t launch(const qg_fp8_gradient_args& a, hipStream_t s) {
-  return a.dy_type == QG_F32    ? launch<TILE, QG_F32, 3>(a, s)
-         : a.dy_type == QG_BF16 ? launch<TILE, QG_BF16, 1>(a, s)
-                                : launch<TILE, QG_F16, 2>(a, s);
+  return a.dy_type == QG_F32    ? launch<TILE, QG_F32, 3, NARROW>(a, s)
+         : a.dy_type == QG_BF16 ? launch<TILE, QG_BF16, 1, NARROW>(a, s)
+                                : launch<TILE, QG_F16, 2, NARROW>(a, s);
 }
 
 }  // namespace
 
 hipError_t qg_launch_fp8_gradient(const qg_fp8_gradient_args& a, int tile, hipStream_t s) {
+  if (a.n < 8) return launch<64, true>(a, s);
   return tile == 256 ? launch<256>(a, s) : tile == 128 ? launch<128>(a, s) : launch<64>(a, s);
 }
