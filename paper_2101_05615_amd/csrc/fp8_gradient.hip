@@ -119,6 +119,15 @@ __global__ __launch_bounds__(256, TILE == 256 || PARTS > 1 ? 1 : 2) void qg_fp8_
   const qg_fp8_rows &dy = second ? p.dy2 : p.dy, &out = second ? p.out2 : p.out;
   const int t0 = slice * p.slice_tokens, t1 = min(t0 + p.slice_tokens, p.tokens);
 
+  if (t0 >= t1) {  // no tokens at all
+    const float none[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    for (int i = t; i < TILE * TILE / 4; i += 256) {
+      const int row = row_tile * TILE + i / (TILE / 4), column = column_tile * TILE + i % (TILE / 4) * 4;
+      if (row < p.k && column < p.n) put<4>(p.out_type, out, row, column, p.n, none);
+    }
+    return;
+  }
+
   // what this thread fetches: columns c0 .. of both operands, tokens 8 * tb .. of a stage
   constexpr int CHUNKS = TILE / CW;
   const int c0 = t % CHUNKS * CW, tb = t / CHUNKS;
@@ -222,100 +231,97 @@ __global__ __launch_bounds__(256, TILE == 256 || PARTS > 1 ? 1 : 2) void qg_fp8_
   auto operand = [&](const uint8_t* plane, int f, int step) {
     return *reinterpret_cast<const b8*>(plane + (f * STEPS + step) * 1024 + (operand_at ^ (unsigned)(((4 * f & 7) ^ (32 * f >> TURN & 1) * 8) * 16)));
   };
-  if (t0 < t1) {
-    // An even number of stages: behind the last token come zeros.  A stage is requested two and a half stages before it is multiplied, and in
-    // registers for one and a half of them; the operands of a stage's first products are read behind a barrier in the stage before, where
-    // all of it has long been in LDS and nobody waits.
-    constexpr int PRODUCTS = GROUPS * PARTS * F, PIECES = PAIRS * SLICES;
-    // Both spread out: a burst of requests holds the matrix instructions up (4096^3: all within an eighth of the products 149 us, 140 so).
-    constexpr int MOVE = PRODUCTS * 3 / 8, REQUEST = PRODUCTS * 3 / 8;
-    constexpr int X_AHEAD = F > 1 ? 1 : 2, X_RING = F > 1 ? 2 : 4;  // steps
-    b8 x[X_RING][F], g[3][PARTS];
-    auto read_x = [&](const uint8_t* stage, int s, int i) { x[s % X_RING][i] = operand(stage, wr * F + i, s); };
-    auto read_g = [&](const uint8_t* stage, int to, int group) {
+  // An even number of stages: behind the last token come zeros.  A stage is requested two and a half stages before it is multiplied, and in
+  // registers for one and a half of them; the operands of a stage's first products are read behind a barrier in the stage before, where
+  // all of it has long been in LDS and nobody waits.
+  constexpr int PRODUCTS = GROUPS * PARTS * F, PIECES = PAIRS * SLICES;
+  // Both spread out: a burst of requests holds the matrix instructions up (4096^3: all within an eighth of the products 149 us, 140 so).
+  constexpr int MOVE = PRODUCTS * 3 / 8, REQUEST = PRODUCTS * 3 / 8;
+  constexpr int X_AHEAD = F > 1 ? 1 : 2, X_RING = F > 1 ? 2 : 4;  // steps
+  b8 x[X_RING][F], g[3][PARTS];
+  auto read_x = [&](const uint8_t* stage, int s, int i) { x[s % X_RING][i] = operand(stage, wr * F + i, s); };
+  auto read_g = [&](const uint8_t* stage, int to, int group) {
 #pragma unroll
-      for (int q = 0; q < PARTS; ++q) g[to][q] = operand(stage + (1 + q) * PLANE, wc * F + group % F, group / F);
-    };
-    auto fetch_all = [&](tokens& to, int from) {
+    for (int q = 0; q < PARTS; ++q) g[to][q] = operand(stage + (1 + q) * PLANE, wc * F + group % F, group / F);
+  };
+  auto fetch_all = [&](tokens& to, int from) {
 #pragma unroll
-      for (int i = 0; i < 24; ++i) fetch(to, from, i / 3, i % 3);
-      __builtin_amdgcn_sched_barrier(0);  // (in this order, or the loop waits for more than it needs)
-    };
-    auto multiply = [&](auto which, tokens& next, int from) {
-      constexpr int now = decltype(which)::value, RING0 = now * GROUPS % 3;
-      const uint8_t* const stage = lds + now * STAGE;
-      uint8_t* const other = lds + (1 - now) * STAGE;
-      const int ahead = from + 3 * TS;
-      if (from + 2 * TS > t1) clear(next, from + TS);
-      // The matrix instructions, one by one: first with pieces of the next stage's way to LDS, then with the requests that take its registers
-      each<0, PRODUCTS>([&](auto number) {
-        constexpr int n = decltype(number)::value, group = n / (PARTS * F), q = n / F % PARTS, i = n % F, s = group / F, j = group % F;
-        if constexpr (n % (PARTS * F) == 0) {
-          if constexpr (group == GROUPS - 2) {
-            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-            __builtin_amdgcn_s_barrier();
-            asm volatile("" ::: "memory");
-            if constexpr (F > 1) {
+    for (int i = 0; i < 24; ++i) fetch(to, from, i / 3, i % 3);
+    __builtin_amdgcn_sched_barrier(0);  // (in this order, or the loop waits for more than it needs)
+  };
+  auto multiply = [&](auto which, tokens& next, int from) {
+    constexpr int now = decltype(which)::value, RING0 = now * GROUPS % 3;
+    const uint8_t* const stage = lds + now * STAGE;
+    uint8_t* const other = lds + (1 - now) * STAGE;
+    const int ahead = from + 3 * TS;
+    if (from + 2 * TS > t1) clear(next, from + TS);
+    // The matrix instructions, one by one: first with pieces of the next stage's way to LDS, then with the requests that take its registers
+    each<0, PRODUCTS>([&](auto number) {
+      constexpr int n = decltype(number)::value, group = n / (PARTS * F), q = n / F % PARTS, i = n % F, s = group / F, j = group % F;
+      if constexpr (n % (PARTS * F) == 0) {
+        if constexpr (group == GROUPS - 2) {
+          asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+          __builtin_amdgcn_s_barrier();
+          asm volatile("" ::: "memory");
+          if constexpr (F > 1) {
 #pragma unroll
-              for (int k = 0; k < F; ++k) read_x(other, 0, k);
-            }
-          }
-          if constexpr (F == 1) read_x(s + 2 < STEPS ? stage : other, (s + 2) % STEPS, 0);
-          if constexpr (group + 2 < GROUPS) read_g(stage, (RING0 + group + 2) % 3, group + 2);
-          if constexpr (group + 2 >= GROUPS) read_g(other, (RING0 + group + 2) % 3, group + 2 - GROUPS);
-          if constexpr (F > 1 && s + 1 < STEPS && j < 2) {  // the next step's rows
-#pragma unroll
-            for (int k = 0; k < F / 2; ++k) read_x(stage, s + 1, j * (F / 2) + k);
+            for (int k = 0; k < F; ++k) read_x(other, 0, k);
           }
         }
-        if constexpr (n < MOVE) {
-          each<n * PIECES / MOVE, (n + 1) * PIECES / MOVE>([&](auto piece) {
-            constexpr int e = decltype(piece)::value;
-            store(next, other, e / SLICES, e % SLICES);
-          });
-        } else if constexpr (n < MOVE + REQUEST) {
-          constexpr int first = (n - MOVE) * 24 / REQUEST, last = (n - MOVE + 1) * 24 / REQUEST;
-          each<first, last>([&](auto number) { fetch(next, ahead, decltype(number)::value / 3, decltype(number)::value % 3); });
+        if constexpr (F == 1) read_x(s + 2 < STEPS ? stage : other, (s + 2) % STEPS, 0);
+        if constexpr (group + 2 < GROUPS) read_g(stage, (RING0 + group + 2) % 3, group + 2);
+        if constexpr (group + 2 >= GROUPS) read_g(other, (RING0 + group + 2) % 3, group + 2 - GROUPS);
+        if constexpr (F > 1 && s + 1 < STEPS && j < 2) {  // the next step's rows
+#pragma unroll
+          for (int k = 0; k < F / 2; ++k) read_x(stage, s + 1, j * (F / 2) + k);
         }
-        add_product(c[i][j], g[(RING0 + group) % 3][q], x[s % X_RING][i]);
-        __builtin_amdgcn_sched_barrier(0);
-      });
-    };
-    static_assert(STEPS % X_RING == 0 && (F == 1 || F % 2 == 0) && (GROUPS - 2) * PARTS * F >= MOVE && MOVE + REQUEST <= PRODUCTS, "the next stage is in LDS when it is read");
-    fetch_all(even, t0);
-    fetch_all(odd, t0 + TS);
-    if (t0 + TS > t1) clear(even, t0);
-#pragma unroll
-    for (int u = 0; u < PAIRS; ++u)
-#pragma unroll
-      for (int e = 0; e < SLICES; ++e) store(even, lds, u, e);
-    fetch_all(even, t0 + 2 * TS);
-    __syncthreads();
-#pragma unroll
-    for (int k = 0; k < F * X_AHEAD; ++k) read_x(lds, k / F, k % F);
-    read_g(lds, 0, 0);
-    read_g(lds, 1, 1);
-#pragma unroll 1
-    for (int from = t0; from < t1; from += 2 * TS) {
-      multiply(std::integral_constant<int, 0>(), odd, from);
-      multiply(std::integral_constant<int, 1>(), even, from + TS);
-      if constexpr (2 * GROUPS % 3 != 0) {  // the ring starts at 0 again
-        constexpr int at = 2 * GROUPS % 3;
-        b8 t[2][PARTS];
-#pragma unroll
-        for (int k = 0; k < 2; ++k)
-#pragma unroll
-          for (int q = 0; q < PARTS; ++q) t[k][q] = g[(at + k) % 3][q];
-#pragma unroll
-        for (int k = 0; k < 2; ++k)
-#pragma unroll
-          for (int q = 0; q < PARTS; ++q) g[k][q] = t[k][q];
       }
+      if constexpr (n < MOVE) {
+        each<n * PIECES / MOVE, (n + 1) * PIECES / MOVE>([&](auto piece) {
+          constexpr int e = decltype(piece)::value;
+          store(next, other, e / SLICES, e % SLICES);
+        });
+      } else if constexpr (n < MOVE + REQUEST) {
+        constexpr int first = (n - MOVE) * 24 / REQUEST, last = (n - MOVE + 1) * 24 / REQUEST;
+        each<first, last>([&](auto number) { fetch(next, ahead, decltype(number)::value / 3, decltype(number)::value % 3); });
+      }
+      add_product(c[i][j], g[(RING0 + group) % 3][q], x[s % X_RING][i]);
+      __builtin_amdgcn_sched_barrier(0);
+    });
+  };
+  static_assert(STEPS % X_RING == 0 && (F == 1 || F % 2 == 0) && (GROUPS - 2) * PARTS * F >= MOVE && MOVE + REQUEST <= PRODUCTS, "the next stage is in LDS when it is read");
+  fetch_all(even, t0);
+  fetch_all(odd, t0 + TS);
+  if (t0 + TS > t1) clear(even, t0);
+#pragma unroll
+  for (int u = 0; u < PAIRS; ++u)
+#pragma unroll
+    for (int e = 0; e < SLICES; ++e) store(even, lds, u, e);
+  fetch_all(even, t0 + 2 * TS);
+  __syncthreads();
+#pragma unroll
+  for (int k = 0; k < F * X_AHEAD; ++k) read_x(lds, k / F, k % F);
+  read_g(lds, 0, 0);
+  read_g(lds, 1, 1);
+#pragma unroll 1
+  for (int from = t0; from < t1; from += 2 * TS) {
+    multiply(std::integral_constant<int, 0>(), odd, from);
+    multiply(std::integral_constant<int, 1>(), even, from + TS);
+    if constexpr (2 * GROUPS % 3 != 0) {  // the ring starts at 0 again
+      constexpr int at = 2 * GROUPS % 3;
+      b8 t[2][PARTS];
+#pragma unroll
+      for (int k = 0; k < 2; ++k)
+#pragma unroll
+        for (int q = 0; q < PARTS; ++q) t[k][q] = g[(at + k) % 3][q];
+#pragma unroll
+      for (int k = 0; k < 2; ++k)
+#pragma unroll
+        for (int q = 0; q < PARTS; ++q) g[k][q] = t[k][q];
     }
-    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-    __syncthreads();   // (nobody reads what the end writes over)
   }
-  asm volatile("s_nop 15\n\ts_nop 15" ::: "memory");
+  // (before anything reads or moves the sums: the compiler does not know that they are being written)
+  asm volatile("s_waitcnt lgkmcnt(0)\n\ts_nop 15\n\ts_nop 15" ::: "memory");
 #pragma unroll
   for (int i = 0; i < F; ++i)
 #pragma unroll

@@ -399,7 +399,15 @@ __device__ inline void add_products(f4 (&c)[4], const wide (&a)[4], const wide& 
       }
     }
 }
-__device__ inline void products_done() { asm volatile("s_nop 15\n\ts_nop 15" ::: "memory"); }
+// Wherever accumulators may change registers, that is behind a loop and at its start: the compiler does not know that they are being written.
+template <typename C, int M, int N>
+__device__ inline void products_done(C (&c)[M][N]) {
+  asm volatile("s_nop 15\n\ts_nop 15" ::: "memory");
+#pragma unroll
+  for (int i = 0; i < M; ++i)
+#pragma unroll
+    for (int j = 0; j < N; ++j) asm volatile("" : "+a"(c[i][j]));
+}
 
 // One block of K a turn, in both kernels.  The weights are requested two turns before their own, and the compiler's wait for them at its
 // start -- no more than the loads of the turn between may still be on their way -- takes the rows in that were requested in front of those.  The
@@ -506,6 +514,7 @@ __global__ __launch_bounds__(256, 1) void qg_fp8_tile_kernel(qg_fp8_product_args
 #pragma unroll 1
   for (int rest = (k1 - k0) % 3; rest > 0; --rest) {  // turns that do not make three: what is on its way is waited for, and moves on
     turn(w0, w2);
+    products_done(acc.c);
     w0 = w1;
     w1 = w2;
   }
@@ -516,11 +525,7 @@ __global__ __launch_bounds__(256, 1) void qg_fp8_tile_kernel(qg_fp8_product_args
     turn(w2, w1);
   }
   asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");   // (what was requested past the end)
-  products_done();
-#pragma unroll
-  for (int i = 0; i < MF; ++i)
-#pragma unroll
-    for (int j = 0; j < 4; ++j) asm volatile("" : "+a"(acc.c[i][j]));
+  products_done(acc.c);
 
   if (p.slices > 1) {  // sums of the slices through memory, past the L2s that the XCDs do not share; the last one to arrive adds them in order
     const int tile = at.row_tile * column_tiles + at.column_tile;
@@ -663,6 +668,7 @@ __global__ __launch_bounds__(256, 1) void qg_fp8_tile256_kernel(qg_fp8_product_a
 #pragma unroll 1
   for (int rest = kbs % 3; rest > 0; --rest) {  // turns that do not make three: what is on its way is waited for, and moves on
     turn(std::integral_constant<int, 0>(), w0, w2);
+    products_done(acc.c);
     w0 = w1;
     w1 = w2;
     const u4 t[2][2] = {{x[2][0][0], x[2][0][1]}, {x[2][1][0], x[2][1][1]}};
@@ -681,9 +687,7 @@ __global__ __launch_bounds__(256, 1) void qg_fp8_tile256_kernel(qg_fp8_product_a
     turn(std::integral_constant<int, 2>(), w2, w1);
   }
   asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");   // (what was requested past the end)
-  products_done();
-#pragma unroll
-  for (int i = 0; i < 8; ++i) asm volatile("" : "+a"(acc.c[i][0]), "+a"(acc.c[i][1]));
+  products_done(acc.c);
   finish<A, END>(p, acc, at, wave, lane, lds);
 }
 

@@ -627,6 +627,30 @@ def test_matmul_large_tiles(env, T, K, N):
     assert torch.equal(y.double(), x.double() @ b.double())
 
 
+@pytest.mark.parametrize("T,N", [(1025, 300), (2100, 1900)])                  # tiles of 64 rows, of 128
+@pytest.mark.parametrize("K", [128, 250, 384, 500, 640, 2300])                # one block to five, and enough to be dealt over workgroups
+def test_matmul_small_tiles(env, T, K, N):
+    fp8, torch, dev = env
+    rng = np.random.default_rng(T + K)
+    say(f"small tiles {T} x {K} x {N}")
+    x, b = tensor(torch, dev, inputs(rng, T, K), "bfloat16"), tensor(torch, dev, weights(rng, K, N), "bfloat16")
+    bias = torch.randn(N, device=dev)
+    w, ws, x8, b8 = fp8.pack(b), fp8.workspace(dev), ref.held(f64(x)), ref.held_weight(f64(b))
+    want, mass = big64(torch, dev, x8, b8) + f64(bias), big64(torch, dev, np.abs(x8), np.abs(b8)) + np.abs(f64(bias))
+    whole = torch.randint(-2, 3, (T, K), device=dev).to(torch.bfloat16)         # sums that stay exact either way
+    whole_b = torch.randint(-2, 3, (K, N), device=dev).to(torch.bfloat16)
+    whole_w = fp8.pack(whole_b)
+    for wide in (False, True):
+        for workspace in (None, ws):
+            for dtype in DTYPES:
+                bound = ref.sum_bound(mass, K, wide)
+                y = fp8.matmul(x, w, bias=bias, dtype=getattr(torch, dtype), workspace=workspace, wide_sums=wide)
+                compare(f64(y), want, bound + ref.rounding(np.abs(want) + bound, dtype), f"{dtype} wide {wide} workspace {workspace is not None}")
+            y = fp8.matmul(whole, whole_w, dtype=torch.float32, workspace=workspace, wide_sums=wide)
+            assert torch.equal(y.double(), whole.double() @ whole_b.double()), f"wide {wide} workspace {workspace is not None}"
+    assert (ws[:fp8.COUNTER_BYTES] == 0).all()
+
+
 @pytest.mark.parametrize("T,K,F", [(2500, 300, 2700), (2561, 140, 2561)])
 @pytest.mark.parametrize("act", ["silu", "relu"])
 def test_gated_large_tiles(env, T, K, F, act):
