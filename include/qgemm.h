@@ -725,7 +725,8 @@ int qg_fp8_gated(const qg_fp8_weight* w, const qg_fp8_product* p, const qg_fp8_b
  * dgu: bf16 [tokens][2][n rounded up to 128], contiguous, 16-byte aligned: dg and du, 0
  * behind the last column, for the weights' gradients; dgu_held: the 8-bit form of
  * their fp32 values, 2 * (n rounded up to 128) channels, for the gradient of x; held:
- * that of h, as qg_fp8_gated writes it.  p: x, tokens, activation and workspace are used.  n >= 8 (QG_EUNSUPPORTED otherwise). */
+ * that of h, as qg_fp8_gated writes it.  p: x, tokens, activation and
+ * workspace are used.  n >= 8, wide_sums 0 (QG_EUNSUPPORTED otherwise). */
 int qg_fp8_gated_backward(const qg_fp8_weight* w, const qg_fp8_product* p, const qg_rows* dh, int dh_dtype, void* dgu,
                           const qg_fp8_blocks* dgu_held, const qg_fp8_blocks* held, void* stream);
 

@@ -11,7 +11,9 @@
 #include <ATen/core/Tensor.h>
 #include <ATen/core/grad_mode.h>
 #include <ATen/ops/empty.h>
+#include <torch/csrc/autograd/function.h>
 #include <torch/csrc/autograd/python_variable.h>
+#include <torch/csrc/autograd/variable.h>
 
 #include <limits.h>
 #include <math.h>
@@ -565,6 +567,21 @@ PyObject* pair_of(const at::Tensor& a, const at::Tensor* b) {  // (a, b or None)
   return both;
 }
 
+// (leaf, number of the current stream): whether a live autograd graph holds the leaf whose work was issued on another stream.  A backward pass
+// that is being captured would make that stream wait for the captured one, which ends the process.
+PyObject* held_elsewhere(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  if (n != 2) Py_RETURN_FALSE;
+  QG_OR_SLOW(
+    const at::Tensor* const t = tensor(a[0]);
+    const long long id = PyLong_AsLongLong(a[1]);
+    if (PyErr_Occurred()) return nullptr;
+    if (!t || !t->is_cuda() || !t->is_leaf() || !t->requires_grad()) Py_RETURN_FALSE;
+    const auto node = torch::autograd::impl::try_get_grad_accumulator(*t);
+    if (!node) Py_RETURN_FALSE;
+    const auto stream = node->stream();
+    return PyBool_FromLong(stream.has_value() && stream->id() != id);)
+}
+
 // (x) -> (codes, scales)
 PyObject* fp8_quantize(PyObject*, PyObject* const* a, Py_ssize_t n) {
   if (n != 1) Py_RETURN_NONE;
@@ -709,10 +726,10 @@ PyObject* fp8_gated(PyObject*, PyObject* const* a, Py_ssize_t n) {
     return held ? pair_of(to.codes, &to.scales) : result.give();)
 }
 
-// (x or blocks, w_in, w_out, activation, element type or None, out or None, workspace or None): gated() and matmul() of what it gives, in
-// fp32 up to 4 * QG_FP8_FEW tokens, else in 8 bits
+// (x or blocks, w_in, w_out, activation, element type or None, out or None, workspace or None, wide sums or None: for fp32 results):
+// gated() and matmul() of what it gives, in fp32 up to 4 * QG_FP8_FEW tokens, else in 8 bits
 PyObject* fp8_feed_forward(PyObject*, PyObject* const* a, Py_ssize_t n) {
-  if (n != 7) Py_RETURN_NONE;
+  if (n != 8) Py_RETURN_NONE;
   QG_OR_SLOW(
     activations x;
     activations h = {};
@@ -731,6 +748,8 @@ PyObject* fp8_feed_forward(PyObject*, PyObject* const* a, Py_ssize_t n) {
     q.workspace = p.workspace;
     q.workspace_bytes = p.workspace_bytes;
     q.wide_sums = q.dtype == QG_F32;
+    if (a[7] != Py_None && !truth(a[7], &q.wide_sums)) Py_RETURN_NONE;
+    p.wide_sums = q.wide_sums;
     const bool few = x.tokens <= 4 * QG_FP8_FEW;
     at::Tensor middle;
     h.options = x.options;
@@ -889,6 +908,7 @@ PyMethodDef methods[] = {
     {"kv4_append", QG_FAST(kv4_append), METH_FASTCALL, nullptr},
     {"kv4_attention", QG_FAST(kv4_attention), METH_FASTCALL, nullptr},
     {"kv4_read", QG_FAST(kv4_read), METH_FASTCALL, nullptr},
+    {"held_elsewhere", QG_FAST(held_elsewhere), METH_FASTCALL, nullptr},
     {"fp8_quantize", QG_FAST(fp8_quantize), METH_FASTCALL, nullptr},
     {"fp8_dequantize", QG_FAST(fp8_dequantize), METH_FASTCALL, nullptr},
     {"fp8_pack", QG_FAST(fp8_pack), METH_FASTCALL, nullptr},

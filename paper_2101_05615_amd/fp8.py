@@ -303,17 +303,18 @@ def gated(x, w, activation="silu", dtype=None, out=None, workspace=None, wide_su
     return out
 
 
-def _gated8(x, w, activation, workspace):
-    done = _binding.fp8_gated(x, w, ACTIVATIONS[activation], -2, None, workspace, None)
+def _gated8(x, w, activation, workspace, wide_sums):
+    done = _binding.fp8_gated(x, w, ACTIVATIONS[activation], -2, None, workspace, wide_sums)
     if done is not None:
         return _blocks(done, w.n)
-    return gated(x, w, activation, out=new_blocks(x.shape[0], w.n, x.device), workspace=workspace)
+    return gated(x, w, activation, out=new_blocks(x.shape[0], w.n, x.device), workspace=workspace, wide_sums=wide_sums)
 
 
 def gated_backward(x, w, dh, activation="silu", workspace=None):
     """The backward pass of gated() from x in 8 bits (Blocks) and the gradient dh [tokens, inner] of its result: (dgu, dgu8, h8).  dgu
     bfloat16 [tokens, 2, inner rounded up to 128] holds the gradients of x Gate and of x Up, dgu8 their 8-bit form (Blocks
-    [tokens, 2 * inner rounded up to 128], for matmul() with w.transposed: the gradient of x), h8 the block's result in 8 bits."""
+    [tokens, 2 * inner rounded up to 128], for matmul() with w.transposed: the gradient of x), h8 the block's result in 8 bits.
+    Sums are those of the 8-bit matrix cores."""
     _no_gradient("gated_backward", dh)
     assert w.gated and isinstance(x, Blocks)
     T, inner = x.shape[0], _up(w.n, BLOCK)
@@ -361,11 +362,13 @@ def weight_gradient(x, dy, dtype=None, out=None, workspace=None):
     return tuple(done) if pair else done[0]
 
 
-def feed_forward(x, w_in, w_out, activation="silu", dtype=None, out=None, workspace=None):
+def feed_forward(x, w_in, w_out, activation="silu", dtype=None, out=None, workspace=None, wide_sums=None):
     """(activation(x Gate) * (x Up)) Down: w_in from pack_gated(), w_out from pack().  What is between goes into the second product in 8
-    bits, made from its fp32 value."""
+    bits, made from its fp32 value.  wide_sums: of both products, as in matmul().  (A sum that is 2e-5 off now and then goes to the next
+    of the 8-bit numbers, which leaves 2e-3 in the result: a tenth of what the 8 bits in between are off themselves.)"""
     if activation in ACTIVATIONS:
-        done = _binding.fp8_feed_forward(x, w_in, w_out, ACTIVATIONS[activation], None if dtype is None else _TYPES.get(dtype, -1), out, workspace)
+        done = _binding.fp8_feed_forward(x, w_in, w_out, ACTIVATIONS[activation], None if dtype is None else _TYPES.get(dtype, -1), out, workspace,
+                                         wide_sums)
         if done is not None:
             return done
     _no_gradient("feed_forward", x, out)
@@ -374,12 +377,20 @@ def feed_forward(x, w_in, w_out, activation="silu", dtype=None, out=None, worksp
     if x.shape[0] <= 4 * FEW:
         h = gated(x, w_in, activation, dtype=torch.float32, workspace=workspace)
     else:
-        h = _gated8(x, w_in, activation, workspace)
-    return matmul(h, w_out, out=out, workspace=workspace)
+        h = _gated8(x, w_in, activation, workspace, out.dtype == torch.float32 if wide_sums is None else wide_sums)
+    return matmul(h, w_out, out=out, workspace=workspace, wide_sums=wide_sums)
 
 
 def _unit(g):
     return g if g.stride(1) == 1 or g.shape[1] <= 1 else g.contiguous()          # (of a sum, say: one number with strides of 0)
+
+
+def _check_capture(name, *leaves):
+    if leaves[0].is_cuda and torch._C._cuda_isCurrentStreamCapturing():
+        stream = torch._C._cuda_getCurrentStream(leaves[0].device.index)[0]
+        if any(_binding.held_elsewhere(t, stream) for t in leaves):
+            raise RuntimeError(f"fp8.{name}: a graph is being captured while a result from outside it holds one of these leaves for its own "
+                               "backward pass; give that up first, or detach")
 
 
 class _Linear(torch.autograd.Function):
@@ -405,6 +416,7 @@ def linear(x, b, workspace=None):
     weights' transpose in 8 bits."""
     _check_rows(x)
     assert b.dim() == 2 and b.shape[0] == x.shape[1]
+    _check_capture("linear", x, b)
     return _Linear.apply(x, b, workspace)
 
 
@@ -414,7 +426,7 @@ class _GatedMlp(torch.autograd.Function):
         back = any(ctx.needs_input_grad)
         w_in, w_out = pack_gated(gate, up, transposed=ctx.needs_input_grad[0]), pack(down, transposed=back)
         x8 = quantize(x)
-        h8 = _gated8(x8, w_in, activation, ws)
+        h8 = _gated8(x8, w_in, activation, ws, False)
         if back:
             ctx.x8, ctx.w_in, ctx.w_out = x8, w_in, w_out.transposed
         ctx.activation, ctx.ws, ctx.types = activation, ws, (x.dtype, gate.dtype, down.dtype)
@@ -442,8 +454,10 @@ class _GatedMlp(torch.autograd.Function):
 
 def gated_mlp(x, gate, up, down, activation="silu", workspace=None):
     """(activation(x Gate) * (x Up)) Down, differentiable in x and in the weights gate, up [in, inner] and down [inner, out], which are put
-    into 8 bits here.  Kept for the backward pass: x and the weights in 8 bits; the rest is computed again."""
+    into 8 bits here.  Kept for the backward pass: x and the weights in 8 bits; the rest is computed again, with the same sums of the
+    8-bit matrix cores."""
     _check_rows(x)
     assert gate.dim() == 2 and gate.shape[0] == x.shape[1] and up.shape == gate.shape and down.dim() == 2 and down.shape[0] == gate.shape[1]
     assert activation in ACTIVATIONS
+    _check_capture("gated_mlp", x, gate, up, down)
     return _GatedMlp.apply(x, gate, up, down, activation, workspace)

@@ -142,6 +142,7 @@ def test_gated_backward_refusals(fp8):
     assert call(both=blocks(fp8, 40, 400)) == EINVAL and call(held=blocks(fp8, 40, 256)) == EINVAL
     raw = dict(x=fp8._BlocksDesc(None, None, 0, 0), x_rows=fp8._Rows(FAKE, 300), tokens=3, both=blocks(fp8, 3, 512), held=blocks(fp8, 3, 200))
     assert call(**raw) == EUNSUPPORTED
+    assert call(wide_sums=1) == EUNSUPPORTED
     assert call(w=weight(fp8, 300, 7, 1), held=blocks(fp8, 40, 7), both=blocks(fp8, 40, 256)) == EUNSUPPORTED   # fewer than 8 columns
     wide = (1 << 20) - 100
     assert call(w=weight(fp8, 300, wide, 1)) == EINVAL                            # the pair's gradient would have too many channels

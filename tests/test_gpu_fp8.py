@@ -366,12 +366,17 @@ def test_feed_forward(env, T, dtype):
     ws = fp8.workspace(dev)
     y = fp8.feed_forward(x, fp8.pack_gated(gate, up), fp8.pack(down), workspace=ws)
     x8, g8, u8, d8 = ref.held(f64(x)), *(ref.held_weight(f64(b)) for b in (gate, up, down))
-    wide = T <= 64
+    wide = T <= 64 or dtype == "float32"
     h, h_err = gated_reference("silu", x8 @ g8, x8 @ u8, *(ref.sum_bound(np.abs(x8) @ np.abs(b), K, wide) for b in (g8, u8)))
     h8, h8_err = ref.held(h), ref.held_bound(h, h_err)
     want = h8 @ d8
     bound = h8_err @ np.abs(d8) + ref.sum_bound((np.abs(h8) + h8_err) @ np.abs(d8), F, wide or dtype == "float32")
     compare(f64(y), want, bound + ref.rounding(np.abs(want) + bound, dtype), "feed forward")
+    h, h_err = gated_reference("silu", x8 @ g8, x8 @ u8, *(ref.sum_bound(np.abs(x8) @ np.abs(b), K, True) for b in (g8, u8)))
+    h8, h8_err = ref.held(h), ref.held_bound(h, h_err)
+    bound = h8_err @ np.abs(d8) + ref.sum_bound((np.abs(h8) + h8_err) @ np.abs(d8), F, True)
+    y = fp8.feed_forward(x, fp8.pack_gated(gate, up), fp8.pack(down), workspace=ws, wide_sums=True)
+    compare(f64(y), h8 @ d8, bound + ref.rounding(np.abs(h8 @ d8) + bound, dtype), "wide sums")
 
 
 @pytest.mark.parametrize("T", [1, 5, 70, 300])

@@ -1,0 +1,173 @@
+"""Every kernel of the 8-bit floats is the one that runs where its rule says, and gives whole numbers exactly at sizes drawn over its range; the
+operators as a program uses them together."""
+import random
+
+import pytest
+
+from gpu_util import kernels_of, say
+from test_gpu_fp8 import env  # noqa: F401
+
+pytestmark = pytest.mark.gpu
+
+
+def whole(torch, dev, *shape, top=2, dtype="bfloat16"):
+    return torch.randint(-top, top + 1, shape, device=dev).to(getattr(torch, dtype))
+
+
+# tokens, k, n, 8-bit sums wanted -> name
+@pytest.mark.parametrize("T,K,N,wide,name", [
+    (1, 4096, 4096, True, "qg_fp8_stream_kernelILi1ELi2E"), (16, 1024, 8192, True, "qg_fp8_stream_kernelILi1ELi4ELi4E"),
+    (9, 10240, 4096, True, "qg_fp8_stream_kernelILi1ELi4ELi4E"), (3, 10240, 4096, True, "qg_fp8_stream_kernelILi1ELi4ELi8E"),
+    (40, 640, 512, True, "qg_fp8_stream_kernelILi2ELi2ELi8E"), (200, 2740, 4100, True, "qg_fp8_stream_kernelILi2ELi4ELi8E"),
+    (1025, 512, 256, False, "qg_fp8_tile_kernelILi4ELi0ELb0E"), (1025, 512, 256, True, "qg_fp8_tile_kernelILi4ELi0ELb1E"),
+    (1100, 384, 8192, False, "qg_fp8_tile_kernelILi8ELi0ELb0E"), (1100, 384, 8192, True, "qg_fp8_tile_kernelILi8ELi0ELb1E"),
+    (2049, 256, 8192, False, "qg_fp8_tile256_kernelILi0E")])
+def test_product_forms(env, T, K, N, wide, name):  # noqa: F811
+    fp8, torch, dev = env
+    x, b = whole(torch, dev, T, K), whole(torch, dev, K, N)
+    w, xq, ws = fp8.pack(b), fp8.quantize(x), fp8.workspace(dev)
+    out = torch.empty(T, N, device=dev)
+    call = lambda: fp8.matmul(xq, w, out=out, workspace=ws, wide_sums=wide)  # noqa: E731
+    names = kernels_of(call)
+    assert len(names) == 1 and name in names[0], names
+    call()
+    assert torch.equal(out.double(), x.double() @ b.double())
+
+
+@pytest.mark.parametrize("T,K,N,dtype,name", [
+    (300, 512, 512, "float32", "qg_fp8_gradient_kernelILi64ELi0ELi3ELb0E"), (300, 512, 512, "bfloat16", "qg_fp8_gradient_kernelILi64ELi1ELi1ELb0E"),
+    (300, 512, 5, "float16", "qg_fp8_gradient_kernelILi64ELi2ELi2ELb1E"), (5000, 256, 300, "bfloat16", "qg_fp8_gradient_kernelILi64ELi1ELi1ELb0E"),
+    (5000, 1200, 1300, "float16", "qg_fp8_gradient_kernelILi128ELi2ELi2ELb0E"), (130, 1200, 1300, "float32", "qg_fp8_gradient_kernelILi128ELi0ELi3ELb0E"),
+    (130, 3700, 3500, "bfloat16", "qg_fp8_gradient_kernelILi256ELi1ELi1ELb0E")])
+@pytest.mark.parametrize("pair", [False, True])
+def test_gradient_forms(env, T, K, N, dtype, name, pair):  # noqa: F811
+    fp8, torch, dev = env
+    if pair and K == 3700:
+        N = 1750
+    x, dy = whole(torch, dev, T, K), [whole(torch, dev, T, N, dtype=dtype) for _ in range(1 + pair)]
+    xq, ws = fp8.quantize(x), fp8.workspace(dev)
+    outs = [torch.empty(K, N, device=dev) for _ in dy]
+    call = lambda: fp8.weight_gradient(xq, dy if pair else dy[0], out=outs if pair else outs[0], workspace=ws)  # noqa: E731
+    names = kernels_of(call)
+    assert len(names) == 1 and name in names[0], names
+    for _ in range(2):
+        call()
+        for o, d in zip(outs, dy):
+            assert torch.equal(o.double(), x.double().t() @ d.double())
+    assert not ws[:fp8.COUNTER_BYTES].any()
+
+
+@pytest.mark.parametrize("seed", range(24))
+def test_drawn_sizes(env, seed):  # noqa: F811
+    """Whole numbers whose sums any order keeps exact, with views of wider rows, and each gradient."""
+    fp8, torch, dev = env
+    r = random.Random(seed)
+    draw = lambda a, b: int(round(a * (b / a) ** r.random()))  # noqa: E731
+    T, K, N = draw(1, 3000), draw(8, 3000), draw(1, 4000)
+    dtype = r.choice(["float32", "bfloat16", "float16"])
+    say(f"drawn {T} x {K} x {N} {dtype}")
+    torch.manual_seed(seed)
+    ws = fp8.workspace(dev)
+    x = whole(torch, dev, T, K + 3, dtype=dtype)[:, 2:2 + K].requires_grad_()
+    b, dy = whole(torch, dev, N, K).float().t().requires_grad_(), whole(torch, dev, T, N + 1, dtype="float32")[:, :N]
+    y = fp8.linear(x.float(), b, workspace=ws)
+    assert torch.equal(y.double(), x.double() @ b.double())
+    dx, db = torch.autograd.grad(y, (x, b), dy)
+    assert torch.equal(dx.double(), (dy.double() @ b.double().t()).to(dx.dtype).double())
+    assert torch.equal(db.double(), x.double().t() @ dy.double())
+    with torch.no_grad():
+        gate, up = whole(torch, dev, K, N, top=1), whole(torch, dev, K, N, top=1)
+        w = fp8.pack_gated(gate, up)
+        for wide in (None, False):
+            h = fp8.gated(x.detach(), w, "relu", dtype=torch.float32, workspace=ws, wide_sums=wide)
+            want = (x.double() @ gate.double()).clamp(min=0) * (x.double() @ up.double())
+            assert float(want.abs().max()) < 2 ** 24 and torch.equal(h.double(), want)
+    assert not ws[:fp8.COUNTER_BYTES].any()
+
+
+def test_two_graphs_and_two_streams(env):  # noqa: F811
+    """Two captured calls on workspaces of their own, replayed at the same time on two streams, several times with eager work between."""
+    fp8, torch, dev = env
+    x, b = whole(torch, dev, 5, 8192), whole(torch, dev, 8192, 700)
+    w, streams = fp8.pack(b), [torch.cuda.Stream() for _ in range(2)]
+    want = x.float() @ b.float()
+    graphs, outs, spaces = [], [], [fp8.workspace(dev) for _ in range(2)]
+    for s, ws in zip(streams, spaces):
+        s.wait_stream(torch.cuda.current_stream())
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=s):
+            outs.append([fp8.matmul(x, w, dtype=torch.float32, workspace=ws) for _ in range(8)])
+        graphs.append(g)
+    for turn in range(4):
+        for o in outs[0] + outs[1]:
+            o.zero_()
+        for s, g in zip(streams, graphs):
+            s.wait_stream(torch.cuda.current_stream())
+            with torch.cuda.stream(s):
+                g.replay()
+        for s in streams:
+            torch.cuda.current_stream().wait_stream(s)
+        eager = fp8.matmul(x, w, dtype=torch.float32)
+        assert torch.equal(eager, want) and all(torch.equal(o, want) for o in outs[0] + outs[1]), turn
+
+
+def test_captured_beside_a_live_graph(env):  # noqa: F811
+    """Leaves that a result from outside holds: refused while a graph is captured, right once it is given up."""
+    fp8, torch, dev = env
+    x, b = whole(torch, dev, 70, 256).float().requires_grad_(), whole(torch, dev, 256, 128).float().requires_grad_()
+    dy, ws = whole(torch, dev, 70, 128).float(), fp8.workspace(dev)
+    mats = [whole(torch, dev, *s).float().requires_grad_() for s in ((256, 128), (256, 128), (128, 128))]
+    held = fp8.linear(x, b, workspace=ws)
+    with torch.no_grad():
+        fp8.linear(x, b, workspace=ws)                                         # (what has no backward pass holds nothing)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        for call in (lambda: fp8.linear(x, b, workspace=ws), lambda: fp8.gated_mlp(x, *mats, workspace=ws)):
+            with pytest.raises(RuntimeError, match="leaves"):
+                call()
+        apart = x.detach().requires_grad_()
+        y = fp8.linear(apart, b.detach(), workspace=ws)
+        dx, = torch.autograd.grad(y, apart, dy)
+    g.replay()
+    want = torch.autograd.grad(held, x, dy)[0]
+    assert torch.equal(dx, want) and torch.equal(y, held)
+    del held, y
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        dx, db = torch.autograd.grad(fp8.linear(x, b, workspace=ws), (x, b), dy)
+    g.replay()
+    assert torch.equal(dx, want) and torch.equal(db.double(), x.double().t() @ dy.double())
+
+
+def test_a_decoder_step(env):  # noqa: F811
+    """Projections in 8 bits around the 4-bit cache's attention, then the feed-forward block, of one new token per sequence: against the same
+    steps in 64 bits from the values that each one has in hand."""
+    fp8, torch, dev = env
+    from paper_2101_05615_amd import kv4
+    torch.manual_seed(3)
+    B, D, H, d, F = 3, 512, 4, 128, 1000
+    x = torch.randn(B, D, device=dev).to(torch.bfloat16)
+    mats = [torch.randn(*s, device=dev).mul_(s[0] ** -0.5).to(torch.bfloat16) for s in ((D, D), (D, D), (D, D), (D, D), (D, F), (D, F), (F, D))]
+    wq, wk, wv, wo, wd = (fp8.pack(mats[i]) for i in (0, 1, 2, 3, 6))
+    w_in, ws = fp8.pack_gated(mats[4], mats[5]), fp8.workspace(dev)
+    cache = kv4.new_cache(B, H, d, 32, device=dev)
+    q, k, v = (fp8.matmul(x, w, workspace=ws).view(B, H, d) for w in (wq, wk, wv))
+    held = lambda t: fp8.dequantize(fp8.quantize(t)).double()  # noqa: E731
+    values = lambda w, n: fp8.matmul(torch.eye(n, device=dev), w, dtype=torch.float32).double()  # noqa: E731
+    for t, w in ((q, wq), (k, wk), (v, wv)):
+        want = held(x) @ values(w, D)
+        assert (t.reshape(B, D).double() - want).abs().max() <= 2 ** -8 * want.abs().max() * 1.01
+    slots = torch.arange(B, device=dev, dtype=torch.int64) * 32
+    kv4.append(cache, k, v, slots)
+    pages, lens = torch.arange(B, device=dev, dtype=torch.int32).view(B, 1), torch.ones(B, dtype=torch.int32, device=dev)
+    a = kv4.attention(q, cache, pages, lens)
+    assert (a.double() - kv4.read(cache, slots)[1].double()).abs().max() <= 2 ** -7 * v.double().abs().max()   # one token: its value
+    o = fp8.matmul(a.reshape(B, D), wo, workspace=ws)
+    want = held(a.reshape(B, D)) @ values(wo, D)
+    assert (o.double() - want).abs().max() <= 2 ** -8 * want.abs().max() * 1.01
+    y = fp8.feed_forward(o, w_in, wd, workspace=ws)
+    g, u = (held(o) @ values(fp8.pack(m), D) for m in mats[4:6])
+    h = held((torch.nn.functional.silu(g) * u).float())
+    want = h @ values(wd, F)
+    assert (y.double() - want).norm() <= 5e-3 * want.norm()
