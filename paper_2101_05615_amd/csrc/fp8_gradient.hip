@@ -131,8 +131,9 @@ __global__ __launch_bounds__(256, TILE == 256 || PARTS > 1 ? 1 : 2) void qg_fp8_
   // what this thread fetches: columns c0 .. of both operands, tokens 8 * tb .. of a stage
   constexpr int CHUNKS = TILE / CW;
   const int c0 = t % CHUNKS * CW, tb = t / CHUNKS;
-  // (chunks that would end behind the last column end there: two threads bring the same columns, and what lies behind is never written)
-  const int cx = min(c0, p.x8.pitch - CW - row_tile * TILE), cy = max(min(c0, p.n - CW - column_tile * TILE), 0);
+  // (Chunks that would end behind the last column end there: two threads bring the same columns.  Those that so begin in front of a tile, which
+  // then has fewer columns than a chunk, are put behind its last one, where nothing is written.)
+  const int cx = min(c0, p.x8.pitch - CW - row_tile * TILE), cy = NARROW ? max(min(c0, p.n - CW), 0) : min(c0, p.n - CW - column_tile * TILE);
   const int xc = row_tile * TILE + cx, yc = column_tile * TILE + cy;
   typedef typename qg_elem<TYPE>::t T;
   // A thread requests its eight tokens of a stage wherever they are: those behind the last token are the last eight again, whose part that
@@ -186,7 +187,7 @@ __global__ __launch_bounds__(256, TILE == 256 || PARTS > 1 ? 1 : 2) void qg_fp8_
   };
   unsigned x_place[CW], y_place[CW];
 #pragma unroll
-  for (int k = 0; k < CW; ++k) x_place[k] = place_of(cx + k), y_place[k] = place_of(cy + k);
+  for (int k = 0; k < CW; ++k) x_place[k] = place_of(cx + k), y_place[k] = place_of((cy + k) & (TILE - 1));
   unsigned line[8], part[8][PARTS];
   auto place = [&](uint8_t* plane, unsigned to, unsigned a0, unsigned a1, unsigned a2, unsigned a3) {
     *reinterpret_cast<u4*>(plane + to) = (u4){a0, a1, a2, a3};
