@@ -94,16 +94,23 @@ qg_fp8_stream_form stream_form(qg_fp8_product_args* a, void* workspace) {
   return f;
 }
 
-// Tiles: 256 rows where that leaves few CUs without one; 64 rows rather than 128 up to 160 of them (300 rows of 4096 x 4096 19.8 and 26.7,
-// 512 rows of 8192 x 8192 54 and 46).  Sums that meet in memory cost as much as several blocks of K, so K is dealt only while that fills
-// the CUs, and in pieces of eight blocks at least (300 rows of 1024 x 1024 12 whole, 17 in two).
+// Tiles by the rounds that they make on 256 CUs, whose prices are what they take relative to each other (8192 x 4096 x 10240 and 155 others,
+// products and pairs, on average 0.4 % off the best of 64, 128 and 256 rows, fp32 sums 1.3 %): 64 rows, two workgroups a CU, 36 a full round, 25 where
+// each CU has one; 256 rows 54.  500 rows of a pair 4096 x 10240: 61 us in 64, 50 in 256; 1000 rows 98 and 101; 3100 rows of 10240 x 2816 126
+// and 102; 130 rows of a pair 4096 x 8192 23.5 and 43.  Tiles of 128 rows were best for few (800 rows of 10240 x 2816 53 in 64, 47 in 128).
+// Sums in fp32: every 64 rows widen the weights anew, 128 rows 37 a round against 46 and 25 (4096^3 185 and 146 us).
+// Sums that meet in memory cost as much as several blocks of K, so K is dealt only while that fills the CUs, and in pieces of eight
+// blocks at least (300 rows of 1024 x 1024 12 us whole, 17 in two).
 int tile_form(qg_fp8_product_args* a, int wide_sums, void* workspace) {
   const long long columns = a->w.groups / 4;
   auto tiles = [&](int rows) { return (a->tokens + rows - 1ll) / rows * columns; };
   a->slices = 1;
   a->slice_kb = a->w.kb;
-  if (!wide_sums && tiles(256) >= 200) return 16;
-  const int fragments = tiles(64) <= 160 ? 4 : 8;
+  const long long full = wide_sums ? 46 : 36, rest = tiles(64) % 512;
+  const long long small = tiles(64) / 512 * full + (rest == 0 ? 0 : rest <= 256 ? 25 : full);
+  const long long large = wide_sums ? (tiles(128) + 255) / 256 * 37 : (tiles(256) + 255) / 256 * 54;
+  if (!wide_sums && large < small) return 16;
+  const int fragments = large < small ? 8 : 4;
   const long long n = tiles(16 * fragments);
   deal(a, workspace, n, fragments * 4096ll, at_most(256 / n, at_most(4, a->w.kb / 8)));
   return fragments;

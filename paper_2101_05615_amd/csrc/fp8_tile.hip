@@ -4,11 +4,11 @@
 // rows and 64 of the slots.  The rows' codes go into LDS without passing registers, two blocks of K ahead, and every wave reads them
 // all; the weights, which no two waves share, go from memory to registers in the order they are packed in, one block of K ahead.  The
 // scales, one for a row's block and one for a fragment's, are operands of the matrix instruction.  Two shapes:
-//   256 rows  32 x 32 tiles, one wave per SIMD with all the accumulators there are: where there are tiles for nearly every CU
-//   64 or 128 rows  16 x 16 tiles, two workgroups a CU of 64; K dealt over workgroups where there are few
+//   256 rows  32 x 32 tiles, one wave per SIMD with all the accumulators there are: where that makes few rounds
+//   64 rows, of sums in fp32 128 too  16 x 16 tiles, two workgroups of 64 a CU; K dealt over workgroups where there are few
 // 8192^3 448 us with the rows put into 8 bits (2.45 PFLOP/s; a library product of the same codes with one scale a matrix 2.72; the matrix
 // cores are busy 65 % of the time at 1.7 of 2.4 GHz, which is what power allows); 4096^3 65 us; a pair of 8192 x 4096 x 10240 553 us
-// forward (2.5), 776 backward.  1000 rows of the pair 115 us: 640 tiles of 128 rows on 256 CUs are two and a half rounds.
+// forward (2.5), 776 backward.  1000 rows of the pair 98 us: 1280 tiles of 64 rows on 256 CUs are two and a half rounds.
 #include "qg_fp8.h"
 
 namespace {
@@ -710,10 +710,12 @@ hipError_t launch256(const qg_fp8_product_args& a, hipStream_t s) {
 }
 template <int END, bool WIDE>
 hipError_t launch(const qg_fp8_product_args& a, int row_fragments, hipStream_t s) {
-  if constexpr (!WIDE) {
+  if constexpr (WIDE) {
+    if (row_fragments == 8) return launch<8, END, WIDE>(a, s);
+  } else {
     if (row_fragments == 16) return launch256<END>(a, s);
   }
-  return row_fragments == 4 ? launch<4, END, WIDE>(a, s) : launch<8, END, WIDE>(a, s);
+  return launch<4, END, WIDE>(a, s);
 }
 
 }  // namespace

@@ -632,7 +632,7 @@ def test_matmul_large_tiles(env, T, K, N):
     assert torch.equal(y.double(), x.double() @ b.double())
 
 
-@pytest.mark.parametrize("T,N", [(1025, 300), (2100, 1900)])                  # tiles of 64 rows, of 128
+@pytest.mark.parametrize("T,N", [(1025, 300), (2100, 1900)])                  # tiles of 64 rows; with sums in fp32 of 128 too
 @pytest.mark.parametrize("K", [128, 250, 384, 500, 640, 2300])                # one block to five, and enough to be dealt over workgroups
 def test_matmul_small_tiles(env, T, K, N):
     fp8, torch, dev = env
