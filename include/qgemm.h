@@ -695,7 +695,7 @@ int qg_fp8_pack(const qg_matrix* b, const qg_matrix* up, int k, int n, int dtype
  * qg_gemm_workspace_init before its first use; every call leaves it ready for the next
  * one on the stream.  Calls that may overlap in time need one each.  NULL is allowed.
  * The result of a call is the same every time it is made with the same workspace
- * or without one. */
+ * or without one.  No call's result may overlap what the call reads. */
 #define QG_FP8_COUNTER_BYTES 16384
 #define QG_FP8_WORKSPACE_BYTES (QG_FP8_COUNTER_BYTES + (32 << 20))
 

@@ -482,6 +482,7 @@ struct activations {
   int64_t tokens, channels;
   int type;  // -1: blocks
   qg_rows raw;
+  const void* memory;  // of the tensor
 };
 bool of_activations(PyObject* o, activations* out) {
   const at::Tensor* const t = tensor(o);
@@ -492,8 +493,10 @@ bool of_activations(PyObject* o, activations* out) {
     out->tokens = t->size(0);
     out->channels = t->size(1);
     out->device = t->get_device();
+    out->memory = t->storage().data();
     return true;
   }
+  out->memory = nullptr;
   if (!old_blocks(o, &out->held)) return false;
   out->type = -1;
   out->options = out->held.codes.options();
@@ -544,7 +547,9 @@ bool of_workspace(PyObject* o, int64_t device, void** ws, size_t* bytes) {
   return true;
 }
 // The caller's output, or a new one; type: of a new one (-1: x's own, of blocks bfloat16).  As a new reference.
-PyObject* rows_output(PyObject* given, const activations& x, int n, int type, qg_fp8_product* p) {
+// *apart: whether it lies in other memory than x, which a kernel that takes x as it is reads while others of its workgroups write.
+PyObject* rows_output(PyObject* given, const activations& x, int n, int type, qg_fp8_product* p, bool* apart) {
+  *apart = true;
   if (given == Py_None) {
     if (type < 0) type = x.type < 0 ? QG_BF16 : x.type;
     const at::Tensor y = at::empty({x.tokens, n}, x.options.dtype(element_type(type)));
@@ -556,6 +561,7 @@ PyObject* rows_output(PyObject* given, const activations& x, int n, int type, qg
   if (!rows(t, &p->out) || !untracked(*t) || t->size(0) != x.tokens || t->size(1) != n || t->get_device() != x.device) return nullptr;
   p->dtype = element(t->scalar_type());
   if (type >= 0 && type != p->dtype) return nullptr;
+  *apart = t->storage().data() != x.memory;
   return Py_NewRef(given);
 }
 PyObject* pair_of(const at::Tensor& a, const at::Tensor* b) {  // (a, b or None)
@@ -681,11 +687,12 @@ PyObject* fp8_matmul(PyObject*, PyObject* const* a, Py_ssize_t n) {
         Py_RETURN_NONE;
       p.bias = static_cast<const float*>(bias->data_ptr());
     }
-    reference result{rows_output(a[4], x, w.c.n, type, &p)};
+    bool apart = true;
+    reference result{rows_output(a[4], x, w.c.n, type, &p, &apart)};
     if (!result.o) { PyErr_Clear(); Py_RETURN_NONE; }
     p.wide_sums = p.dtype == QG_F32;
     if (a[6] != Py_None && !truth(a[6], &p.wide_sums)) Py_RETURN_NONE;
-    int rc = into_product(&x, true, &p, s);
+    int rc = into_product(&x, apart, &p, s);
     if (rc != QG_OK) Py_RETURN_NONE;
     Py_BEGIN_ALLOW_THREADS
     rc = qg_fp8_matmul(&w.c, &p, s);
@@ -710,16 +717,17 @@ PyObject* fp8_gated(PyObject*, PyObject* const* a, Py_ssize_t n) {
         !of_workspace(a[5], x.device, &p.workspace, &p.workspace_bytes))
       Py_RETURN_NONE;
     const bool held = type == -2;
+    bool apart = true;
     reference result{nullptr};
     if (held) {
       if (a[4] != Py_None || !new_blocks(x.options, x.tokens, w.c.n, &to)) Py_RETURN_NONE;
     } else {
-      result.o = rows_output(a[4], x, w.c.n, type, &p);
+      result.o = rows_output(a[4], x, w.c.n, type, &p, &apart);
       if (!result.o) { PyErr_Clear(); Py_RETURN_NONE; }
       p.wide_sums = p.dtype == QG_F32;
     }
     if (a[6] != Py_None && !truth(a[6], &p.wide_sums)) Py_RETURN_NONE;
-    int rc = into_product(&x, !held, &p, s);
+    int rc = into_product(&x, !held && apart, &p, s);
     if (rc != QG_OK) Py_RETURN_NONE;
     Py_BEGIN_ALLOW_THREADS
     rc = qg_fp8_gated(&w.c, &p, held ? &to.c : nullptr, s);
@@ -745,7 +753,8 @@ PyObject* fp8_feed_forward(PyObject*, PyObject* const* a, Py_ssize_t n) {
         in.data.get_device() != x.device || down.data.get_device() != x.device || !here(x.device, &s) || !integer(a[3], &p.activation) ||
         (a[4] != Py_None && (!integer(a[4], &type) || type < QG_F32 || type > QG_F16)) || !of_workspace(a[6], x.device, &p.workspace, &p.workspace_bytes))
       Py_RETURN_NONE;
-    reference result{rows_output(a[5], x, down.c.n, type, &q)};
+    bool apart = true;  // (of no matter: the kernel that writes it starts when all of x has been read)
+    reference result{rows_output(a[5], x, down.c.n, type, &q, &apart)};
     if (!result.o) { PyErr_Clear(); Py_RETURN_NONE; }
     q.workspace = p.workspace;
     q.workspace_bytes = p.workspace_bytes;

@@ -240,7 +240,9 @@ def _product(x, w, dtype, activation=0, bias=None, ws=None, out=None, wide_sums=
         held = x
     else:
         _check_rows(x)
-        held = None if tokens <= FEW and k % 16 == 0 else quantize(x)
+        # (as it is, x is read while other workgroups write the result)
+        apart = out is None or out.untyped_storage().data_ptr() != x.untyped_storage().data_ptr()
+        held = None if tokens <= FEW and k % 16 == 0 and apart else quantize(x)
     if held is not None:
         p.x = held._desc
     else:
@@ -350,6 +352,7 @@ def weight_gradient(x, dy, dtype=None, out=None, workspace=None):
         else:
             _check_rows(o, x.shape[1], d.shape[1])
             assert o.dtype == dtype and o.device == d.device
+            assert all(o.untyped_storage().data_ptr() != t.untyped_storage().data_ptr() for t in dys), "the result may not lie in dy's memory"
         done.append(o)
     ws, size = None, 0
     if workspace is not None:

@@ -140,6 +140,31 @@ def test_captured_beside_a_live_graph(env):  # noqa: F811
     assert torch.equal(dx, want) and torch.equal(db.double(), x.double().t() @ dy.double())
 
 
+@pytest.mark.parametrize("T", [5, 16, 40, 300])
+def test_result_in_the_memory_of_x(env, T, monkeypatch):  # noqa: F811
+    """out = x: what x held is what counts."""
+    fp8, torch, dev = env
+    x, b, c = whole(torch, dev, T, 512).float(), whole(torch, dev, 512, 512, top=1).float(), whole(torch, dev, 512, 512, top=1).float()
+    w, pair, ws = fp8.pack(b), fp8.pack_gated(b, c), fp8.workspace(dev)
+    want, gated = (x.double() @ b.double()), (x.double() @ b.double()).clamp(min=0) * (x.double() @ c.double())
+    served = fp8.feed_forward(x, pair, w, "relu", workspace=ws)
+
+    class slow:
+        def __getattr__(self, name):
+            return (lambda *a: None) if name in ("fp8_matmul", "fp8_gated", "fp8_feed_forward") else getattr(binding, name)
+
+    binding = fp8._binding
+    for way in (binding, slow()):
+        monkeypatch.setattr(fp8, "_binding", way)
+        for call, result in ((lambda t: fp8.matmul(t, w, out=t, workspace=ws), want), (lambda t: fp8.gated(t, pair, "relu", out=t, workspace=ws), gated),
+                             (lambda t: fp8.feed_forward(t, pair, w, "relu", out=t, workspace=ws), served.double())):
+            t = x.clone()
+            assert call(t) is t and torch.equal(t.double(), result)
+        both = torch.zeros(512, 512, device=dev)
+        with pytest.raises(AssertionError, match="memory"):
+            fp8.weight_gradient(fp8.quantize(torch.zeros(512, 512, device=dev)), both, out=both)
+
+
 def test_a_decoder_step(env):  # noqa: F811
     """Projections in 8 bits around the 4-bit cache's attention, then the feed-forward block, of one new token per sequence: against the same
     steps in 64 bits from the values that each one has in hand."""
