@@ -97,7 +97,7 @@ __device__ inline void add_product(f16v& c, b8 a, b8 b) {
 // the result.  While a stage is multiplied the next one, which is in registers, goes to the other half of LDS, and the one after that is
 // requested: both in pieces between the matrix instructions, in whose shadow they cost little.
 //   256 x 256, one wave per SIMD: LDS is read 64 KiB a stage and half-filled once, 96 of its 128 bytes a cycle; a wave of 64 x 64 would read
-//   as much for a quarter of the products.  8192 x 4096 x 10240 685 us, 1.0 PFLOP/s, where a large bf16 library product reaches 1.27;
+//   as much for a quarter of the products.  8192 x 4096 x 10240 664 us, 1.03 PFLOP/s, where a large bf16 library product reaches 1.27;
 //   4096^3, one tile a CU, 140 us, 0.98.  What is left is the clock under this load (1.8 of 2.4 GHz) and waves that do all in turn.  128 x 128 and 64 x 64 where there are few tiles.
 // NARROW: fewer columns of dy than a thread brings at a time.
 template <int TILE, int TYPE, int PARTS, bool NARROW>
@@ -140,14 +140,19 @@ __global__ __launch_bounds__(256, TILE == 256 || PARTS > 1 ? 1 : 2) void qg_fp8_
   // other threads have becomes zeros on the way to LDS.  So every stage makes the same requests, and waits are for exactly those they mean.
   const int count = min(8, t1 - t0), back = t1 - count;
   struct tokens {  // this thread's part of a stage, on its way
-    unsigned x[8][CW / 4], scale[8];
+    unsigned x[8][CW / 4], scale;
     dy_line<TYPE, PARTS, CW> y[8];
   };
   tokens even, odd;
-  auto fetch = [&](tokens& to, int from, int i, int part) {  // of token i of this thread's eight of the stage that begins at `from`
-    const int shared = min(from, back), row = shared + min(i, count - 1);          // the same in all threads
-    const unsigned further = (unsigned)(min(from + 8 * tb, back) - shared);        // this thread's part
-    if (part == 0) {
+  // Request r of a stage that begins at `from`: codes of this thread's eight tokens, a scale, lines of dy.  The 16 lanes of a DPP row have columns of
+  // one block and the same tokens, so each brings one token's scale, and they pass them on to each other (777 x 1000 x 520
+  // fp32 19.9 us with a request a token, 18.4 so).
+  static_assert(16 * CW <= QG_FP8_BLOCK, "a block");
+  constexpr int REQUESTS = 17;
+  auto fetch = [&](tokens& to, int from, int r) {
+    const int shared = min(from, back), i = r % 8, row = shared + min(i, count - 1);   // the same in all threads
+    const unsigned further = (unsigned)(min(from + 8 * tb, back) - shared);            // this thread's part
+    if (r < 8) {
       const uint8_t* const src = p.x8.codes + (long long)row * p.x8.pitch + (further * (unsigned)p.x8.pitch + (unsigned)xc);
       if constexpr (CW == 8) {
         const u2 v = from_memory<u2>(src);
@@ -156,14 +161,16 @@ __global__ __launch_bounds__(256, TILE == 256 || PARTS > 1 ? 1 : 2) void qg_fp8_
       } else {
         to.x[i][0] = from_memory<unsigned>(src);
       }
-    } else if (part == 1) {
-      to.scale[i] = from_memory<uint8_t>(p.x8.scales + (long long)row * p.x8.scale_pitch + (further * (unsigned)p.x8.scale_pitch + (unsigned)(xc / QG_FP8_BLOCK)));
+    } else if (r == 8) {
+      to.scale = from_memory<uint8_t>(p.x8.scales + (long long)shared * p.x8.scale_pitch +
+                                      ((further + (unsigned)min(lane & 7, count - 1)) * (unsigned)p.x8.scale_pitch + (unsigned)(xc / QG_FP8_BLOCK)));
     } else {
-      const T* const line = static_cast<const T*>(dy.data) + (further * dy.stride + yc) + row * dy.stride;
+      const int j = r - 9, line_row = shared + min(j, count - 1);
+      const T* const line = static_cast<const T*>(dy.data) + (further * dy.stride + yc) + line_row * dy.stride;
       if constexpr (NARROW) {
-        to.y[i].load_some(line, p.n - 1);
+        to.y[j].load_some(line, p.n - 1);
       } else {
-        to.y[i].load(line);
+        to.y[j].load(line);
       }
     }
   };
@@ -174,9 +181,9 @@ __global__ __launch_bounds__(256, TILE == 256 || PARTS > 1 ? 1 : 2) void qg_fp8_
       const bool keep = i >= skip && i < count;
 #pragma unroll
       for (int k = 0; k < CW / 4; ++k) of.x[i][k] = keep ? of.x[i][k] : 0u;
-      of.scale[i] = keep ? of.scale[i] : 0u;
       of.y[i].keep(keep);
     }
+    of.scale = (lane & 7) >= skip && (lane & 7) < count ? of.scale : 0u;
   };
   // A stage's planes: [32 columns][TS / 16 steps][2 halves of 8 tokens][32 columns, turned about][8 tokens]: 8 lanes, or 16, whose 16 bytes are
   // written or read at a time go through all banks.  Two columns of this thread's eight tokens go there in SLICES pieces.
@@ -189,6 +196,14 @@ __global__ __launch_bounds__(256, TILE == 256 || PARTS > 1 ? 1 : 2) void qg_fp8_
 #pragma unroll
   for (int k = 0; k < CW; ++k) x_place[k] = place_of(cx + k), y_place[k] = place_of((cy + k) & (TILE - 1));
   unsigned line[8], part[8][PARTS];
+  float power[8];
+  auto spread = [&](const tokens& of) {  // the scales of this thread's eight tokens
+    const int mine = __builtin_bit_cast(int, scale_of(of.scale));
+    each<0, 8>([&](auto token) {
+      constexpr int i = decltype(token)::value;
+      power[i] = __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, mine, 0x150 + i, 0xf, 0xf, false));  // row_newbcast
+    });
+  };
   auto place = [&](uint8_t* plane, unsigned to, unsigned a0, unsigned a1, unsigned a2, unsigned a3) {
     *reinterpret_cast<u4*>(plane + to) = (u4){a0, a1, a2, a3};
   };
@@ -199,7 +214,7 @@ __global__ __launch_bounds__(256, TILE == 256 || PARTS > 1 ? 1 : 2) void qg_fp8_
       for (int i = 0; i < 4; ++i) {
         const int k = slice % 2 * 4 + i;
         if (slice < 2) {
-          line[k] = widened(of.x[k][pair / 2], scale_of(of.scale[k]), pair & 1);
+          line[k] = widened(of.x[k][pair / 2], power[k], pair & 1);
         } else {
           of.y[k].split(pair, part[k]);
         }
@@ -247,7 +262,7 @@ __global__ __launch_bounds__(256, TILE == 256 || PARTS > 1 ? 1 : 2) void qg_fp8_
   };
   auto fetch_all = [&](tokens& to, int from) {
 #pragma unroll
-    for (int i = 0; i < 24; ++i) fetch(to, from, i / 3, i % 3);
+    for (int r = 0; r < REQUESTS; ++r) fetch(to, from, r);
     __builtin_amdgcn_sched_barrier(0);  // (in this order, or the loop waits for more than it needs)
   };
   auto multiply = [&](auto which, tokens& next, int from) {
@@ -256,6 +271,7 @@ __global__ __launch_bounds__(256, TILE == 256 || PARTS > 1 ? 1 : 2) void qg_fp8_
     uint8_t* const other = lds + (1 - now) * STAGE;
     const int ahead = from + 3 * TS;
     if (from + 2 * TS > t1) clear(next, from + TS);
+    spread(next);
     // The matrix instructions, one by one: first with pieces of the next stage's way to LDS, then with the requests that take its registers
     each<0, PRODUCTS>([&](auto number) {
       constexpr int n = decltype(number)::value, group = n / (PARTS * F), q = n / F % PARTS, i = n % F, s = group / F, j = group % F;
@@ -283,8 +299,8 @@ __global__ __launch_bounds__(256, TILE == 256 || PARTS > 1 ? 1 : 2) void qg_fp8_
           store(next, other, e / SLICES, e % SLICES);
         });
       } else if constexpr (n < MOVE + REQUEST) {
-        constexpr int first = (n - MOVE) * 24 / REQUEST, last = (n - MOVE + 1) * 24 / REQUEST;
-        each<first, last>([&](auto number) { fetch(next, ahead, decltype(number)::value / 3, decltype(number)::value % 3); });
+        constexpr int first = (n - MOVE) * REQUESTS / REQUEST, last = (n - MOVE + 1) * REQUESTS / REQUEST;
+        each<first, last>([&](auto number) { fetch(next, ahead, decltype(number)::value); });
       }
       add_product(c[i][j], g[(RING0 + group) % 3][q], x[s % X_RING][i]);
       __builtin_amdgcn_sched_barrier(0);
@@ -294,6 +310,7 @@ __global__ __launch_bounds__(256, TILE == 256 || PARTS > 1 ? 1 : 2) void qg_fp8_
   fetch_all(even, t0);
   fetch_all(odd, t0 + TS);
   if (t0 + TS > t1) clear(even, t0);
+  spread(even);
 #pragma unroll
   for (int u = 0; u < PAIRS; ++u)
 #pragma unroll
